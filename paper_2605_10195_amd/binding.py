@@ -90,6 +90,14 @@ SCHED_EXPORTS = [
     "spex_sched_allocate_budget", "spex_sched_early_termination", "spex_tree_path_kv_bytes",
 ]
 
+# spex_prompt.h: attention over whole prompts
+PROMPT_EXPORTS = ["spex_prompt_attention"]
+
+
+class PromptConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("num_q_heads", "num_kv_heads", "head_dim", "dtype")] + \
+               [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride", "out_stride")]
+
 
 class SearchTreeView(C.Structure):
     _fields_ = [("n_nodes", C.c_int32), ("parent", C.POINTER(C.c_int32)), ("visits", C.POINTER(C.c_int64)),
@@ -141,7 +149,8 @@ def _load():
     lib.spex_sched_allocate_budget.argtypes = [_I32P, _F64P, _F64P, i32, C.c_double, C.c_double, i32, _I32P, _F64P]
     lib.spex_sched_early_termination.argtypes = [_I32P, _F64P, i32, i32, C.c_double, _I32P, _I32P]
     lib.spex_tree_path_kv_bytes.argtypes = [vp, i32, _F64P]
-    for name in EXPORTS + SCHED_EXPORTS:
+    lib.spex_prompt_attention.argtypes = [C.POINTER(PromptConfig), ip, i32, vp, vp, vp, vp, vp, f32, vp]
+    for name in EXPORTS + SCHED_EXPORTS + PROMPT_EXPORTS:
         fn = getattr(lib, name)
         if name not in ("spex_status_string", "spex_last_device_error", "spex_tree_destroy"):
             fn.restype = C.c_int
@@ -517,6 +526,49 @@ def spex_tree_decode_attention_masked(tree: SpexTree, leaves, q_lens, draft_mask
 
 def spex_tree_append_tokens_quantize(tree: SpexTree, nodes, k, v, k_scales, v_scales) -> None:
     tree.append_tokens(nodes, k, v, k_scales, v_scales, quantize=True)
+
+
+# ---- spex_prompt.h -------------------------------------------------------------------------
+def _token_stride(t: torch.Tensor, heads: int, dim: int) -> int:
+    """Elements between tokens of [tokens, heads, dim]; the heads of a token must be dense."""
+    assert t.dim() == 3 and t.shape[1:] == (heads, dim), t.shape
+    assert (dim == 1 or t.stride(2) == 1) and (heads == 1 or t.stride(1) == dim), "the heads of a token must be contiguous"
+    if t.shape[0] <= 1:
+        return 0
+    assert t.stride(0) >= heads * dim, "tokens must not overlap"
+    return t.stride(0)
+
+
+def _on_current_device(*tensors: Optional[torch.Tensor]) -> bool:
+    """The calls run on the current stream of the current device."""
+    here = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None
+    return all(t is None or (t.is_cuda and t.get_device() == here) for t in tensors)
+
+
+def spex_prompt_attention(lens: Sequence[int], q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sm_scale: float,
+                          out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = True):
+    """Causal attention over packed prompts: q [tokens, Hq, D], k and v [tokens, Hkv, D] in float32 or bfloat16, dense or with
+    a stride between tokens (parts of one projection); out has q's shape and type.  Returns (out, lse)."""
+    la = _i32(lens)
+    total, hq, dim = q.shape
+    hkv = k.shape[1]
+    assert q.dtype in (torch.float32, torch.bfloat16) and k.dtype == q.dtype and v.dtype == q.dtype
+    assert k.shape[0] == total and v.shape[0] == total and int(la.sum(dtype=np.int64)) == total
+    if out is None:
+        out = torch.empty((total, hq, dim), dtype=q.dtype, device=q.device)
+    assert out.dtype == q.dtype and out.shape == q.shape
+    if lse is None and want_lse:
+        lse = torch.empty((total, hq), dtype=torch.float32, device=q.device)
+    assert lse is None or (lse.dtype == torch.float32 and lse.shape == (total, hq) and lse.is_contiguous())
+    assert _on_current_device(q, k, v, out, lse), "all tensors must lie on the current device"
+    cfg = PromptConfig(hq, hkv, dim, F32 if q.dtype == torch.float32 else BF16, _token_stride(q, hq, dim), _token_stride(k, hkv, dim),
+                       _token_stride(v, hkv, dim), _token_stride(out, hq, dim))
+    _check(lib.spex_prompt_attention(C.byref(cfg), _addr(la), len(la), _dev(q), _dev(k), _dev(v), _dev(out), _dev(lse),
+                                     float(sm_scale), _stream()))
+    return out, lse
+
+
+prompt_attention = spex_prompt_attention
 
 
 # ---- spex_sched.h: argument marshalling only ------------------------------------------------

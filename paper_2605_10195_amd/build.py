@@ -9,7 +9,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libspex_tree.so")
-SOURCES = ["api.cpp", "page_table.cpp", "planner.cpp", "sched.cpp", "kernels.hip"]
+SOURCES = ["api.cpp", "page_table.cpp", "planner.cpp", "sched.cpp", "prompt.cpp"]
+KERNELS = ["kernels.hip", "prompt.hip"]
 
 
 def hipcc() -> str:
@@ -40,11 +41,14 @@ def build_library(verbose: bool = False) -> str:
     # integer compares and never by NaN tests, and without the flag every fmaxf on an MFMA result
     # costs an extra instruction that quiets a NaN which cannot occur.  Host code keeps NaN
     # semantics (argument checks rely on them).
-    kernels_obj = os.path.join(HERE, "kernels.o")
-    _run(common + ["-fno-honor-nans", "-c", os.path.join(CSRC, "kernels.hip"), "-o", kernels_obj], verbose)
-    host = [os.path.join(CSRC, s) for s in SOURCES if s != "kernels.hip"]
-    _run(common + ["-shared"] + host + ["-x", "none", kernels_obj, "-o", LIB_PATH], verbose)
-    os.remove(kernels_obj)
+    objects = []
+    for src in KERNELS:
+        objects.append(os.path.join(HERE, src.replace(".hip", ".o")))
+        _run(common + ["-fno-honor-nans", "-c", os.path.join(CSRC, src), "-o", objects[-1]], verbose)
+    host = [os.path.join(CSRC, s) for s in SOURCES]
+    _run(common + ["-shared"] + host + ["-x", "none"] + objects + ["-o", LIB_PATH], verbose)
+    for obj in objects:
+        os.remove(obj)
     return LIB_PATH
 
 

@@ -18,14 +18,20 @@
 #include "planner.hpp"
 
 namespace {
-
 thread_local std::string g_last_error;
+}  // namespace
 
+namespace spex {
 bool hip_failed(hipError_t e, const char *what) {
   if (e == hipSuccess) return false;
   g_last_error = std::string(what) + ": " + hipGetErrorString(e);
   return true;
 }
+}  // namespace spex
+
+namespace {
+
+using spex::hip_failed;
 
 #define HIP_TRY(expr)                                      \
   do {                                                     \

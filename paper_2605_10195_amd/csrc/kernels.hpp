@@ -11,6 +11,9 @@ namespace spex {
 
 enum Dtype : int32_t { kF32 = 0, kBF16 = 1, kFP8 = 2 };
 
+// Whether a HIP call failed; the error's text is then what spex_last_device_error tells this thread.  In api.cpp.
+bool hip_failed(hipError_t e, const char *what);
+
 // Element arrangement inside a (page, kv head) tile; see the pool layout in spex_tree.h.
 enum Layout : int32_t { kRowMajor = 0, kMfmaTiled = 1 };
 

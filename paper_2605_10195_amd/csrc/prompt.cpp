@@ -1,0 +1,111 @@
+// spex_prompt_attention: argument checks and the lists of its launches.  See include/spex_prompt.h.
+#include "../../include/spex_prompt.h"
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "kernels.hpp"
+#include "prompt.hpp"
+
+namespace {
+
+constexpr int32_t kMaxPromptTokens = 1 << 24;
+// Workgroups of a launch: with 256 threads each, a launch stays below 2^32 threads.
+constexpr int64_t kMaxLaunchGroups = int64_t(1) << 23;
+
+bool aligned16(const void *x) { return (reinterpret_cast<uintptr_t>(x) & 15) == 0; }
+
+}  // namespace
+
+extern "C" spex_status_t spex_prompt_attention(const spex_prompt_config_t *cfg, const int32_t *lens, int32_t n_prompts,
+                                               const void *q, const void *k, const void *v, void *out, float *lse,
+                                               float sm_scale, void *hip_stream) {
+  if (!cfg || n_prompts < 0 || (n_prompts > 0 && !lens)) return SPEX_ERR_INVALID_ARG;
+  if (cfg->num_q_heads <= 0 || cfg->num_kv_heads <= 0 || cfg->num_kv_heads > 255 || cfg->num_q_heads % cfg->num_kv_heads != 0 ||
+      cfg->head_dim < 1 || cfg->head_dim > 256)
+    return SPEX_ERR_INVALID_ARG;
+  if (cfg->dtype != SPEX_F32 && cfg->dtype != SPEX_BF16) return SPEX_ERR_UNSUPPORTED;
+  if (!(sm_scale > 0.f) || std::isinf(sm_scale)) return SPEX_ERR_INVALID_ARG;
+  const int64_t q_row = static_cast<int64_t>(cfg->num_q_heads) * cfg->head_dim;
+  const int64_t kv_row = static_cast<int64_t>(cfg->num_kv_heads) * cfg->head_dim;
+  const int64_t strides[4] = {cfg->q_stride ? cfg->q_stride : q_row, cfg->k_stride ? cfg->k_stride : kv_row,
+                              cfg->v_stride ? cfg->v_stride : kv_row, cfg->out_stride ? cfg->out_stride : q_row};
+  if (strides[0] < q_row || strides[1] < kv_row || strides[2] < kv_row || strides[3] < q_row) return SPEX_ERR_INVALID_ARG;
+  for (int64_t s : strides)
+    if (s > INT32_MAX) return SPEX_ERR_UNSUPPORTED;
+  int64_t total = 0;
+  for (int32_t i = 0; i < n_prompts; ++i) {
+    if (lens[i] < 0) return SPEX_ERR_INVALID_ARG;
+    if (lens[i] > kMaxPromptTokens) return SPEX_ERR_UNSUPPORTED;
+    total += lens[i];
+  }
+  if (total > INT32_MAX) return SPEX_ERR_UNSUPPORTED;
+  if (total == 0) return SPEX_OK;
+  if (!q || !k || !v || !out) return SPEX_ERR_INVALID_ARG;
+
+  const int64_t per16 = cfg->dtype == SPEX_F32 ? 4 : 8;
+  bool wide = cfg->head_dim % per16 == 0 && aligned16(q) && aligned16(k) && aligned16(v) && aligned16(out);
+  for (int64_t s : strides) wide = wide && s % per16 == 0;
+  const spex::PromptKernel kernel = spex::prompt_kernel(cfg->dtype == SPEX_F32, wide);
+  const int32_t G = cfg->num_q_heads / cfg->num_kv_heads;
+
+  struct Prompt {
+    int32_t start, len;
+  };
+  Prompt few[64], *list = few;
+  std::vector<Prompt> many;
+  try {
+    if (n_prompts > 64) {
+      many.resize(static_cast<size_t>(n_prompts));
+      list = many.data();
+    }
+  } catch (const std::bad_alloc &) {
+    return SPEX_ERR_CAPACITY;
+  }
+  int32_t n = 0, at = 0;
+  for (int32_t i = 0; i < n_prompts; ++i) {
+    if (lens[i] > 0) {
+      list[n++] = {at, lens[i]};
+      if (spex::prompt_items(kernel, G, lens[i]) * cfg->num_kv_heads > kMaxLaunchGroups) return SPEX_ERR_UNSUPPORTED;
+    }
+    at += lens[i];
+  }
+  // Longest first: the workgroups with most work start first, within a prompt and over all of them.
+  std::sort(list, list + n, [](const Prompt &a, const Prompt &b) { return a.len != b.len ? a.len > b.len : a.start < b.start; });
+
+  spex::PromptArgs a;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.out = out;
+  a.lse = lse;
+  a.q_stride = strides[0];
+  a.k_stride = strides[1];
+  a.v_stride = strides[2];
+  a.out_stride = strides[3];
+  a.scale_log2 = sm_scale * 1.4426950408889634f;
+  a.Hkv = cfg->num_kv_heads;
+  a.G = G;
+  a.D = cfg->head_dim;
+  for (int32_t i = 0; i < n;) {
+    int64_t items = 0;
+    a.n = 0;
+    for (; i < n && a.n < spex::kMaxPromptsPerLaunch; ++i, ++a.n) {
+      const int64_t more = spex::prompt_items(kernel, G, list[i].len);
+      if ((items + more) * cfg->num_kv_heads > kMaxLaunchGroups) break;
+      a.first[a.n] = static_cast<int32_t>(items);
+      a.start[a.n] = list[i].start;
+      a.len[a.n] = list[i].len;
+      items += more;
+    }
+    for (int32_t j = a.n; j < spex::kMaxPromptsPerLaunch; ++j) {
+      a.first[j] = INT32_MAX;
+      a.start[j] = a.len[j] = 0;
+    }
+    if (spex::hip_failed(spex::launch_prompt(kernel, a, items, static_cast<hipStream_t>(hip_stream)), "launch_prompt"))
+      return SPEX_ERR_DEVICE;
+  }
+  return SPEX_OK;
+}

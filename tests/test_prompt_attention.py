@@ -1,0 +1,242 @@
+"""spex_prompt_attention: refusals on the CPU (nothing is launched), values on the GPU against the definition in 64 bits."""
+
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_10195_amd as spex
+from paper_2605_10195_amd import binding
+
+OK, INVALID, UNSUPPORTED = 0, 1, 6
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+# ---- refusals, on the CPU: every call ends before a launch -----------------------------------------
+def call(lens, heads=(4, 2, 64), dtype=binding.BF16, strides=(0, 0, 0, 0), scale=0.125, pointers=(64, 64, 64, 64), n=None, cfg=True):
+    la = np.asarray(lens, dtype=np.int32)
+    c = binding.PromptConfig(*heads, dtype, *strides)
+    return binding.lib.spex_prompt_attention(C.byref(c) if cfg else None, la.ctypes.data if lens is not None else None,
+                                             len(la) if n is None else n, *pointers, None, scale, None)
+
+
+@pytest.mark.parametrize("want,kw", [
+    (INVALID, dict(lens=[3], cfg=False)), (INVALID, dict(lens=[3], n=-1)), (INVALID, dict(lens=[3, -1])),
+    (INVALID, dict(lens=[3], heads=(5, 2, 64))), (INVALID, dict(lens=[3], heads=(4, 0, 64))), (INVALID, dict(lens=[3], heads=(256, 256, 64))),
+    (INVALID, dict(lens=[3], heads=(4, 2, 0))), (INVALID, dict(lens=[3], heads=(4, 2, 257))),
+    (INVALID, dict(lens=[3], scale=0.0)), (INVALID, dict(lens=[3], scale=-1.0)), (INVALID, dict(lens=[3], scale=float("nan"))),
+    (INVALID, dict(lens=[3], scale=float("inf"))),
+    (INVALID, dict(lens=[3], strides=(255, 0, 0, 0))), (INVALID, dict(lens=[3], strides=(0, 127, 0, 0))),
+    (INVALID, dict(lens=[3], strides=(0, 0, -128, 0))), (INVALID, dict(lens=[3], strides=(0, 0, 0, 255))),
+    (INVALID, dict(lens=[3], pointers=(None, 64, 64, 64))), (INVALID, dict(lens=[3], pointers=(64, None, 64, 64))),
+    (INVALID, dict(lens=[3], pointers=(64, 64, None, 64))), (INVALID, dict(lens=[3], pointers=(64, 64, 64, None))),
+    (UNSUPPORTED, dict(lens=[3], dtype=binding.FP8_E4M3)), (UNSUPPORTED, dict(lens=[(1 << 24) + 1])),
+    (UNSUPPORTED, dict(lens=[1 << 24] * 128)), (UNSUPPORTED, dict(lens=[3], strides=(1 << 31, 0, 0, 0))),
+    (UNSUPPORTED, dict(lens=[1 << 24], heads=(4096, 1, 64))),
+    (OK, dict(lens=[])), (OK, dict(lens=[0, 0])), (OK, dict(lens=[0], pointers=(None, None, None, None))),
+])
+def test_arguments_are_checked_before_anything_is_launched(want, kw):
+    assert call(**kw) == want
+
+
+def test_binding_refuses_tensors_that_it_cannot_describe():
+    q, k = torch.zeros(3, 4, 64, dtype=torch.bfloat16), torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(AssertionError):                   # not on a GPU
+        spex.prompt_attention([3], q, k, k, 0.125)
+    for bad in (dict(lens=[2], q=q, k=k, v=k), dict(lens=[3], q=q, k=k.float(), v=k), dict(lens=[3], q=q, k=k, v=k[:2]),
+                dict(lens=[3], q=q[:1].expand(3, 4, 64), k=k, v=k), dict(lens=[3], q=q, k=k.transpose(1, 2), v=k),
+                dict(lens=[3], q=q.half(), k=k.half(), v=k.half())):
+        with pytest.raises(AssertionError):
+            spex.prompt_attention(bad["lens"], bad["q"], bad["k"], bad["v"], 0.125)
+
+
+# ---- values --------------------------------------------------------------------------------------
+def inputs(lens, heads, dtype, seed=0, fused=False, shift=0, spread=2.0):
+    hq, hkv, d = heads
+    t = sum(lens)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    if fused:
+        x = torch.randn((t, hq + 2 * hkv, d), generator=g, device="cuda")
+        x[:, :hq] *= spread
+        x = x.to(TYPES[dtype])
+        return x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:]
+
+    def one(h, mult):
+        x = (torch.randn((t * h * d + shift,), generator=g, device="cuda") * mult).to(TYPES[dtype])
+        return x[shift:].view(t, h, d)
+    return one(hq, spread), one(hkv, 1.0), one(hkv, 1.0)
+
+
+def reference(lens, q, k, v, scale):
+    """out, lse, the weighted mean of |v|, the largest |score| and the largest sum |q_d k_d| * scale of every row, in 64 bits."""
+    hq, hkv = q.shape[1], k.shape[1]
+    q, k, v = q.double().cpu(), k.double().cpu(), v.double().cpu()
+    outs, at = [], 0
+    for n in (x for x in lens if x):
+        qs, ks, vs = (x[at:at + n].transpose(0, 1) for x in (q, k, v))
+        ks, vs = ks.repeat_interleave(hq // hkv, 0), vs.repeat_interleave(hq // hkv, 0)
+        x = scale * (qs @ ks.transpose(1, 2)).masked_fill(torch.ones(n, n).triu(1).bool(), -torch.inf)
+        lse = torch.logsumexp(x, -1)
+        w = torch.exp(x - lse[..., None])
+        top = torch.where(torch.isinf(x), torch.zeros(()).double(), x.abs()).amax(-1)
+        sums = scale * (qs.abs() @ ks.abs().transpose(1, 2)).amax(-1)
+        outs.append([(w @ vs).transpose(0, 1), lse.t(), (w @ vs.abs()).transpose(0, 1), top.t(), sums.t()])
+        at += n
+    return [torch.cat(z).numpy() for z in zip(*outs)]
+
+
+def check(lens, q, k, v, out, lse, scale):
+    """Error bounds by counting roundings (half a step: bf16 2^-8, fp32 2^-24).
+    A score: a sum of D products in fp32, off by at most D 2^-24 sum|q_d k_d|; scale, log2(e) and the difference to the
+    reference point round it a few times more, 4 * 2^-24 of |score| + 8 (the slack of the reference point, in log2).
+    A weight 2^x: that error times ln 2 each way, relative, plus 2 steps of the exponential; so out is off by at most twice
+    that (numerator and denominator) plus n 2^-24 for each of the two sums, of the weighted mean of |v|.
+    bf16: every weight is rounded once more by 2^-8, and the result."""
+    ref, ref_lse, mean, top, sums = reference(lens, q, k, v, scale)
+    d, n = q.shape[2], max(lens)
+    score = (d + 2) * 2.0 ** -24 * sums + 4 * 2.0 ** -24 * (1.45 * top + 24)
+    rel = 2 * (score + 4 * 2.0 ** -24 + n * 2.0 ** -24)
+    got = out.double().cpu().numpy()
+    assert np.all(np.isfinite(got))
+    half = 2.0 ** -8 if out.dtype == torch.bfloat16 else 2.0 ** -24
+    bound = rel[..., None] * mean + half * np.abs(ref) * 1.01 + (half * mean * 1.01 if out.dtype == torch.bfloat16 else 2 * half * mean)
+    worst = float(np.max(np.abs(got - ref) / bound))
+    assert worst <= 1.0, worst
+    if lse is not None:
+        off = np.abs(lse.double().cpu().numpy() - ref_lse) / (score + (n + 4) * 2.0 ** -24 + 4 * 2.0 ** -24 * (np.abs(ref_lse) + 8))
+        assert float(np.max(off)) <= 1.0, float(np.max(off))
+
+
+HEADS = [(8, 2, 64), (8, 8, 128), (7, 1, 128), (10, 2, 96), (4, 1, 256), (6, 3, 40), (32, 4, 128), (4, 2, 192), (2, 1, 8)]
+LENS = [[1], [2, 1], [31, 32, 33], [64], [65, 0, 63, 1], [130, 7], [300]]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads", HEADS, ids=str)
+@pytest.mark.parametrize("lens", LENS, ids=str)
+def test_against_the_definition(dtype, heads, lens):
+    q, k, v = inputs(lens, heads, dtype, seed=len(lens) + heads[2])
+    out, lse = spex.prompt_attention(lens, q, k, v, heads[2] ** -0.5)
+    check(lens, q, k, v, out, lse, heads[2] ** -0.5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,heads", [([700, 129, 511], (16, 4, 128)), ([1025], (4, 1, 64)), ([1500], (2, 2, 256)), ([640, 640], (5, 1, 96))], ids=str)
+@pytest.mark.parametrize("fused", [False, True])
+def test_longer_prompts(dtype, lens, heads, fused):
+    q, k, v = inputs(lens, heads, dtype, seed=3, fused=fused)
+    out, lse = spex.prompt_attention(lens, q, k, v, heads[2] ** -0.5)
+    check(lens, q, k, v, out, lse, heads[2] ** -0.5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,shift", [((4, 2, 64), 1), ((4, 2, 7), 0), ((3, 1, 130), 0), ((2, 2, 1), 0), ((4, 1, 250), 3)], ids=str)
+def test_rows_that_are_not_made_of_16_byte_pieces(dtype, heads, shift):
+    lens = [70, 1, 33]
+    q, k, v = inputs(lens, heads, dtype, seed=5, shift=shift)
+    out, lse = spex.prompt_attention(lens, q, k, v, heads[2] ** -0.5)
+    check(lens, q, k, v, out, lse, heads[2] ** -0.5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_only_the_prompts_rows_are_written_and_strides_are_kept(dtype):
+    """out and the inputs are windows of larger tensors; everything around the windows stays as it was, and q, k and v around them
+    hold NaN, which nothing may read into a result."""
+    lens, (hq, hkv, d) = [37, 5, 64], (4, 2, 64)
+    t = sum(lens)
+    want = [torch.full((t + 70, h + 2, d), float("nan"), dtype=TYPES[dtype], device="cuda") for h in (hq, hkv, hkv)]
+    views = [x[3:3 + t, 1:1 + h] for x, h in zip(want, (hq, hkv, hkv))]
+    for view, x in zip(views, inputs(lens, (hq, hkv, d), dtype, seed=6)):
+        view.copy_(x)
+    big = torch.full((t + 70, hq + 2, d), 9.0, dtype=TYPES[dtype], device="cuda")
+    lse = torch.full((t + 3, hq), 9.0, device="cuda")
+    spex.prompt_attention(lens, *views, 0.125, out=big[3:3 + t, 1:1 + hq], lse=lse[:t])
+    check(lens, *views, big[3:3 + t, 1:1 + hq], lse[:t], 0.125)
+    big[3:3 + t, 1:1 + hq] = 9.0
+    assert bool((big == 9.0).all()) and bool((lse[t:] == 9.0).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [127, 128, 129, 300])
+def test_many_prompts_take_several_launches(n):
+    lens = [(i * 7) % 23 for i in range(n)]
+    q, k, v = inputs(lens, (4, 2, 64), "bf16", seed=n)
+    out, lse = spex.prompt_attention(lens, q, k, v, 0.125)
+    check(lens, q, k, v, out, lse, 0.125)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("what", ["rising", "falling", "far", "flat", "huge"])
+def test_scores_that_move_the_running_maximum(dtype, what):
+    """Keys whose scores rise along the prompt (the maximum moves in every tile), fall, lie far below or above zero, are all equal,
+    or spread so far that one key takes all the weight."""
+    lens, (hq, hkv, d) = [400], (4, 2, 64)
+    q, k, v = (x.float() for x in inputs(lens, (hq, hkv, d), dtype, seed=8, spread=1.0))
+    if what == "flat":
+        k.zero_()
+    else:
+        q[..., 0] = 8.0
+        pos = torch.arange(400, device="cuda")[:, None].float()
+        k[..., 0] += {"rising": pos * 0.25, "falling": -pos * 0.25, "far": torch.full_like(pos, -200.0), "huge": 50.0 * (pos % 7)}[what]
+    q, k, v = (x.to(TYPES[dtype]) for x in (q, k, v))
+    out, lse = spex.prompt_attention(lens, q, k, v, 0.5)
+    check(lens, q, k, v, out, lse, 0.5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_captured_replayed_and_on_another_stream(dtype):
+    lens = [200, 31, 90]
+    q, k, v = inputs(lens, (8, 2, 128), dtype, seed=9)
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        spex.prompt_attention(lens, q, k, v, 0.1, out=out, lse=lse)
+    torch.cuda.current_stream().wait_stream(side)
+    check(lens, q, k, v, out, lse, 0.1)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        spex.prompt_attention(lens, q, k, v, 0.1, out=out, lse=lse)
+    for seed in (10, 11, 12):
+        for x, y in zip((q, k, v), inputs(lens, (8, 2, 128), dtype, seed=seed)):
+            x.copy_(y)
+        graph.replay()
+        eager, eager_lse = spex.prompt_attention(lens, q, k, v, 0.1)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager) and torch.equal(lse, eager_lse)
+        check(lens, q, k, v, out, lse, 0.1)
+
+
+@pytest.mark.gpu
+def test_same_result_every_time_and_without_lse():
+    lens = [513, 70]
+    q, k, v = inputs(lens, (8, 2, 128), "bf16", seed=13)
+    first, lse = spex.prompt_attention(lens, q, k, v, 0.1)
+    for _ in range(3):
+        again, none = spex.prompt_attention(lens, q, k, v, 0.1, want_lse=False)
+        assert none is None and torch.equal(first, again)
+
+
+@pytest.mark.gpu
+def test_equals_decode_attention_over_the_appended_prompt():
+    """The same prompt through the page pool: both are within their bounds of the definition, hence of each other."""
+    lens, (hq, hkv, d) = [150, 64], (8, 2, 128)
+    q, k, v = inputs(lens, (hq, hkv, d), "bf16", seed=14)
+    out, lse = spex.prompt_attention(lens, q, k, v, d ** -0.5)
+    tree = spex.SpexTree(hq, hkv, d, num_pages=20, device="cuda")
+    roots, at = tree.fork(-1, 2), 0
+    for u, n in zip(roots, lens):
+        tree.append_step(u, k[at:at + n].contiguous(), v[at:at + n].contiguous())
+        at += n
+    ref, ref_lse = tree.decode_attention(roots, lens, q, d ** -0.5)
+    # 2^-8 of the weighted mean of |v| and of the result (here), 2e-3 (there)
+    bound = 2.0 ** -8 * 1.01 * (torch.as_tensor(reference(lens, q, k, v, d ** -0.5)[2], device="cuda") + ref.abs().double()) + 2e-3
+    assert bool(((out.double() - ref.double()).abs() <= bound).all()) and float((lse - ref_lse).abs().max()) <= 2e-3
+    tree.close()
