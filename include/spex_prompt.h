@@ -49,7 +49,8 @@ typedef struct {
  * softmax weights are rounded to bf16 (to nearest) for their product with v, so that an output is within
  * 2^-8 of the weighted mean of |v| besides its own rounding.
  * Rows whose address, stride or head_dim is no multiple of 16 bytes take a slower kernel.
- * A prompt may have up to 2^24 tokens and all of them INT32_MAX (else SPEX_ERR_UNSUPPORTED).
+ * A prompt may have up to 2^24 tokens and all of them INT32_MAX (else SPEX_ERR_UNSUPPORTED).  SPEX_ERR_CAPACITY: no host memory
+ * for the list of the prompts.
  */
 spex_status_t spex_prompt_attention(const spex_prompt_config_t *cfg, const int32_t *lens, int32_t n_prompts,
                                     const void *q, const void *k, const void *v, void *out, float *lse,

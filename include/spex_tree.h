@@ -211,6 +211,52 @@ spex_status_t spex_tree_append_new_pages(const spex_tree_t *tree, spex_node_t no
                                          int32_t n_tokens, int32_t *n_new_pages);
 
 /*
+ * Position rotation.  What a model does to queries and keys before attention: the pair (x1, x2) number i of a head, of a token
+ * at position p, becomes
+ *     y1 = x1 cos(p f_i) - x2 sin(p f_i),   y2 = x2 cos(p f_i) + x1 sin(p f_i),   i < rotary_dim / 2,
+ * and the head's dims from rotary_dim on stay.  interleaved 0: pair i is dims (i, i + rotary_dim / 2); 1: dims (2i, 2i + 1).
+ *   inv_freq : HOST [rotary_dim / 2], the f_i in radians a position (finite), copied; a scaled variant of the rotation is its
+ *     frequencies
+ *   rotary_dim : even, 2 .. head_dim; 0 (inv_freq then NULL) takes the setting away
+ * The angle is evaluated in 64 bits with whole turns dropped exactly, cosine and sine are rounded to fp32, each product and sum
+ * is rounded to fp32, and y is rounded once to the type it is stored in.  Host only; calls already made keep their setting.
+ */
+spex_status_t spex_tree_set_rotation(spex_tree_t *tree, int32_t rotary_dim, const double *inv_freq, int32_t interleaved);
+
+/* The tensors of spex_tree_append_rotated.  All DEVICE, 16-bit ones in bf16; fp32 for an fp32 pool. */
+typedef struct {
+  const void *q;      /* [n_tokens][num_q_heads][head_dim], or NULL: keys and values only */
+  const void *k, *v;  /* [n_tokens][num_kv_heads][head_dim] */
+  void *q_out;        /* rotated queries, shape of q; given with q only, may be q (with q's stride) */
+  void *k_out;        /* rotated keys, shape of k, or NULL; may be k (with k's stride) */
+  /* elements between consecutive tokens; 0 = dense.  The heads of a token are dense; q, k and v may be parts of one tensor */
+  int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
+  const float *k_scales, *v_scales; /* fp8 pools: [n_scales][num_kv_heads], a row per page the call starts, or both NULL; else NULL */
+  int64_t n_scales;                 /* rows of k_scales and v_scales, at least the pages the call starts */
+} spex_rotated_t;
+
+/*
+ * The append of a decode iteration or of new prompts straight from a model's projections: queries and keys are rotated by their
+ * positions (spex_tree_set_rotation, else SPEX_ERR_INVALID_ARG), queries and, where wanted, keys written back for attention,
+ * keys and values appended to the nodes -- one launch for all of them.
+ *   nodes, counts : HOST [n_nodes]; node i, distinct and without live children, gets the next counts[i] >= 0 tokens of the
+ *     tensors (counts NULL: one each)
+ *   positions : HOST [sum(counts)], >= 0, or NULL: a token's position is the number of tokens before it on its path.  To be given
+ *     where the two differ, as for the drafts of a token tree, whose position is their depth
+ * fp8 pools are quantised on the way, from the rotated keys in fp32: code = e4m3fn(x * (1 / scale)), round to nearest even,
+ * saturating.  A page the call starts takes its row of k_scales / v_scales (pages in the order of the nodes, within a node in token
+ * order) if they are given, and else scale = max(amax / 448, 2^-40) over the tokens the call puts into it, as
+ * spex_tree_append_step_quantize; other pages keep the scale they have.
+ * All or nothing, page order, structure version and patches of the cached launch lists as spex_tree_append_tokens; like it,
+ * the call is not for recording in a HIP graph.  Rows, rotary_dim or buffers that are not made of 16-byte pieces take a slower
+ * kernel.  More than 2^22 pages written by one call are SPEX_ERR_UNSUPPORTED, as is a position beyond INT32_MAX; SPEX_ERR_CAPACITY:
+ * no host memory for the lists.
+ * The first call after spex_tree_set_rotation copies the frequencies to the device (and synchronises it if it replaces others).
+ */
+spex_status_t spex_tree_append_rotated(spex_tree_t *tree, const spex_node_t *nodes, const int32_t *counts, int32_t n_nodes,
+                                       const int32_t *positions, const spex_rotated_t *data, void *hip_stream);
+
+/*
  * Sec. 4.2 mis-speculation / Sec. 4.4 early termination: remove node and its whole subtree and
  * return their pages to the allocator (pre-order over the subtree, children in creation order,
  * each node's pages in order; the page returned last is handed out first).  Pruning a root ends

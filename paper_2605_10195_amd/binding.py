@@ -47,6 +47,12 @@ class Config(C.Structure):
     ]
 
 
+class Rotated(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v", "q_out", "k_out")] + \
+               [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride", "k_out_stride")] + \
+               [(n, C.c_void_p) for n in ("k_scales", "v_scales")] + [("n_scales", C.c_int64)]
+
+
 class NodeInfo(C.Structure):
     _fields_ = [("parent", C.c_int32), ("n_tokens", C.c_int32), ("n_pages", C.c_int32),
                 ("n_live_children", C.c_int32)]
@@ -83,6 +89,7 @@ EXPORTS = [
     "spex_tree_free_pages", "spex_tree_stats", "spex_tree_plan_dump", "spex_tree_gather_kv",
     "spex_tree_set_tuning", "spex_tree_set_profiling", "spex_tree_read_profile",
     "spex_tree_last_launch_info", "spex_tree_split_form", "spex_tree_walk_dump", "spex_tree_append_tokens", "spex_tree_append_tokens_quantize", "spex_tree_append_step_quantize",
+    "spex_tree_set_rotation", "spex_tree_append_rotated",
 ]
 # spex_sched.h: host-side scheduling primitives
 SCHED_EXPORTS = [
@@ -126,6 +133,8 @@ def _load():
     lib.spex_tree_append_new_pages.argtypes = [vp, i32, i32, _I32P]
     lib.spex_tree_append_tokens.argtypes = [vp, ip, i32, vp, vp, vp, vp, vp]
     lib.spex_tree_append_tokens_quantize.argtypes = [vp, ip, i32, vp, vp, vp, vp, vp]
+    lib.spex_tree_set_rotation.argtypes = [vp, i32, vp, i32]
+    lib.spex_tree_append_rotated.argtypes = [vp, ip, ip, i32, ip, C.POINTER(Rotated), vp]
     lib.spex_tree_prune.argtypes = [vp, i32]
     lib.spex_tree_decode_attention.argtypes = [vp, ip, ip, i32, vp, vp, vp, f32, vp]
     lib.spex_tree_decode_attention_masked.argtypes = [vp, ip, ip, ip, i32, vp, vp, vp, f32, vp]
@@ -328,6 +337,52 @@ class SpexTree:
             assert not quantize or (k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16)
         fn = lib.spex_tree_append_tokens_quantize if quantize else lib.spex_tree_append_tokens
         _check(fn(self._h, _addr(na), len(na), _dev(k), _dev(v), _dev(k_scales), _dev(v_scales), _stream()))
+
+    def set_rotation(self, rotary_dim: int, inv_freq: Optional[Sequence[float]] = None, base: float = 10000.0,
+                     interleaved: bool = False) -> None:
+        """Position rotation of append_rotated: the frequencies of the rotary_dim / 2 pairs, or base ** (-2 i / rotary_dim).
+        rotary_dim 0: none."""
+        if rotary_dim == 0:
+            _check(lib.spex_tree_set_rotation(self._h, 0, None, 0))
+            return
+        f = base ** (-np.arange(0, rotary_dim, 2, dtype=np.float64) / rotary_dim) if inv_freq is None else \
+            np.ascontiguousarray(np.asarray(inv_freq, dtype=np.float64))
+        assert f.shape == (rotary_dim // 2,)
+        _check(lib.spex_tree_set_rotation(self._h, rotary_dim, f.ctypes.data, int(interleaved)))
+
+    def append_rotated(self, nodes: Sequence[int], counts: Optional[Sequence[int]], q: Optional[torch.Tensor], k: torch.Tensor,
+                       v: torch.Tensor, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                       positions: Optional[Sequence[int]] = None, k_scales: Optional[torch.Tensor] = None,
+                       v_scales: Optional[torch.Tensor] = None, want_k: bool = False):
+        """Rotate and append counts[i] tokens (None: one) to each of nodes, one launch.  q [tokens, Hq, D] or None, k and v
+        [tokens, Hkv, D] in bfloat16 (float32 for fp32 pools), dense or with a stride between tokens.  Returns the rotated
+        queries and -- want_k, or k_out given -- keys; q_out=q and k_out=k rotate in place."""
+        na = _i32(nodes)
+        ca = None if counts is None else _i32(counts)
+        pa = None if positions is None else _i32(positions)
+        total = len(na) if ca is None else int(ca.sum(dtype=np.int64))
+        want = torch.float32 if self.kv_dtype == F32 else torch.bfloat16
+        assert ca is None or len(ca) == len(na)
+        assert pa is None or pa.shape == (total,)
+        assert k.shape[0] == total and v.shape[0] == total and (q is None or q.shape[0] == total)
+        if q_out is None and q is not None:
+            q_out = torch.empty((total, self.Hq, self.D), dtype=want, device=q.device)
+        if k_out is None and want_k:
+            k_out = torch.empty((total, self.Hkv, self.D), dtype=want, device=k.device)
+        assert all(t is None or t.dtype == want for t in (q, k, v, q_out, k_out))
+        assert (q is None) == (q_out is None) and (q_out is None or q_out.shape == q.shape) and (k_out is None or k_out.shape == k.shape)
+        assert _on_current_device(q, k, v, q_out, k_out, k_scales, v_scales), "all tensors must lie on the current device"
+        if k_scales is not None:
+            assert k_scales.dtype == torch.float32 and v_scales.dtype == torch.float32
+            assert k_scales.is_contiguous() and v_scales.is_contiguous() and k_scales.shape == v_scales.shape
+            assert k_scales.dim() == 2 and k_scales.shape[1] == self.Hkv
+        d = Rotated(_dev(q), _dev(k), _dev(v), _dev(q_out), _dev(k_out),
+                    0 if q is None else _token_stride(q, self.Hq, self.D), _token_stride(k, self.Hkv, self.D),
+                    _token_stride(v, self.Hkv, self.D), 0 if q is None else _token_stride(q_out, self.Hq, self.D),
+                    0 if k_out is None else _token_stride(k_out, self.Hkv, self.D), _dev(k_scales), _dev(v_scales),
+                    0 if k_scales is None else k_scales.shape[0])
+        _check(lib.spex_tree_append_rotated(self._h, _addr(na), _addr(ca), len(na), _addr(pa), C.byref(d), _stream()))
+        return q_out, k_out
 
     def prune(self, node: int) -> None:
         _check(lib.spex_tree_prune(self._h, node))
@@ -569,6 +624,11 @@ def spex_prompt_attention(lens: Sequence[int], q: torch.Tensor, k: torch.Tensor,
 
 
 prompt_attention = spex_prompt_attention
+
+
+def spex_tree_append_rotated(tree: SpexTree, nodes, counts, q, k, v, q_out=None, k_out=None, positions=None, k_scales=None,
+                             v_scales=None):
+    return tree.append_rotated(nodes, counts, q, k, v, q_out, k_out, positions, k_scales, v_scales)
 
 
 # ---- spex_sched.h: argument marshalling only ------------------------------------------------

@@ -32,6 +32,8 @@
 //       The same element by element, for rows or buffers that are not 16-byte aligned.
 //   spex_append_tokens_kernel
 //       One token for each of many nodes.
+//   spex_append_rotated_kernel / spex_append_rotated_any_kernel (rotated_append.hpp)
+//       Tokens of many nodes, queries and keys turned by their positions on the way.
 //   spex_patch_plan_kernel
 //       Applies {index, value} patches to the device copy of the cached launch lists.
 #include "kernels.hpp"
@@ -2900,6 +2902,8 @@ __global__ __launch_bounds__(256) void spex_append_tokens_kernel(AppendTokensArg
   }
 }
 
+#include "rotated_append.hpp"
+
 template <int KV, int LAYOUT>
 __global__ __launch_bounds__(256) void spex_gather_kv_kernel(GatherArgs a, Shape sh) {
   typedef typename std::conditional<KV == kF32, float,
@@ -3304,6 +3308,57 @@ hipError_t launch_append_tokens(const Shape &sh, const AppendTokensArgs &a, hipS
     case kF32: return append_tokens_layout<kF32, false>(sh, a, stream);
     case kBF16: return append_tokens_layout<kBF16, false>(sh, a, stream);
     case kFP8: return append_tokens_layout<kFP8, false>(sh, a, stream);
+  }
+  return hipErrorInvalidValue;
+}
+
+template <int KV, int DT>
+static void append_rotated_wide(const Shape &sh, const RotateArgs &a, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(a.n_recs), static_cast<unsigned>(a.parts)), block(256);
+  const size_t lds = static_cast<size_t>(a.most_tokens) * (a.rotary_dim / 2) * sizeof(float) * 2;
+  if (a.interleaved)
+    hipLaunchKernelGGL((spex_append_rotated_kernel<KV, DT, true>), grid, block, lds, stream, a, sh);
+  else
+    hipLaunchKernelGGL((spex_append_rotated_kernel<KV, DT, false>), grid, block, lds, stream, a, sh);
+}
+
+template <int KV>
+static hipError_t append_rotated(const Shape &sh, const RotateArgs &args, hipStream_t stream) {
+  RotateArgs a = args;
+  const bool tiled = sh.layout == kMfmaTiled;
+  const int64_t per16 = KV == kF32 ? 4 : 8;
+  bool wide = sh.D % 8 == 0 && a.rotary_dim % (a.interleaved ? 8 : 16) == 0;
+  for (const void *x : {a.q, a.k, a.v, static_cast<const void *>(a.q_out), static_cast<const void *>(a.k_out),
+                        static_cast<const void *>(a.k_pool), static_cast<const void *>(a.v_pool)})
+    wide = wide && aligned16(x);
+  for (int64_t s : {a.q_stride, a.k_stride, a.v_stride, a.q_out_stride, a.k_out_stride}) wide = wide && s % per16 == 0;
+  if (!wide) {
+    const dim3 grid(static_cast<unsigned>(a.n_recs), static_cast<unsigned>(sh.Hkv)), block(256);
+    a.parts = sh.Hkv;
+    if (tiled)
+      hipLaunchKernelGGL((spex_append_rotated_any_kernel<KV, KV == kF32 ? kRowMajor : kMfmaTiled>), grid, block, 0, stream, a, sh);
+    else
+      hipLaunchKernelGGL((spex_append_rotated_any_kernel<KV, kRowMajor>), grid, block, 0, stream, a, sh);
+    return hipGetLastError();
+  }
+  // Pages few in number are shared by several workgroups, each with some kv heads, as long as a workgroup keeps two rounds.
+  const int64_t units = static_cast<int64_t>(a.most_tokens) * (sh.Hq + 2 * sh.Hkv) * ((sh.D + 15) / 16);
+  a.parts = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>({sh.Hkv, units / 512, 2048 / a.n_recs})));
+  if (KV != kF32 && tiled && sh.D == 64)
+    append_rotated_wide<KV, KV == kF32 ? 0 : 64>(sh, a, stream);
+  else if (KV != kF32 && tiled)
+    append_rotated_wide<KV, KV == kF32 ? 0 : 128>(sh, a, stream);
+  else
+    append_rotated_wide<KV, 0>(sh, a, stream);
+  return hipGetLastError();
+}
+
+hipError_t launch_append_rotated(const Shape &sh, const RotateArgs &a, hipStream_t stream) {
+  if (a.n_recs <= 0) return hipSuccess;
+  switch (sh.kv_dtype) {
+    case kF32: return append_rotated<kF32>(sh, a, stream);
+    case kBF16: return append_rotated<kBF16>(sh, a, stream);
+    case kFP8: return append_rotated<kFP8>(sh, a, stream);
   }
   return hipErrorInvalidValue;
 }

@@ -86,11 +86,12 @@ __device__ __forceinline__ RowSet row_set(const PromptArgs &p, int wave) {
 }
 
 // 16 bytes a lane from memory to LDS, to lds + 16 * lane.  In assembly, because the compiler lets every transposing read wait for
-// all such copies under way, those into the other buffers too; tile_barrier() is what waits for them.
+// all such copies under way, those into the other buffers too; tile_barrier() is what waits for them.  (The compiler keeps nothing
+// in m0 between instructions of its own.)
 __device__ __forceinline__ void copy_to_lds(const void *src, lds_char *lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(uniform(static_cast<int>(reinterpret_cast<uintptr_t>(lds)))),
                "v"(src)
-               : "memory", "m0");
+               : "memory");
 }
 // Behind it every wavefront's copies have landed, and none of them reads LDS of the step before.
 __device__ __forceinline__ void tile_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }

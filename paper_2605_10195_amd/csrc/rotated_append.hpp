@@ -1,0 +1,471 @@
+// Kernels of spex_tree_append_rotated; part of kernels.hip, whose helpers they use.
+//
+//   spex_append_rotated_kernel
+//       One workgroup per (page that the call writes to, range of kv heads): the cosines and sines of its tokens into LDS,
+//       then queries, keys and values 16 bytes at a time.
+//   spex_append_rotated_any_kernel
+//       The same element by element, for rows, buffers or rotated parts that are not made of 16-byte pieces.
+//
+// Mathematics: the pair (x1, x2) number i of a head at position p turns by the angle p * inv_freq[i],
+//   y1 = x1 cos - x2 sin,  y2 = x2 cos + x1 sin.
+// The angle is taken in 64 bits, as turns, so that whole turns can be dropped exactly however far the position; cosine
+// and sine are rounded to fp32, products and sums are fp32 operations rounded one by one, and the result is rounded once to the
+// type it is stored in.
+#pragma once
+
+// Cosine and sine of 2 pi p (f.hi + f.lo).  p f.hi is split exactly into its rounded value and the rest; after whole turns and
+// quarter turns at most an eighth of a turn is left, where the Taylor series to the 13th and 14th power are off by less than 3e-14.
+__device__ __forceinline__ f32x2 cos_sin_turns(int p, const Turns f) {
+  const double x = static_cast<double>(p);
+  const double t = x * f.hi, rest = __builtin_fma(x, f.hi, -t) + x * f.lo;
+  const double r = (t - __builtin_rint(t)) + rest;         // in [-0.5, 0.5], almost
+  const double quarter = __builtin_rint(4.0 * r);
+  const double a = 6.283185307179586476925 * __builtin_fma(-0.25, quarter, r);
+  const double a2 = a * a;
+  double s = 1.0 / 6227020800.0;
+  s = __builtin_fma(s, a2, -1.0 / 39916800.0);
+  s = __builtin_fma(s, a2, 1.0 / 362880.0);
+  s = __builtin_fma(s, a2, -1.0 / 5040.0);
+  s = __builtin_fma(s, a2, 1.0 / 120.0);
+  s = __builtin_fma(s, a2, -1.0 / 6.0);
+  s = __builtin_fma(s * a2, a, a);
+  double c = -1.0 / 87178291200.0;
+  c = __builtin_fma(c, a2, 1.0 / 479001600.0);
+  c = __builtin_fma(c, a2, -1.0 / 3628800.0);
+  c = __builtin_fma(c, a2, 1.0 / 40320.0);
+  c = __builtin_fma(c, a2, -1.0 / 720.0);
+  c = __builtin_fma(c, a2, 1.0 / 24.0);
+  c = __builtin_fma(c, a2, -0.5);
+  c = __builtin_fma(c, a2, 1.0);
+  const int n = static_cast<int>(quarter) & 3;
+  const double cn = (n & 1) ? s : c, sn = (n & 1) ? c : s;
+  return f32x2{static_cast<float>(n == 1 || n == 2 ? -cn : cn), static_cast<float>(n >= 2 ? -sn : sn)};
+}
+
+__device__ __forceinline__ f32x2 turned(float x1, float x2, f32x2 cs) {
+#pragma clang fp contract(off)
+  return f32x2{x1 * cs[0] - x2 * cs[1], x2 * cs[0] + x1 * cs[1]};
+}
+
+// A record of a.recs: tokens tok0 .. tok0 + hi - lo - 1 of the call go to slots [lo, hi) of the page.
+struct PageVisit {
+  int page, lo, hi, fill, tok0, pos0, new_index;
+  bool is_new;  // this call starts the page: slots up to fill = P are written, zeros behind the tokens
+};
+__device__ __forceinline__ PageVisit page_visit(const RotateArgs &a, int P) {
+  const int32_t *r = a.recs + static_cast<int64_t>(blockIdx.x) * kVisitInts;
+  const u32x4 x = *reinterpret_cast<const u32x4 *>(r);
+  PageVisit v;
+  v.page = uniform(static_cast<int>(x[0]));
+  const int flags = uniform(static_cast<int>(x[1]));
+  v.tok0 = uniform(static_cast<int>(x[2]));
+  v.pos0 = uniform(static_cast<int>(x[3]));
+  v.new_index = uniform(r[4]);
+  v.lo = flags & 0xff;
+  v.hi = (flags >> 8) & 0xff;
+  v.is_new = (flags >> 16) != 0;
+  v.fill = v.is_new ? P : v.hi;
+  return v;
+}
+
+__device__ __forceinline__ void apply_patches(const RotateArgs &a) {
+  if (blockIdx.y != 0) return;
+  for (int i = static_cast<int>(blockIdx.x * 256 + threadIdx.x); i < a.n_patches; i += static_cast<int>(gridDim.x) * 256)
+    a.plan[a.patches[2 * i]] = a.patches[2 * i + 1];
+}
+
+// Eight dims of a row.
+struct Eight {
+  float x[8];
+};
+template <bool F32>
+__device__ __forceinline__ Eight load_eight(const void *base, int64_t at) {
+  Eight r;
+  if (F32) {
+    const f32x4 *p = reinterpret_cast<const f32x4 *>(static_cast<const float *>(base) + at);
+    const f32x4 a = p[0], b = p[1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.x[i] = a[i], r.x[4 + i] = b[i];
+  } else {
+    const u32x4 w = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(base) + at);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.x[i] = bf16_bits_to_float(half_word(w, i));
+  }
+  return r;
+}
+__device__ __forceinline__ uint32_t pair_bf16(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+}
+template <bool F32>
+__device__ __forceinline__ void store_eight(void *base, int64_t at, const Eight &e) {
+  if (F32) {
+    f32x4 *p = reinterpret_cast<f32x4 *>(static_cast<float *>(base) + at);
+    p[0] = f32x4{e.x[0], e.x[1], e.x[2], e.x[3]};
+    p[1] = f32x4{e.x[4], e.x[5], e.x[6], e.x[7]};
+  } else {
+    *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(base) + at) =
+        u32x4{pair_bf16(e.x[0], e.x[1]), pair_bf16(e.x[2], e.x[3]), pair_bf16(e.x[4], e.x[5]), pair_bf16(e.x[6], e.x[7])};
+  }
+}
+__device__ __forceinline__ float largest(const Eight &e) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, __builtin_fabsf(e.x[i]));
+  return m;
+}
+
+// The reciprocal of a page's scale.  A scale of 0 is a page of zeros: finite here, so that 0 times it is 0.
+__device__ __forceinline__ float inverse_scale(float s) { return fminf(1.0f / s, __FLT_MAX__); }
+__device__ __forceinline__ float page_scale(float amax) { return fmaxf(amax / 448.0f, 0x1p-40f); }
+
+// Two pieces of eight dims that are turned together: unit u of a row of D dims has dims d[0] .. + 7 and, where it has a second
+// piece, d[1] .. + 7.  Halves: pair i is (i, i + R/2); interleaved: (2i, 2i + 1).
+template <bool F32, bool INTER>
+struct Unit {
+  Eight e[2];
+  int d[2];
+  bool two, rotated[2];
+  __device__ __forceinline__ void place(int u, int D, int R) {
+    const bool halves = !INTER && 16 * u < R;
+    d[0] = halves ? 8 * u : 16 * u;
+    d[1] = halves ? 8 * u + R / 2 : 16 * u + 8;
+    two = d[1] < D;
+    rotated[0] = d[0] < R;
+    rotated[1] = d[1] < R;
+  }
+  __device__ __forceinline__ void load(const void *base, int64_t row) {
+    e[0] = load_eight<F32>(base, row + d[0]);
+    e[1] = two ? load_eight<F32>(base, row + d[1]) : e[0];
+  }
+  // cs: cosines and sines of the token's pairs.
+  __device__ __forceinline__ void turn(const f32x2 *cs) {
+    if (INTER) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if (rotated[k]) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f32x2 y = turned(e[k].x[2 * i], e[k].x[2 * i + 1], cs[d[k] / 2 + i]);
+            e[k].x[2 * i] = y[0];
+            e[k].x[2 * i + 1] = y[1];
+          }
+        }
+    } else if (rotated[0]) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const f32x2 y = turned(e[0].x[i], e[1].x[i], cs[d[0] + i]);
+        e[0].x[i] = y[0];
+        e[1].x[i] = y[1];
+      }
+    }
+  }
+  __device__ __forceinline__ void store(void *base, int64_t row) const {
+    store_eight<F32>(base, row + d[0], e[0]);
+    if (two) store_eight<F32>(base, row + d[1], e[1]);
+  }
+  __device__ __forceinline__ float top() const { return fmaxf(largest(e[0]), two ? largest(e[1]) : 0.f); }
+};
+
+__device__ __forceinline__ u32x2 encode_eight(const Eight &e, float inv) {
+  u32x2 r = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i >> 2] |= encode_e4m3(e.x[i] * inv) << (8 * (i & 3));
+  return r;
+}
+// Eight dims of a token into a tile.
+template <int KV>
+__device__ __forceinline__ void put_eight(char *tile, int at, const Eight &e, float inv) {
+  if (KV == kFP8)
+    *reinterpret_cast<u32x2 *>(tile + at) = encode_eight(e, inv);
+  else
+    store_eight<KV == kF32>(tile, at, e);
+}
+
+// DT: head_dim of tiled pools, else 0.
+template <int KV, int DT, bool INTER>
+__global__ __launch_bounds__(256) void spex_append_rotated_kernel(RotateArgs a, Shape sh) {
+  constexpr bool F32 = KV == kF32, FP8 = KV == kFP8, TILED = DT > 0;
+  constexpr int LAYOUT = TILED ? kMfmaTiled : kRowMajor, ESZ = F32 ? 4 : (FP8 ? 1 : 2);
+  extern __shared__ __attribute__((aligned(16))) char lds_[];
+  f32x2 *cs = reinterpret_cast<f32x2 *>(lds_);  // [token][R / 2]
+  const int D = TILED ? DT : sh.D, P = TILED ? 16 : sh.P, U = (D + 15) / 16, R = a.rotary_dim;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const PageVisit pv = page_visit(a, P);
+  apply_patches(a);
+  const int n = pv.hi - pv.lo;  // tokens
+  for (int i = tid; i < n * (R / 2); i += 256) {
+    const int t = i / (R / 2), pair = i - t * (R / 2);
+    const int pos = a.positions ? a.positions[pv.tok0 + t] : pv.pos0 + t;
+    cs[i] = cos_sin_turns(pos, a.freq[pair]);
+  }
+  __syncthreads();
+  const int g0 = static_cast<int>(blockIdx.y) * sh.Hkv / a.parts, g1 = (static_cast<int>(blockIdx.y) + 1) * sh.Hkv / a.parts, ng = g1 - g0;
+  Unit<F32, INTER> un;
+  if (a.q) {
+    const int nq = ng * sh.G;
+    for (int i = tid; i < n * nq * U; i += 256) {
+      const int r = i / U, t = r / nq, head = g0 * sh.G + r - t * nq;
+      un.place(i - r * U, D, R);
+      un.load(a.q, (pv.tok0 + t) * a.q_stride + static_cast<int64_t>(head) * D);
+      un.turn(cs + t * (R / 2));
+      un.store(a.q_out, (pv.tok0 + t) * a.q_out_stride + static_cast<int64_t>(head) * D);
+    }
+  }
+  const int64_t tile0 = static_cast<int64_t>(pv.page) * sh.page_tiles, tile_bytes = static_cast<int64_t>(P) * D * ESZ;
+  const int slots = pv.fill - pv.lo;
+  // Keys: rows of the tile's layout.  fp8: a wavefront a kv head, because the page's scale comes from all of its tokens.
+  const int first = FP8 ? lane : tid, step = FP8 ? 64 : 256;
+  for (int gi = FP8 ? wave : 0; gi < (FP8 ? ng : 1); gi += FP8 ? 4 : 1) {
+    const int heads = FP8 ? 1 : ng;
+    float inv = 1.f;
+    if (FP8) {
+      const int g = g0 + gi, at = pv.page * sh.Hkv + g;
+      float s;
+      if (!pv.is_new) {
+        s = a.k_scale[at];
+      } else if (a.k_scale_src) {
+        s = a.k_scale_src[static_cast<int64_t>(pv.new_index) * sh.Hkv + g];
+      } else {
+        float top = 0.f;
+        for (int i = lane; i < n * U; i += 64) {
+          const int t = i / U;
+          un.place(i - t * U, D, R);
+          un.load(a.k, (pv.tok0 + t) * a.k_stride + static_cast<int64_t>(g) * D);
+          un.turn(cs + t * (R / 2));
+          top = fmaxf(top, un.top());
+        }
+        s = page_scale(wave_max(top));
+      }
+      if (pv.is_new && lane == 0) a.k_scale[at] = s;
+      inv = inverse_scale(s);
+    }
+    for (int i = first; i < slots * heads * U; i += step) {
+      const int r = i / U, t = r / heads, g = g0 + (FP8 ? gi : r - t * heads);
+      const int slot = pv.lo + t;
+      un.place(i - r * U, D, R);
+      if (t < n) {
+        un.load(a.k, (pv.tok0 + t) * a.k_stride + static_cast<int64_t>(g) * D);
+        un.turn(cs + t * (R / 2));
+        if (a.k_out) un.store(a.k_out, (pv.tok0 + t) * a.k_out_stride + static_cast<int64_t>(g) * D);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) un.e[0].x[j] = un.e[1].x[j] = 0.f;
+      }
+      char *tile = static_cast<char *>(a.k_pool) + (tile0 + g) * tile_bytes;
+      put_eight<KV>(tile, k_offset<KV, LAYOUT>(slot, un.d[0], D), un.e[0], inv);
+      if (un.two) put_eight<KV>(tile, k_offset<KV, LAYOUT>(slot, un.d[1], D), un.e[1], inv);
+    }
+  }
+  // Values.  Row-major pools: as the keys, unturned.
+  if (!TILED) {
+    const int C = D / 8;
+    for (int gi = FP8 ? wave : 0; gi < (FP8 ? ng : 1); gi += FP8 ? 4 : 1) {
+      const int heads = FP8 ? 1 : ng;
+      float inv = 1.f;
+      if (FP8) {
+        const int g = g0 + gi, at = pv.page * sh.Hkv + g;
+        float s;
+        if (!pv.is_new) {
+          s = a.v_scale[at];
+        } else if (a.v_scale_src) {
+          s = a.v_scale_src[static_cast<int64_t>(pv.new_index) * sh.Hkv + g];
+        } else {
+          float top = 0.f;
+          for (int i = lane; i < n * C; i += 64)
+            top = fmaxf(top, largest(load_eight<F32>(a.v, (pv.tok0 + i / C) * a.v_stride + static_cast<int64_t>(g) * D + i % C * 8)));
+          s = page_scale(wave_max(top));
+        }
+        if (pv.is_new && lane == 0) a.v_scale[at] = s;
+        inv = inverse_scale(s);
+      }
+      for (int i = first; i < slots * heads * C; i += step) {
+        const int r = i / C, t = r / heads, g = g0 + (FP8 ? gi : r - t * heads), d = (i - r * C) * 8;
+        Eight e = {};
+        if (t < n) e = load_eight<F32>(a.v, (pv.tok0 + t) * a.v_stride + static_cast<int64_t>(g) * D + d);
+        put_eight<KV>(static_cast<char *>(a.v_pool) + (tile0 + g) * tile_bytes, (pv.lo + t) * D + d, e, inv);
+      }
+    }
+    return;
+  }
+  // Tiled pools hold values token-minor: a thread takes eight dims of eight tokens and turns them round in registers.  The threads of a
+  // kv head are 2 D / 8 lanes beside each other.
+  constexpr int C = TILED ? DT / 8 : 1;
+  for (int i = tid; i < ng * 2 * C; i += 256) {
+    const int g = g0 + i / (2 * C), t0 = i / C % 2 * 8, d = i % C * 8;
+    u32x4 w[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      w[s] = u32x4{0, 0, 0, 0};
+      const int t = t0 + s - pv.lo;
+      if (t >= 0 && t < n)
+        w[s] = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.v) + (pv.tok0 + t) * a.v_stride + static_cast<int64_t>(g) * D + d);
+    }
+    float inv = 1.f;
+    if (FP8) {
+      const int at = pv.page * sh.Hkv + g;
+      float s;
+      if (!pv.is_new) {
+        s = a.v_scale[at];
+      } else if (a.v_scale_src) {
+        s = a.v_scale_src[static_cast<int64_t>(pv.new_index) * sh.Hkv + g];
+      } else {
+        float top = 0.f;
+#pragma unroll
+        for (int s2 = 0; s2 < 8; ++s2) top = fmaxf(top, abs_max8(w[s2]));
+#pragma unroll
+        for (int o = C; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+        s = page_scale(top);
+      }
+      if (pv.is_new && i % (2 * C) == 0) a.v_scale[at] = s;
+      inv = inverse_scale(s);
+    }
+    char *tile = static_cast<char *>(a.v_pool) + (tile0 + g) * tile_bytes;
+    const bool whole = t0 >= pv.lo && t0 + 8 <= pv.fill;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {  // dim d + k of the eight tokens
+      char *dst = tile + ESZ * v_offset<KV, kMfmaTiled>(t0, d + k, D);
+      if (FP8) {
+        u32x2 c = {0, 0};
+#pragma unroll
+        for (int s = 0; s < 8; ++s) c[s >> 2] |= encode_e4m3(bf16_bits_to_float(half_word(w[s], k)) * inv) << (8 * (s & 3));
+        if (whole) {
+          *reinterpret_cast<u32x2 *>(dst) = c;
+        } else {
+#pragma unroll
+          for (int s = 0; s < 8; ++s)
+            if (t0 + s >= pv.lo && t0 + s < pv.fill) dst[s] = static_cast<char>(c[s >> 2] >> (8 * (s & 3)));
+        }
+      } else {
+        u32x4 h;
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+          h[s] = bf16_bits_to_f16_bits(half_word(w[2 * s], k)) | static_cast<uint32_t>(bf16_bits_to_f16_bits(half_word(w[2 * s + 1], k))) << 16;
+        if (whole) {
+          *reinterpret_cast<u32x4 *>(dst) = h;
+        } else {
+#pragma unroll
+          for (int s = 0; s < 8; ++s)
+            if (t0 + s >= pv.lo && t0 + s < pv.fill) *reinterpret_cast<uint16_t *>(dst + 2 * s) = static_cast<uint16_t>(h[s >> 1] >> (16 * (s & 1)));
+        }
+      }
+    }
+  }
+}
+
+// Element by element: a workgroup per (page, kv head), with the query heads of the kv head; a thread turns whole pairs.
+template <int KV, int LAYOUT>
+__global__ __launch_bounds__(256) void spex_append_rotated_any_kernel(RotateArgs a, Shape sh) {
+  typedef typename std::conditional<KV == kF32, float, typename std::conditional<KV == kBF16, uint16_t, uint8_t>::type>::type T;
+  typedef typename std::conditional<KV == kF32, float, uint16_t>::type S;
+  constexpr bool FP8 = KV == kFP8;
+  __shared__ float red[2][4];
+  const int D = sh.D, P = sh.P, R = a.rotary_dim, half = R / 2, per = half + D - R;  // per: pairs and single dims of a row
+  const int tid = threadIdx.x, g = blockIdx.y;
+  const PageVisit pv = page_visit(a, P);
+  apply_patches(a);
+  const int n = pv.hi - pv.lo, slots = pv.fill - pv.lo;
+  auto widen = [](S x) { return KV == kF32 ? static_cast<float>(x) : bf16_bits_to_float(static_cast<uint16_t>(x)); };
+  auto narrow = [](float x) {
+    if (KV == kF32) return static_cast<S>(x);
+    return static_cast<S>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(x)));
+  };
+  // Values and dims of element j of a row: a turned pair (j < half) or a dim behind the turned part (twice).
+  struct Two {
+    float x[2];
+    int d[2];
+  };
+  auto element = [&](const void *base, int64_t row, int t, int j) {
+    Two e;
+    e.d[0] = j >= half ? R + j - half : (a.interleaved ? 2 * j : j);
+    e.d[1] = j >= half ? e.d[0] : (a.interleaved ? 2 * j + 1 : j + half);
+    e.x[0] = widen(static_cast<const S *>(base)[row + e.d[0]]);
+    e.x[1] = widen(static_cast<const S *>(base)[row + e.d[1]]);
+    if (j < half) {
+      const f32x2 y = turned(e.x[0], e.x[1], cos_sin_turns(a.positions ? a.positions[pv.tok0 + t] : pv.pos0 + t, a.freq[j]));
+      e.x[0] = y[0];
+      e.x[1] = y[1];
+    }
+    return e;
+  };
+  if (a.q)
+    for (int i = tid; i < n * sh.G * per; i += 256) {
+      const int t = i / per / sh.G, head = g * sh.G + i / per % sh.G;
+      const Two e = element(a.q, (pv.tok0 + t) * a.q_stride + static_cast<int64_t>(head) * D, t, i % per);
+      S *o = static_cast<S *>(a.q_out) + (pv.tok0 + t) * a.q_out_stride + static_cast<int64_t>(head) * D;
+      o[e.d[0]] = narrow(e.x[0]);
+      o[e.d[1]] = narrow(e.x[1]);
+    }
+  const int64_t tile = (static_cast<int64_t>(pv.page) * sh.page_tiles + g) * (static_cast<int64_t>(P) * D);
+  T *kp = static_cast<T *>(a.k_pool) + tile, *vp = static_cast<T *>(a.v_pool) + tile;
+  auto k_row = [&](int t) { return (pv.tok0 + t) * a.k_stride + static_cast<int64_t>(g) * D; };
+  auto v_row = [&](int t) { return (pv.tok0 + t) * a.v_stride + static_cast<int64_t>(g) * D; };
+  float kinv = 1.f, vinv = 1.f;
+  if (FP8) {
+    const int at = pv.page * sh.Hkv + g;
+    float ks, vs;
+    if (!pv.is_new) {
+      ks = a.k_scale[at];
+      vs = a.v_scale[at];
+    } else {
+      if (a.k_scale_src) {
+        ks = a.k_scale_src[static_cast<int64_t>(pv.new_index) * sh.Hkv + g];
+        vs = a.v_scale_src[static_cast<int64_t>(pv.new_index) * sh.Hkv + g];
+      } else {
+        float ka = 0.f, va = 0.f;
+        for (int i = tid; i < n * per; i += 256) {
+          const Two e = element(a.k, k_row(i / per), i / per, i % per);
+          ka = fmaxf(ka, fmaxf(__builtin_fabsf(e.x[0]), __builtin_fabsf(e.x[1])));
+        }
+        for (int i = tid; i < n * D; i += 256) va = fmaxf(va, __builtin_fabsf(widen(static_cast<const S *>(a.v)[v_row(i / D) + i % D])));
+        ka = wave_max(ka);
+        va = wave_max(va);
+        if ((tid & 63) == 0) {
+          red[0][tid >> 6] = ka;
+          red[1][tid >> 6] = va;
+        }
+        __syncthreads();
+        ks = page_scale(fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3])));
+        vs = page_scale(fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3])));
+      }
+      if (tid == 0) {
+        a.k_scale[at] = ks;
+        a.v_scale[at] = vs;
+      }
+    }
+    kinv = inverse_scale(ks);
+    vinv = inverse_scale(vs);
+    // k_out may be k: every thread has read the whole page's keys before one of them is replaced
+    __syncthreads();
+  }
+  for (int i = tid; i < slots * per; i += 256) {
+    const int t = i / per, slot = pv.lo + t;
+    if (t < n) {
+      const Two e = element(a.k, k_row(t), t, i % per);
+      if (a.k_out) {
+        S *o = static_cast<S *>(a.k_out) + (pv.tok0 + t) * a.k_out_stride + static_cast<int64_t>(g) * D;
+        o[e.d[0]] = narrow(e.x[0]);
+        o[e.d[1]] = narrow(e.x[1]);
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        kp[k_offset<KV, LAYOUT>(slot, e.d[k], D)] = FP8 ? static_cast<T>(encode_e4m3(e.x[k] * kinv)) : static_cast<T>(narrow(e.x[k]));
+    } else {
+      const int j = i % per, d0 = j >= half ? R + j - half : j;
+      kp[k_offset<KV, LAYOUT>(slot, d0, D)] = T(0);
+      if (j < half) kp[k_offset<KV, LAYOUT>(slot, j + half, D)] = T(0);
+    }
+  }
+  for (int i = tid; i < slots * D; i += 256) {
+    const int t = i / D, d = i % D;
+    T x = T(0);
+    if (t < n) {
+      const S s = static_cast<const S *>(a.v)[v_row(t) + d];
+      if (FP8)
+        x = static_cast<T>(encode_e4m3(widen(s) * vinv));
+      else
+        x = v_is_f16<KV, LAYOUT>() ? static_cast<T>(bf16_bits_to_f16_bits(static_cast<uint16_t>(s))) : static_cast<T>(s);
+    }
+    vp[v_offset<KV, LAYOUT>(pv.lo + t, d, D)] = x;
+  }
+}

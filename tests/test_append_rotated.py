@@ -1,0 +1,462 @@
+"""spex_tree_append_rotated: refusals on the CPU (nothing is launched, nothing changes), page table and values on the GPU
+against the definition in 64 bits."""
+
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_10195_amd as spex
+from gpu_common import assert_v_round_trip
+from paper_2605_10195_amd import binding
+
+OK, INVALID, BAD_NODE, NOT_LEAF, OOM, UNSUPPORTED = 0, 1, 2, 3, 4, 6
+SRC = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8_e4m3": torch.bfloat16}
+
+
+# ---- refusals: a handle whose pools are addresses that nothing may touch --------------------------------
+@pytest.fixture
+def handle():
+    made = []
+
+    def make(heads=(4, 2, 64), page=16, kv=binding.BF16, num_pages=8, pools=True, rotary=64):
+        cfg = binding.Config()
+        cfg.num_q_heads, cfg.num_kv_heads, cfg.head_dim = heads
+        cfg.page_size, cfg.kv_dtype, cfg.num_pages = page, kv, num_pages
+        cfg.q_dtype = binding.F32 if kv == binding.F32 else binding.BF16
+        if pools:
+            cfg.k_pool, cfg.v_pool = 64, 64
+            if kv == binding.FP8_E4M3:
+                cfg.k_scale, cfg.v_scale = 64, 64
+        h = C.c_void_p()
+        assert binding.lib.spex_tree_create(C.byref(cfg), C.byref(h)) == OK
+        made.append(h)
+        if rotary:
+            f = np.ones(rotary // 2)
+            assert binding.lib.spex_tree_set_rotation(h, rotary, f.ctypes.data, 0) == OK
+        ids = np.zeros(4, np.int32)
+        assert binding.lib.spex_tree_fork(h, -1, 3, ids.ctypes.data) == OK
+        assert binding.lib.spex_tree_fork(h, 2, 1, ids.ctypes.data) == OK      # node 2 has a child, node 3
+        return h
+    yield make
+    for h in made:
+        binding.lib.spex_tree_destroy(h)
+
+
+def append(h, nodes, counts=None, positions=None, n=None, data=True, **fields):
+    d = binding.Rotated(q=64, k=64, v=64, q_out=64)
+    for name, x in fields.items():
+        setattr(d, name, x)
+    na = np.asarray(nodes, np.int32)
+    ca = None if counts is None else np.asarray(counts, np.int32)
+    pa = None if positions is None else np.asarray(positions, np.int32)
+    address = lambda a: None if a is None else a.ctypes.data  # noqa: E731
+    return binding.lib.spex_tree_append_rotated(h, address(na), address(ca), len(na) if n is None else n, address(pa),
+                                                C.byref(d) if data else None, None)
+
+
+def state(h):
+    free, n = np.zeros(16, np.int32), C.c_int32()
+    assert binding.lib.spex_tree_free_pages(h, free.ctypes.data_as(binding._I32P), 16, C.byref(n)) == OK
+    infos = []
+    for u in range(4):
+        info = binding.NodeInfo()
+        assert binding.lib.spex_tree_node_info(h, u, C.byref(info)) == OK
+        infos.append((info.n_tokens, info.n_pages))
+    return free[:n.value].tolist(), infos
+
+
+@pytest.mark.parametrize("want,nodes,kw", [
+    (INVALID, [0], dict(data=False)), (INVALID, [0], dict(n=-1)), (INVALID, [0], dict(counts=[-1])), (INVALID, [0, 1], dict(counts=[3, -3])),
+    (INVALID, [0, 0], {}), (INVALID, [1, 0, 1], dict(counts=[1, 1, 0])), (BAD_NODE, [4], {}), (BAD_NODE, [-1], {}), (NOT_LEAF, [0, 2], {}),
+    (INVALID, [0], dict(k=None)), (INVALID, [0], dict(v=None)), (INVALID, [0], dict(q=None)), (INVALID, [0], dict(q_out=None)),
+    (INVALID, [0], dict(k_scales=64, v_scales=64, n_scales=4)),
+    (INVALID, [0], dict(q_stride=255)), (INVALID, [0], dict(k_stride=127)), (INVALID, [0], dict(v_stride=-128)),
+    (INVALID, [0], dict(q_out_stride=8)), (INVALID, [0], dict(k_out_stride=8)), (INVALID, [0], dict(q_stride=512)),
+    (INVALID, [0], dict(k_out=64, k_stride=256)), (UNSUPPORTED, [0], dict(k_stride=1 << 31)),
+    (INVALID, [0, 1], dict(positions=[0, -1])), (OOM, [0], dict(counts=[129])), (OOM, [0, 1, 3], dict(counts=[64, 64, 1])),
+    (UNSUPPORTED, [0], dict(counts=[1 << 30])),
+    (OK, [], {}), (OK, [0, 1], dict(counts=[0, 0])), (OK, [0], dict(counts=[0], k=None, v=None)),
+])
+def test_arguments_are_checked_and_nothing_changes(handle, want, nodes, kw):
+    h = handle()
+    before = state(h)
+    assert append(h, nodes, **kw) == want
+    assert state(h) == before
+
+
+def test_handles_that_cannot_append(handle):
+    assert append(handle(pools=False), [0]) == INVALID          # host-only
+    assert append(handle(rotary=0), [0]) == INVALID             # no rotation set
+    assert append(None, [0]) == INVALID
+    h = handle(kv=binding.FP8_E4M3)
+    assert append(h, [0], k_scales=64) == INVALID               # one of two
+    assert append(h, [0, 1], k_scales=64, v_scales=64, n_scales=1) == INVALID
+
+
+@pytest.mark.parametrize("rotary,freq,want", [(2, [1.0], OK), (64, [0.5] * 32, OK), (0, None, OK), (3, [1.0], INVALID), (66, [1.0] * 33, INVALID),
+                                              (-2, None, INVALID), (4, None, INVALID), (0, [1.0], INVALID),
+                                              (4, [1.0, float("inf")], INVALID), (4, [float("nan"), 1.0], INVALID)])
+def test_rotation_settings(handle, rotary, freq, want):
+    h = handle()
+    f = None if freq is None else np.asarray(freq, np.float64)
+    assert binding.lib.spex_tree_set_rotation(h, rotary, None if f is None else f.ctypes.data, 0) == want
+    if want == OK and rotary == 0:
+        assert append(h, [0]) == INVALID
+    assert binding.lib.spex_tree_set_rotation(None, 2, np.ones(1).ctypes.data, 0) == INVALID
+
+
+# ---- values ----------------------------------------------------------------------------------------
+def turned(x, pos, freq, rotary, interleaved):
+    """64-bit rotation of [tokens, heads, dim]."""
+    x = x.double().cpu()
+    t = torch.as_tensor(np.asarray(pos, np.float64))[:, None, None] * torch.as_tensor(np.asarray(freq, np.float64))
+    c, s = torch.cos(t), torch.sin(t)
+    i = torch.arange(rotary // 2)
+    a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + rotary // 2)
+    y = x.clone()
+    y[..., a], y[..., b] = x[..., a] * c - x[..., b] * s, x[..., b] * c + x[..., a] * s
+    return y
+
+
+def magnitude(x, rotary, interleaved):
+    """|x1| + |x2| of each dim's pair (0 where a dim is not rotated)."""
+    x = x.double().cpu().abs()
+    i = torch.arange(rotary // 2)
+    a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + rotary // 2)
+    m = torch.zeros_like(x)
+    m[..., a] = m[..., b] = x[..., a] + x[..., b]
+    return m
+
+
+def assert_rotated(got, x, pos, freq, rotary, interleaved, what=""):
+    """Cosine and sine are off by half a step of fp32 (2^-24 of at most 1), two products by 2^-24 of their size and the
+    sum by 2^-24: at most 3 * 2^-24 (|x1| + |x2|), a little more for the angle; then half a step of the result's type."""
+    want = turned(x, pos, freq, rotary, interleaved)
+    half = 2.0 ** -8 if got.dtype == torch.bfloat16 else 2.0 ** -24
+    bound = 3.2 * 2.0 ** -24 * magnitude(x, rotary, interleaved) + half * want.abs() * 1.0001 + 1e-38
+    off = (got.double().cpu() - want).abs()
+    assert bool((off <= bound).all()), (what, float((off / bound).max()))
+    same = torch.ones(x.shape[-1], dtype=torch.bool)
+    same[:rotary] = False
+    assert torch.equal(got.cpu()[..., same], x.cpu()[..., same]), what
+
+
+def assert_encoded(codes, scales, value, slack, what=""):
+    """e4m3 codes [t, h, d] and scales [t, h] of values known to within `slack`: half a step is 2^-4 of a normal result and
+    2^-10 of the scale below 2^-6 of it; 1 / scale and its product add three roundings of fp32; results saturate at 448."""
+    got = codes.cpu().view(torch.float8_e4m3fn).double() * scales.double().cpu()[..., None]
+    s = scales.double().cpu()[..., None].expand_as(got)
+    want = torch.maximum(torch.minimum(value, 448 * s), -448 * s)
+    bound = torch.maximum(want.abs() * 2.0 ** -4, s * 2.0 ** -10) * 1.0001 + slack
+    off = (got - want).abs()
+    assert bool((off <= bound).all()), (what, float((off / bound).max()))
+
+
+FREQ = lambda r, base=10000.0: base ** (-np.arange(0, r, 2) / r)  # noqa: E731
+# heads, page, rotary, interleaved; rows of 16-byte pieces in both pool layouts, and rows or rotated parts that are not
+SHAPES = [((8, 2, 128), 16, 128, False), ((8, 2, 128), 16, 128, True), ((6, 3, 64), 16, 64, False), ((8, 8, 64), 16, 32, True), ((4, 1, 128), 16, 32, False),
+          ((4, 2, 40), 16, 40, True), ((4, 2, 40), 16, 40, False), ((6, 2, 96), 32, 96, False), ((2, 2, 256), 64, 256, False),
+          ((2, 1, 128), 16, 20, True), ((4, 2, 7), 4, 6, False), ((4, 2, 7), 1, 2, True), ((10, 5, 128), 8, 64, True), ((4, 4, 256), 16, 2, False)]
+
+
+def tree_of(heads, page, kv, num_pages, rotary, interleaved, freq=None, **kw):
+    t = spex.SpexTree(heads[0], heads[1], heads[2], page, "f32" if kv == "f32" else "bf16", kv, num_pages=num_pages, device="cuda",
+                      pool_fill=0xFF, **kw)
+    t.set_rotation(rotary, FREQ(rotary) if freq is None else freq, interleaved=interleaved)
+    return t
+
+
+def draw(n, heads, kv, seed, shift=0, fused=False):
+    hq, hkv, d = heads
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    if fused:
+        x = torch.randn((n, hq + 2 * hkv, d), generator=g, device="cuda").to(SRC[kv])
+        return x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:]
+    return tuple(torch.randn((n * h * d + shift,), generator=g, device="cuda").to(SRC[kv])[shift:].view(n, h, d) for h in (hq, hkv, hkv))
+
+
+def check_node(t, u, first, k, v, pos, kv, freq, rotary, interleaved, page, what=""):
+    """Tokens first .. of node u against unrotated k and v; fp8 scales are taken as stored."""
+    n = k.shape[0]
+    gk, gv, ks, vs = t.gather_kv(u, first, n)
+    if kv == "fp8_e4m3":
+        assert_encoded(gk, ks, turned(k, pos, freq, rotary, interleaved), 3.2 * 2.0 ** -24 * magnitude(k, rotary, interleaved) + 1e-12, what)
+        assert_encoded(gv, vs, v.double().cpu(), 1e-12, what)
+    else:
+        assert_rotated(gk.view(SRC[kv]), k, pos, freq, rotary, interleaved, what)
+        if kv == "bf16" and page == 16 and k.shape[2] in (64, 128):
+            assert_v_round_trip(gv.view(SRC[kv]), v)
+        else:
+            assert torch.equal(gv.view(SRC[kv]), v.contiguous()), what
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3", "f32"])
+@pytest.mark.parametrize("heads,page,rotary,interleaved", SHAPES, ids=str)
+@pytest.mark.parametrize("fused,shift", [(False, 0), (True, 0), (False, 1)])
+def test_several_nodes_at_once(kv, heads, page, rotary, interleaved, fused, shift):
+    """Three calls for five nodes: starting pages, ending inside them, continuing them, over page borders; counts of zero."""
+    freq = FREQ(rotary)
+    t = tree_of(heads, page, kv, 400, rotary, interleaved)
+    (root,) = t.fork(-1, 1)
+    t.append_step(root, None, None, n_tokens=5)
+    nodes = t.fork(root, 4) + t.fork(-1, 1)
+    nodes = [nodes[i] for i in (2, 0, 4, 1, 3)]                    # not ascending
+    start = {u: (0 if u == max(nodes) else 5) for u in nodes}
+    done = {u: [] for u in nodes}
+    for call, counts in enumerate(([1, 0, page, 3, 2 * page + 1], [1, 1, 1, 1, 1], [page, 2, 0, page + 3, 1])):
+        total = sum(counts)
+        q, k, v = draw(total, heads, kv, 10 * call + 1, shift, fused)
+        before = [x.clone() for x in (q, k, v)]
+        at_page = [t.node_info(u)["n_tokens"] for u in nodes]
+        q_out, k_out = t.append_rotated(nodes, None if call == 1 else counts, q, k, v, want_k=True)
+        assert all(torch.equal(x, y) for x, y in zip((q, k, v), before))
+        pos = np.concatenate([start[u] + a + np.arange(c) for u, a, c in zip(nodes, at_page, counts)])
+        assert_rotated(q_out, q, pos, freq, rotary, interleaved, ("q", call))
+        assert_rotated(k_out, k, pos, freq, rotary, interleaved, ("k", call))
+        at = 0
+        for u, a, c in zip(nodes, at_page, counts):
+            if c:
+                assert t.node_info(u)["n_tokens"] == a + c
+                done[u].append((a, k[at:at + c], v[at:at + c], pos[at:at + c]))
+            at += c
+    for u in nodes:                                               # everything, once all calls are through
+        for a, k, v, pos in done[u]:
+            check_node(t, u, a, k, v, pos, kv, freq, rotary, interleaved, page, (u, a))
+    # unused slots of the last pages are zero
+    esz = {"f32": 4, "bf16": 2, "fp8_e4m3": 1}[kv]
+    tile = page * heads[2] * esz
+    for u in nodes:
+        pages, valid = t.path_pages(u)
+        left = page - valid[-1]
+        for pool in (t.k_pool, t.v_pool):
+            for h in range(heads[1]):
+                x = pool[(pages[-1] * heads[1] + h) * tile:][:tile].view({4: torch.int32, 2: torch.int16, 1: torch.uint8}[esz])
+                assert int((x == 0).sum()) >= left * heads[2]
+    t.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads,page", [((8, 2, 128), 16), ((4, 2, 64), 16), ((4, 2, 96), 32), ((3, 3, 20), 8)], ids=str)
+def test_page_scales_computed_and_given(heads, page):
+    """Without scales a started page has max(amax / 448, 2^-40) of the call's tokens in it, per head, from the rotated keys; with
+    scales theirs, row by row in the order of the pages; a page of zeros, and a scale of zero, hold zeros."""
+    rotary = heads[2] // 4 * 2
+    freq, n = FREQ(rotary), 2 * page + 3
+    t = tree_of(heads, page, "fp8_e4m3", 40, rotary, False)
+    a, b, z = t.fork(-1, 3)
+    q, k, v = draw(2 * n + 1, heads, "fp8_e4m3", 3)
+    k[-1], v[-1] = 0, 0
+    t.append_rotated([a, b, z], [n, n, 1], q, k, v)
+    want_k = turned(k, np.concatenate([np.arange(n), np.arange(n), [0]]), freq, rotary, False)
+    for u, at, count in ((a, 0, n), (b, n, n), (z, 2 * n, 1)):
+        _, _, ks, vs = t.gather_kv(u, 0, count)
+        for p in range(0, count, page):
+            m = min(page, count - p)
+            for s, x in ((ks, want_k[at + p:at + p + m]), (vs, v.double().cpu()[at + p:at + p + m])):
+                top = (x.abs().amax(dim=(0, 2)) / 448).clamp_min(2.0 ** -40)
+                # fp32 rotation (3.2 * 2^-24 of |x1| + |x2| <= 1.5 |y|, doubled for the larger pair) and one division
+                assert bool(((s[p].double().cpu() - top).abs() <= 8 * 2.0 ** -24 * top * 1.5).all())
+                assert bool((s[p:p + m] == s[p]).all())
+    gk, gv, _, _ = t.gather_kv(z, 0, 1)
+    assert not gk.any() and not gv.any()
+    # given scales: three pages for c, none for b's continued page, one for d
+    c, d = t.fork(-1, 2)
+    ks = torch.rand((4, heads[1]), device="cuda") * 0.01 + 0.004
+    vs = torch.rand((4, heads[1]), device="cuda") * 0.01 + 0.004
+    ks[3], vs[3] = 0.0, 0.0
+    counts = [n, 1, 1]
+    q, k, v = draw(n + 2, heads, "fp8_e4m3", 4)
+    old = t.gather_kv(b, n - 1, 1)[2:]
+    t.append_rotated([c, b, d], counts, q, k, v, k_scales=ks, v_scales=vs)
+    _, _, gs, hs = t.gather_kv(c, 0, n)
+    rows = torch.arange(n, device="cuda") // page
+    assert torch.equal(gs, ks[rows]) and torch.equal(hs, vs[rows])
+    assert torch.equal(t.gather_kv(b, n, 1)[2], old[0]) and torch.equal(t.gather_kv(b, n, 1)[3], old[1])
+    gk, gv, gs, _ = t.gather_kv(d, 0, 1)
+    decoded = [x.cpu().view(torch.float8_e4m3fn).float() * 0.0 for x in (gk, gv)]
+    assert not gs.any() and all(bool((x == 0).all()) for x in decoded)       # finite codes: 0 times them is 0
+    check_node(t, c, 0, k[:n], v[:n], np.arange(n), "fp8_e4m3", freq, rotary, False, page)
+    check_node(t, b, n, k[n:n + 1], v[n:n + 1], [n], "fp8_e4m3", freq, rotary, False, page)
+    t.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3", "f32"])
+@pytest.mark.parametrize("rotary,interleaved", [(128, False), (128, True), (20, False)])
+def test_positions_given_and_far(kv, rotary, interleaved):
+    """Positions up to INT32_MAX: the angle is off by less than fp32's half step however far.  The 64-bit reference itself loses the angle
+    there, so it takes frequencies that are powers of two times 2 pi / 2^k, whose turns are exact."""
+    heads = (4, 2, 128)
+    freq = 2 * np.pi * 2.0 ** -(np.arange(rotary // 2) % 40 + 1)
+    t = tree_of(heads, 16, kv, 20, rotary, interleaved, freq)
+    (u,) = t.fork(-1, 1)
+    pos = np.array([0, 1, 2, 7, 4095, 65537, (1 << 20) + 3, (1 << 24) + 1, (1 << 30) + 5, (1 << 31) - 1], np.int32)
+    q, k, v = draw(len(pos), heads, kv, 5)
+    q_out, k_out = t.append_rotated([u], [len(pos)], q, k, v, positions=pos, want_k=True)
+    turns = pos.astype(np.float64)[:, None] * 2.0 ** -(np.arange(rotary // 2) % 40 + 1)
+    # np.pi is a little less than pi: 2 * np.pi is 1 - short whole turns
+    short = -np.sin(2 * np.pi) / (2 * np.pi)
+    turns = np.mod(turns, 1.0) - turns * short
+    for got, x in ((q_out, q), (k_out, k)):
+        for i, row in enumerate(turns):                           # a rotation by `turns` at position 1
+            assert_rotated(got[i:i + 1], x[i:i + 1], [1.0], 2 * np.pi * row, rotary, interleaved, int(pos[i]))
+    t.close()
+
+
+@pytest.mark.gpu
+def test_angles_between_the_exact_ones():
+    """Angles that are no fractions of a turn, against cosines in 64 bits: positions below 2^20 times frequencies of at most 1 are known there
+    to 2^-33."""
+    heads, rotary = (2, 1, 256), 256
+    t = tree_of(heads, 16, "f32", 200, rotary, False)
+    (u,) = t.fork(-1, 1)
+    pos = np.random.default_rng(0).integers(0, 1 << 20, 2000).astype(np.int32)
+    q, k, v = draw(len(pos), heads, "f32", 6)
+    q_out, _ = t.append_rotated([u], [len(pos)], q, k, v, positions=pos)
+    assert_rotated(q_out, q, pos, FREQ(rotary), rotary, False)
+    t.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3", "f32"])
+@pytest.mark.parametrize("heads,rotary", [((8, 2, 128), 128), ((4, 2, 20), 10)], ids=str)
+def test_in_place_and_without_queries(kv, heads, rotary):
+    results = []
+    for mode in ("apart", "in place", "keys only"):
+        t = tree_of(heads, 16, kv, 20, rotary, False)
+        nodes = t.fork(-1, 2)
+        q, k, v = draw(30, heads, kv, 7, fused=True)
+        if mode == "keys only":
+            assert t.append_rotated(nodes, [19, 11], None, k, v) == (None, None)
+            q_out = k_out = None
+        else:
+            q_out, k_out = t.append_rotated(nodes, [19, 11], q, k, v, want_k=True, **(dict(q_out=q, k_out=k) if mode == "in place" else {}))
+        results.append((q_out, k_out, [t.gather_kv(u, 0, n) for u, n in zip(nodes, (19, 11))]))
+        t.close()
+    (qa, ka, ca), (qb, kb, cb), (_, _, cc) = results
+    assert torch.equal(qa, qb) and torch.equal(ka, kb)
+    for x, y, z in zip(ca, cb, cc):
+        for i in range(4 if kv == "fp8_e4m3" else 2):
+            assert torch.equal(x[i], y[i]) and torch.equal(x[i], z[i])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3", "f32"])
+def test_rows_around_are_left_alone(kv):
+    """Windows of larger tensors and of a pool: what lies around them stays."""
+    heads = (4, 2, 64)
+    t = tree_of(heads, 16, kv, 6, 64, False, interleave_kv=True)
+    (u,) = t.fork(-1, 1)
+    q, k, v = draw(20, heads, kv, 8)
+    big_q = torch.full((30, 6, 64), 9.0, dtype=SRC[kv], device="cuda")
+    big_k = torch.full((30, 4, 64), 9.0, dtype=SRC[kv], device="cuda")
+    t.append_rotated([u], [20], q, k, v, q_out=big_q[4:24, 1:5], k_out=big_k[4:24, 1:3])
+    assert_rotated(big_q[4:24, 1:5], q, np.arange(20), FREQ(64), 64, False)
+    check_node(t, u, 0, k, v, np.arange(20), kv, FREQ(64), 64, False, 16)
+    big_q[4:24, 1:5], big_k[4:24, 1:3] = 9.0, 9.0
+    assert bool((big_q == 9.0).all()) and bool((big_k == 9.0).all())
+    page_bytes = t.k_pool.numel() // 6
+    assert bool((t.k_pool[2 * page_bytes:] == 0xFF).all())         # pages that were not taken
+    t.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3"])
+def test_refused_calls_change_nothing_on_a_live_tree(kv):
+    heads = (4, 2, 128)
+    t = tree_of(heads, 16, kv, 3, 128, False)
+    a, b = t.fork(-1, 2)
+    q, k, v = draw(40, heads, kv, 9)
+    t.append_rotated([a], [20], q[:20], k[:20], v[:20])
+    before = [x.clone() for x in (t.k_pool, t.v_pool)]
+    for bad in (lambda: t.append_rotated([a, b], [20, 20], q, k, v), lambda: t.append_rotated([a, a], [20, 20], q, k, v),
+                lambda: t.append_rotated([a, 7], [20, 20], q, k, v)):
+        with pytest.raises(spex.SpexError):
+            bad()
+    assert t.node_info(a)["n_tokens"] == 20 and t.node_info(b)["n_tokens"] == 0 and len(t.free_pages()) == 1
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(before, (t.k_pool, t.v_pool)))
+    t.close()
+
+
+@pytest.mark.gpu
+def test_another_rotation_for_later_calls_and_other_streams():
+    """A setting holds for the calls made while it stands, also where those still run when it is replaced."""
+    heads = (8, 2, 128)
+    t = tree_of(heads, 16, "bf16", 300, 128, False)
+    (u,) = t.fork(-1, 1)
+    side = torch.cuda.Stream()
+    outs = []
+    for i, (rotary, inter, base) in enumerate([(128, False, 1e4), (64, True, 1e6), (128, True, 5e5), (2, False, 10.0)]):
+        t.set_rotation(rotary, base=base, interleaved=inter)
+        q, k, v = draw(1000, heads, "bf16", 20 + i)
+        stream = side if i % 2 else torch.cuda.current_stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            q_out, _ = t.append_rotated([u], [1000], q, k, v)
+        outs.append((q_out, q, 1000 * i, base, rotary, inter))
+    torch.cuda.synchronize()
+    for q_out, q, at, base, rotary, inter in outs:
+        assert_rotated(q_out, q, at + np.arange(1000), FREQ(rotary, base), rotary, inter)
+    t.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3"])
+def test_a_search_from_its_prompts_on(kv):
+    """The operators together, as a serving program runs them: prompts rotated and appended, attention over them from the rotated
+    tensors, then branches generated token by token with decode_attention over what the appends left, every result against
+    the definition.  The cached launch lists follow the appends (plan state 2)."""
+    hq, hkv, d = heads = (8, 2, 128)
+    lens, base = [70, 33], 1e4
+    freq = FREQ(d, base)
+    t = tree_of(heads, 16, kv, 64, d, False)
+    roots = t.fork(-1, 2)
+    q, k, v = draw(sum(lens), heads, kv, 30, fused=True)
+    q_rot, k_rot = t.append_rotated(roots, lens, q, k, v, want_k=True)
+    out, _ = spex.prompt_attention(lens, q_rot, k_rot, v, d ** -0.5)
+
+    def attention(qr, keys, values):
+        """qr [Hq, D] over keys, values [n, Hkv, D], 64 bits; also the weighted mean of |v|."""
+        keys, values = (x.repeat_interleave(hq // hkv, 1).transpose(0, 1) for x in (keys, values))
+        w = torch.softmax((keys @ qr[..., None])[..., 0] * d ** -0.5, -1)
+        return (w[..., None] * values).sum(1), (w[..., None] * values.abs()).sum(1)
+
+    pos = np.concatenate([np.arange(n) for n in lens])
+    kt, vt, qt = turned(k, pos, freq, d, False), v.double().cpu(), turned(q, pos, freq, d, False)
+    at = 0
+    for n in lens:
+        for i in (0, n // 2, n - 1):
+            want, mean = attention(qt[at + i], kt[at:at + i + 1], vt[at:at + i + 1])
+            # q and k rounded to bf16 (2^-8 each) move a score by at most 2 * 2^-8 sum|q k| scale; a weight follows it twice
+            moved = 4 * 2.0 ** -8 * float((qt[at + i].abs().amax() * kt[at:at + i + 1].abs().sum(-1)).max()) * d ** -0.5
+            assert bool(((out[at + i].double().cpu() - want).abs() <= mean * min(2.0, moved) + 2.0 ** -7 * (mean + want.abs())).all())
+        at += n
+    # what attention saw, exactly: the rotated tensors as they were rounded
+    kr, vr = k_rot.double().cpu(), v.double().cpu()
+    want, mean = attention(q_rot[at - 1].double().cpu(), kr[lens[0]:], vr[lens[0]:])
+    assert bool(((out[at - 1].double().cpu() - want).abs() <= 2.0 ** -8 * 1.02 * (mean + want.abs())).all())
+
+    branches = [b for r in roots for b in t.fork(r, 3)]
+    paths = {b: roots[i // 3] for i, b in enumerate(branches)}
+    states = []
+    for step in range(20):
+        q, k, v = draw(len(branches), heads, kv, 40 + step, fused=True)
+        q_rot, _ = t.append_rotated(branches, None, q, k, v)
+        out, lse = t.decode_attention(branches, None, q_rot, d ** -0.5)
+        states.append(t.last_launch_info()["plan_rebuilt"])
+        if step in (0, 7, 16, 19):
+            for i in (0, 2, 5):
+                b = branches[i]
+                parts = [t.gather_kv(u, 0, t.node_info(u)["n_tokens"]) for u in (paths[b], b)]
+                if kv == "fp8_e4m3":
+                    keys, values = (torch.cat([p[j].view(torch.float8_e4m3fn).double() * p[j + 2].double()[..., None] for p in parts]).cpu() for j in (0, 1))
+                else:
+                    keys, values = (torch.cat([p[j].double() for p in parts]).cpu() for j in (0, 1))
+                want, _ = attention(q_rot[i].double().cpu(), keys, values)
+                assert float((out[i].double().cpu() - want).abs().max()) <= 2e-3
+    assert states.count(2) >= 17 and states[0] == 1                # patched in the append's own launch, planned afresh at most now and then
+    t.close()
