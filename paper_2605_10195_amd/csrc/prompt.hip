@@ -85,12 +85,19 @@ __device__ __forceinline__ RowSet row_set(const PromptArgs &p, int wave) {
   return r;
 }
 
+// Rows of one head from token t0 on, as a buffer of the bytes that follow.
+__device__ __forceinline__ u32x4 rows_from(const char *base, int64_t stride_b, int t0, int len, int row_b) {
+  const uint64_t at = reinterpret_cast<uint64_t>(base) + static_cast<int64_t>(t0) * stride_b;
+  const int64_t left = static_cast<int64_t>(len - 1 - t0) * stride_b + row_b;
+  return u32x4{static_cast<uint32_t>(at), static_cast<uint32_t>(at >> 32) & 0xffffu, static_cast<uint32_t>(min(left, int64_t(0x7fffffff))), 0x00020000u};
+}
 // 16 bytes a lane from memory to LDS, to lds + 16 * lane.  In assembly, because the compiler lets every transposing read wait for
 // all such copies under way, those into the other buffers too; tile_barrier() is what waits for them.  (The compiler keeps nothing
 // in m0 between instructions of its own.)
-__device__ __forceinline__ void copy_to_lds(const void *src, lds_char *lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(uniform(static_cast<int>(reinterpret_cast<uintptr_t>(lds)))),
-               "v"(src)
+__device__ __forceinline__ void copy_to_lds(const u32x4 rows, int lane_off, int off, lds_char *lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(
+                   uniform(static_cast<int>(reinterpret_cast<uintptr_t>(lds)))),
+               "v"(lane_off), "s"(rows), "s"(off)
                : "memory");
 }
 // Behind it every wavefront's copies have landed, and none of them reads LDS of the step before.
@@ -113,18 +120,48 @@ struct TileB {
   static constexpr int kBytes = kKeys * kRowB;
 };
 
-// One tile of K or V (64 tokens from t0, those past the prompt repeat its last; pieces past the head repeat its last, which
-// meet zeros of q or dims that are not stored).
-template <int DP, int NW>
-__device__ __forceinline__ void stage_tile(const char *src, int64_t stride_b, int t0, int len, int pieces, lds_char *lds, int wave, int lane) {
-  constexpr int ROWB = TileB<DP>::kRowB, PER = ROWB / 16, ROUNDS = TileB<DP>::kBytes / 1024 / NW;
+// Copies tiles of KEYS tokens of one head, ROWB bytes a row in LDS, into LDS; place(t, c) is where piece c of row t lies in its row.
+// Tokens past the prompt repeat its last; pieces past the head repeat its last, which meet zeros of q or dims that are not stored.
+// A wavefront's rounds are a fixed number of rows apart, so that in all but a prompt's last tile the offsets of a lane are the
+// same from tile to tile and the rest is scalar.
+template <int KEYS, int ROWB, int NW, class Place>
+struct Stager {
+  static constexpr int PER = ROWB / 16, ROUNDS = KEYS * ROWB / 1024 / NW, STEP = NW * 64 / PER;  // STEP: rows a round
+  static constexpr int KINDS = STEP >= 16 ? 1 : 16 / STEP;  // rounds whose pieces lie differently: places repeat every 16 rows
+  static_assert(ROUNDS % KINDS == 0, "");
+  const char *base;
+  int64_t stride_b;
+  int len, row_b, row[KINDS], piece[KINDS], off[KINDS];
+  __device__ __forceinline__ Stager(const char *b, int64_t s, int n, int bytes, int wave, int lane) : base(b), stride_b(s), len(n), row_b(bytes) {
 #pragma unroll
-  for (int i = 0; i < ROUNDS; ++i) {
-    const int at = (i * NW + wave) * 64 + lane;
-    const int t = at / PER, c = (at % PER) ^ swz<ROWB>(t);
-    copy_to_lds(src + static_cast<int64_t>(min(t0 + t, len - 1)) * stride_b + min(c, pieces - 1) * 16, lds + (i * NW + wave) * 1024);
+    for (int k = 0; k < KINDS; ++k) {
+      const int at = (k * NW + wave) * 64 + lane;
+      row[k] = at / PER;
+      piece[k] = min(Place::at(row[k], at % PER), row_b / 16 - 1) * 16;
+      off[k] = row[k] * static_cast<int>(stride_b) + piece[k];
+    }
   }
-}
+  __device__ __forceinline__ void tile(int t0, lds_char *lds, int wave) const {
+    const u32x4 rows = rows_from(base, stride_b, t0, len, row_b);
+    if (t0 + KEYS <= len) {
+#pragma unroll
+      for (int i = 0; i < ROUNDS; ++i)
+        copy_to_lds(rows, off[i % KINDS], i / KINDS * KINDS * STEP * static_cast<int>(stride_b), lds + (i * NW + wave) * 1024);
+    } else {
+#pragma unroll
+      for (int i = 0; i < ROUNDS; ++i)
+        copy_to_lds(rows, min(row[i % KINDS] + i / KINDS * KINDS * STEP, len - 1 - t0) * static_cast<int>(stride_b) + piece[i % KINDS], 0,
+                    lds + (i * NW + wave) * 1024);
+    }
+  }
+};
+template <int ROWB>
+struct PlaceB {
+  static __device__ __forceinline__ int at(int t, int c) { return c ^ swz<ROWB>(t); }
+};
+struct PlaceF {
+  static __device__ __forceinline__ int at(int t, int c) { return c ^ (t & 15); }
+};
 
 template <int DP, int NW>
 __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_kernel(PromptArgs p) {
@@ -134,11 +171,11 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_k
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
   const RowSet rs = row_set<NW>(p, wave);
   const int pieces = p.D / 8;
-  const char *kbase = static_cast<const char *>(p.k) + (rs.row0 * p.k_stride + rs.kv * p.D) * 2;
-  const char *vbase = static_cast<const char *>(p.v) + (rs.row0 * p.v_stride + rs.kv * p.D) * 2;
+  const Stager<64, ROWB, NW, PlaceB<ROWB>> ks(static_cast<const char *>(p.k) + (rs.row0 * p.k_stride + rs.kv * p.D) * 2, p.k_stride * 2, rs.len, p.D * 2, wave, lane);
+  const Stager<64, ROWB, NW, PlaceB<ROWB>> vs(static_cast<const char *>(p.v) + (rs.row0 * p.v_stride + rs.kv * p.D) * 2, p.v_stride * 2, rs.len, p.D * 2, wave, lane);
   const int tiles = rs.last / 64 + 1, mine = rs.live ? min(rs.q0 + kPromptRows - 1, rs.len - 1) / 64 + 1 : 0;
-  stage_tile<DP, NW>(kbase, p.k_stride * 2, 0, rs.len, pieces, lds, wave, lane);
-  stage_tile<DP, NW>(vbase, p.v_stride * 2, 0, rs.len, pieces, lds + 2 * TILE, wave, lane);
+  ks.tile(0, lds, wave);
+  vs.tile(0, lds + 2 * TILE, wave);
 
   bf16x8 qf[KS];
   {
@@ -175,8 +212,8 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_k
     tile_barrier();
     lds_char *kt = lds + (t & 1) * TILE, *vt = lds + (2 + (t & 1)) * TILE;
     if (t + 1 < tiles) {
-      stage_tile<DP, NW>(kbase, p.k_stride * 2, (t + 1) * 64, rs.len, pieces, lds + ((t + 1) & 1) * TILE, wave, lane);
-      stage_tile<DP, NW>(vbase, p.v_stride * 2, (t + 1) * 64, rs.len, pieces, lds + (2 + ((t + 1) & 1)) * TILE, wave, lane);
+      ks.tile((t + 1) * 64, lds + ((t + 1) & 1) * TILE, wave);
+      vs.tile((t + 1) * 64, lds + (2 + ((t + 1) & 1)) * TILE, wave);
     }
     if (t >= mine) continue;
     f32x16 s[2];
@@ -250,17 +287,6 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_k
 // ---- fp32 ----------------------------------------------------------------------------------------
 // Tiles of 32 keys; piece c (four dims) of row t at place c ^ (t & 15).
 template <int DP, int NW>
-__device__ __forceinline__ void stage_tile_f32(const char *src, int64_t stride_b, int t0, int len, int pieces, lds_char *lds, int wave, int lane) {
-  constexpr int PER = DP / 4, ROUNDS = 32 * DP * 4 / 1024 / NW;
-#pragma unroll
-  for (int i = 0; i < ROUNDS; ++i) {
-    const int at = (i * NW + wave) * 64 + lane;
-    const int t = at / PER, c = (at % PER) ^ (t & 15);
-    copy_to_lds(src + static_cast<int64_t>(min(t0 + t, len - 1)) * stride_b + min(c, pieces - 1) * 16, lds + (i * NW + wave) * 1024);
-  }
-}
-
-template <int DP, int NW>
 __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_f32_kernel(PromptArgs p) {
   constexpr int ROWB = DP * 4, TILE = 32 * ROWB, KS = DP / 8, DT = DP / 32;
   __shared__ __attribute__((aligned(1024))) char lds_[4 * TILE];
@@ -268,11 +294,11 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_f32_ke
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
   const RowSet rs = row_set<NW>(p, wave);
   const int pieces = p.D / 4;
-  const char *kbase = static_cast<const char *>(p.k) + (rs.row0 * p.k_stride + rs.kv * p.D) * 4;
-  const char *vbase = static_cast<const char *>(p.v) + (rs.row0 * p.v_stride + rs.kv * p.D) * 4;
+  const Stager<32, ROWB, NW, PlaceF> ks(static_cast<const char *>(p.k) + (rs.row0 * p.k_stride + rs.kv * p.D) * 4, p.k_stride * 4, rs.len, p.D * 4, wave, lane);
+  const Stager<32, ROWB, NW, PlaceF> vs(static_cast<const char *>(p.v) + (rs.row0 * p.v_stride + rs.kv * p.D) * 4, p.v_stride * 4, rs.len, p.D * 4, wave, lane);
   const int tiles = rs.last / 32 + 1, mine = rs.live ? min(rs.q0 + kPromptRows - 1, rs.len - 1) / 32 + 1 : 0;
-  stage_tile_f32<DP, NW>(kbase, p.k_stride * 4, 0, rs.len, pieces, lds, wave, lane);
-  stage_tile_f32<DP, NW>(vbase, p.v_stride * 4, 0, rs.len, pieces, lds + 2 * TILE, wave, lane);
+  ks.tile(0, lds, wave);
+  vs.tile(0, lds + 2 * TILE, wave);
   f32x4 qf[KS];
   {
     const char *qrow = static_cast<const char *>(p.q) +
@@ -299,8 +325,8 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_f32_ke
     tile_barrier();
     lds_char *kt = lds + (t & 1) * TILE, *vt = lds + (2 + (t & 1)) * TILE;
     if (t + 1 < tiles) {
-      stage_tile_f32<DP, NW>(kbase, p.k_stride * 4, (t + 1) * 32, rs.len, pieces, lds + ((t + 1) & 1) * TILE, wave, lane);
-      stage_tile_f32<DP, NW>(vbase, p.v_stride * 4, (t + 1) * 32, rs.len, pieces, lds + (2 + ((t + 1) & 1)) * TILE, wave, lane);
+      ks.tile((t + 1) * 32, lds + ((t + 1) & 1) * TILE, wave);
+      vs.tile((t + 1) * 32, lds + (2 + ((t + 1) & 1)) * TILE, wave);
     }
     if (t >= mine) continue;
     f32x16 s;
