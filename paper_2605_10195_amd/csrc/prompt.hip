@@ -120,10 +120,10 @@ struct TileB {
   static constexpr int kBytes = kKeys * kRowB;
 };
 
-// Copies tiles of KEYS tokens of one head, ROWB bytes a row in LDS, into LDS; place(t, c) is where piece c of row t lies in its row.
-// Tokens past the prompt repeat its last; pieces past the head repeat its last, which meet zeros of q or dims that are not stored.
-// A wavefront's rounds are a fixed number of rows apart, so that in all but a prompt's last tile the offsets of a lane are the
-// same from tile to tile and the rest is scalar.
+// Copies tiles of KEYS tokens of one head, ROWB bytes a row in LDS, into LDS; Place::at(t, c) is where piece c of row t lies in its
+// row.  Tokens past the prompt lie behind the end of the buffer and come out as zeros; pieces past the head repeat its last, which
+// meet zeros of q or dims that are not stored.  A wavefront's rounds are a fixed number of rows apart, so that a lane's
+// offsets are the same from tile to tile and the rest is scalar.
 template <int KEYS, int ROWB, int NW, class Place>
 struct Stager {
   static constexpr int PER = ROWB / 16, ROUNDS = KEYS * ROWB / 1024 / NW, STEP = NW * 64 / PER;  // STEP: rows a round
@@ -131,28 +131,20 @@ struct Stager {
   static_assert(ROUNDS % KINDS == 0, "");
   const char *base;
   int64_t stride_b;
-  int len, row_b, row[KINDS], piece[KINDS], off[KINDS];
+  int len, row_b, off[KINDS];
   __device__ __forceinline__ Stager(const char *b, int64_t s, int n, int bytes, int wave, int lane) : base(b), stride_b(s), len(n), row_b(bytes) {
 #pragma unroll
     for (int k = 0; k < KINDS; ++k) {
-      const int at = (k * NW + wave) * 64 + lane;
-      row[k] = at / PER;
-      piece[k] = min(Place::at(row[k], at % PER), row_b / 16 - 1) * 16;
-      off[k] = row[k] * static_cast<int>(stride_b) + piece[k];
+      const int at = (k * NW + wave) * 64 + lane, row = at / PER;
+      off[k] = row * static_cast<int>(stride_b) + min(Place::at(row, at % PER), row_b / 16 - 1) * 16;
     }
   }
-  __device__ __forceinline__ void tile(int t0, lds_char *lds, int wave) const {
+  // lds: of the wavefront's first round
+  __device__ __forceinline__ void tile(int t0, lds_char *lds) const {
     const u32x4 rows = rows_from(base, stride_b, t0, len, row_b);
-    if (t0 + KEYS <= len) {
+    const int step_b = KINDS * STEP * static_cast<int>(stride_b);
 #pragma unroll
-      for (int i = 0; i < ROUNDS; ++i)
-        copy_to_lds(rows, off[i % KINDS], i / KINDS * KINDS * STEP * static_cast<int>(stride_b), lds + (i * NW + wave) * 1024);
-    } else {
-#pragma unroll
-      for (int i = 0; i < ROUNDS; ++i)
-        copy_to_lds(rows, min(row[i % KINDS] + i / KINDS * KINDS * STEP, len - 1 - t0) * static_cast<int>(stride_b) + piece[i % KINDS], 0,
-                    lds + (i * NW + wave) * 1024);
-    }
+    for (int i = 0; i < ROUNDS; ++i) copy_to_lds(rows, off[i % KINDS], i / KINDS * step_b, lds + i * NW * 1024);
   }
 };
 template <int ROWB>
@@ -174,8 +166,9 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_k
   const Stager<64, ROWB, NW, PlaceB<ROWB>> ks(static_cast<const char *>(p.k) + (rs.row0 * p.k_stride + rs.kv * p.D) * 2, p.k_stride * 2, rs.len, p.D * 2, wave, lane);
   const Stager<64, ROWB, NW, PlaceB<ROWB>> vs(static_cast<const char *>(p.v) + (rs.row0 * p.v_stride + rs.kv * p.D) * 2, p.v_stride * 2, rs.len, p.D * 2, wave, lane);
   const int tiles = rs.last / 64 + 1, mine = rs.live ? min(rs.q0 + kPromptRows - 1, rs.len - 1) / 64 + 1 : 0;
-  ks.tile(0, lds, wave);
-  vs.tile(0, lds + 2 * TILE, wave);
+  lds_char *const mine_at = lds + wave * 1024;  // where this wavefront's copies into the first buffer go
+  ks.tile(0, mine_at);
+  vs.tile(0, mine_at + 2 * TILE);
 
   bf16x8 qf[KS];
   {
@@ -212,8 +205,9 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_k
     tile_barrier();
     lds_char *kt = lds + (t & 1) * TILE, *vt = lds + (2 + (t & 1)) * TILE;
     if (t + 1 < tiles) {
-      ks.tile((t + 1) * 64, lds + ((t + 1) & 1) * TILE, wave);
-      vs.tile((t + 1) * 64, lds + (2 + ((t + 1) & 1)) * TILE, wave);
+      lds_char *to = mine_at + (~t & 1) * TILE;
+      ks.tile((t + 1) * 64, to);
+      vs.tile((t + 1) * 64, to + 2 * TILE);
     }
     if (t >= mine) continue;
     f32x16 s[2];
@@ -297,8 +291,9 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_f32_ke
   const Stager<32, ROWB, NW, PlaceF> ks(static_cast<const char *>(p.k) + (rs.row0 * p.k_stride + rs.kv * p.D) * 4, p.k_stride * 4, rs.len, p.D * 4, wave, lane);
   const Stager<32, ROWB, NW, PlaceF> vs(static_cast<const char *>(p.v) + (rs.row0 * p.v_stride + rs.kv * p.D) * 4, p.v_stride * 4, rs.len, p.D * 4, wave, lane);
   const int tiles = rs.last / 32 + 1, mine = rs.live ? min(rs.q0 + kPromptRows - 1, rs.len - 1) / 32 + 1 : 0;
-  ks.tile(0, lds, wave);
-  vs.tile(0, lds + 2 * TILE, wave);
+  lds_char *const mine_at = lds + wave * 1024;  // where this wavefront's copies into the first buffer go
+  ks.tile(0, mine_at);
+  vs.tile(0, mine_at + 2 * TILE);
   f32x4 qf[KS];
   {
     const char *qrow = static_cast<const char *>(p.q) +
@@ -325,8 +320,9 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_f32_ke
     tile_barrier();
     lds_char *kt = lds + (t & 1) * TILE, *vt = lds + (2 + (t & 1)) * TILE;
     if (t + 1 < tiles) {
-      ks.tile((t + 1) * 32, lds + ((t + 1) & 1) * TILE, wave);
-      vs.tile((t + 1) * 32, lds + (2 + ((t + 1) & 1)) * TILE, wave);
+      lds_char *to = mine_at + (~t & 1) * TILE;
+      ks.tile((t + 1) * 32, to);
+      vs.tile((t + 1) * 32, to + 2 * TILE);
     }
     if (t >= mine) continue;
     f32x16 s;
