@@ -49,7 +49,7 @@ extern "C" spex_status_t spex_prompt_attention(const spex_prompt_config_t *cfg, 
   bool wide = cfg->head_dim % per16 == 0 && aligned16(q) && aligned16(k) && aligned16(v) && aligned16(out);
   for (int64_t s : strides) wide = wide && s % per16 == 0;
   // offsets inside a tile of up to 64 tokens are 32 bits
-  wide = wide && std::max(strides[1], strides[2]) * (16 / per16) < (int64_t(1) << 24);
+  wide = wide && std::max({strides[0], strides[1], strides[2]}) * (16 / per16) < (int64_t(1) << 24);
   const spex::PromptKernel kernel = spex::prompt_kernel(cfg->dtype == SPEX_F32, wide);
   const int32_t G = cfg->num_q_heads / cfg->num_kv_heads;
 

@@ -32,6 +32,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
 typedef __attribute__((address_space(3))) float lds_float;
 
 // Start value of the running maximum: finite, and below any score that the rows can have.
@@ -167,21 +168,17 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_k
   const Stager<64, ROWB, NW, PlaceB<ROWB>> vs(static_cast<const char *>(p.v) + (rs.row0 * p.v_stride + rs.kv * p.D) * 2, p.v_stride * 2, rs.len, p.D * 2, wave, lane);
   const int tiles = rs.last / 64 + 1, mine = rs.live ? min(rs.q0 + kPromptRows - 1, rs.len - 1) / 64 + 1 : 0;
   lds_char *const mine_at = lds + wave * 1024;  // where this wavefront's copies into the first buffer go
+  // Queries and results cross LDS, so that memory sees whole rows: as the operands lie a load or store has 32 or 16 bytes of
+  // each of 32 rows.  Every wavefront has 32 rows of the buffer that is free then: a quarter of a tile of K and one of V.
+  static_assert(NW == 4, "");
+  auto rows_at = [&](int buffer) { return lds + ((wave >> 1) * 2 + buffer) * TILE + (wave & 1) * (TILE / 2); };
+  const int64_t row = rs.row0 + rs.q0, head0 = static_cast<int64_t>(rs.live ? rs.head : 0) * p.D;
+  if (rs.live) {
+    const Stager<32, ROWB, 1, PlaceB<ROWB>> qs(static_cast<const char *>(p.q) + (row * p.q_stride + head0) * 2, p.q_stride * 2, rs.len - rs.q0, p.D * 2, 0, lane);
+    qs.tile(0, rows_at(1));
+  }
   ks.tile(0, mine_at);
   vs.tile(0, mine_at + 2 * TILE);
-
-  bf16x8 qf[KS];
-  {
-    const char *qrow = static_cast<const char *>(p.q) +
-                       ((rs.row0 + min(rs.q0 + col, rs.len - 1)) * p.q_stride + static_cast<int64_t>(rs.live ? rs.head : 0) * p.D) * 2;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const int c = 2 * s + h;
-      u32x4 x = *reinterpret_cast<const u32x4 *>(qrow + min(c, pieces - 1) * 16);
-      if (c >= pieces) x = u32x4{0, 0, 0, 0};
-      qf[s] = __builtin_bit_cast(bf16x8, x);
-    }
-  }
   // Places of the operand pieces in a tile; the other keys of the tile lie at constant distances.
   int koff[KS], voff[DT][2];
 #pragma unroll
@@ -193,6 +190,17 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_k
       const int t = 8 * j + 4 * h + ((lane & 15) >> 2), c = 4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
       voff[dt][j] = t * ROWB + (c ^ swz<ROWB>(t)) * 16 + (lane & 1) * 8;
     }
+  bf16x8 qf[KS];
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * TILE / 1024 / NW) : "memory");  // the copies of K and V are younger
+  {
+    const lds_char *rows = rows_at(1);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      u32x4 x = *(const lds_u32x4 *)(rows + koff[s]);
+      if (2 * s + h >= pieces) x = u32x4{0, 0, 0, 0};
+      qf[s] = __builtin_bit_cast(bf16x8, x);
+    }
+  }
   f32x16 o[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
@@ -261,21 +269,26 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_k
       }
     }
   }
-  if (!rs.live || qpos >= rs.len) return;
+  if (!rs.live) return;
   l += other_half(l);
-  const int64_t row = rs.row0 + qpos;
   const float inv = 1.0f / l;
-  char *out = static_cast<char *>(p.out) + (row * p.out_stride + static_cast<int64_t>(rs.head) * p.D) * 2;
+  lds_char *rows = rows_at(tiles & 1);  // the last tile lies in the others
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int d = 32 * dt + 8 * j + 4 * h;
-      if (d < p.D)
-        *reinterpret_cast<u32x2 *>(out + 2 * d) = u32x2{pack_bf16(o[dt][4 * j] * inv, o[dt][4 * j + 1] * inv),
-                                                        pack_bf16(o[dt][4 * j + 2] * inv, o[dt][4 * j + 3] * inv)};
-    }
-  if (p.lse && h == 0) p.lse[row * (static_cast<int64_t>(p.Hkv) * p.G) + rs.head] = (m + __builtin_log2f(l)) * 0.6931471805599453f;
+    for (int j = 0; j < 4; ++j)
+      *(lds_u32x2 *)(rows + col * ROWB + ((4 * dt + j) ^ swz<ROWB>(col)) * 16 + 8 * h) =
+          u32x2{pack_bf16(o[dt][4 * j] * inv, o[dt][4 * j + 1] * inv), pack_bf16(o[dt][4 * j + 2] * inv, o[dt][4 * j + 3] * inv)};
+  constexpr int PER = ROWB / 16;
+  char *out = static_cast<char *>(p.out) + (row * p.out_stride + head0) * 2;
+#pragma unroll
+  for (int i = 0; i < 32 * PER / 64; ++i) {
+    const int r = (i * 64 + lane) / PER, c = lane % PER;
+    const u32x4 x = *(const lds_u32x4 *)(rows + r * ROWB + (c ^ swz<ROWB>(r)) * 16);
+    if (rs.q0 + r < rs.len && c < pieces) *reinterpret_cast<u32x4 *>(out + r * p.out_stride * 2 + c * 16) = x;
+  }
+  if (p.lse && h == 0 && qpos < rs.len)
+    p.lse[(row + col) * (static_cast<int64_t>(p.Hkv) * p.G) + rs.head] = (m + __builtin_log2f(l)) * 0.6931471805599453f;
 }
 
 // ---- fp32 ----------------------------------------------------------------------------------------
