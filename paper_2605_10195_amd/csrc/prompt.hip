@@ -86,12 +86,6 @@ __device__ __forceinline__ RowSet row_set(const PromptArgs &p, int wave) {
   return r;
 }
 
-// Rows of one head from token t0 on, as a buffer of the bytes that follow.
-__device__ __forceinline__ u32x4 rows_from(const char *base, int64_t stride_b, int t0, int len, int row_b) {
-  const uint64_t at = reinterpret_cast<uint64_t>(base) + static_cast<int64_t>(t0) * stride_b;
-  const int64_t left = static_cast<int64_t>(len - 1 - t0) * stride_b + row_b;
-  return u32x4{static_cast<uint32_t>(at), static_cast<uint32_t>(at >> 32) & 0xffffu, static_cast<uint32_t>(min(left, int64_t(0x7fffffff))), 0x00020000u};
-}
 // 16 bytes a lane from memory to LDS, to lds + 16 * lane.  In assembly, because the compiler lets every transposing read wait for
 // all such copies under way, those into the other buffers too; tile_barrier() is what waits for them.  (The compiler keeps nothing
 // in m0 between instructions of its own.)
@@ -130,22 +124,27 @@ struct Stager {
   static constexpr int PER = ROWB / 16, ROUNDS = KEYS * ROWB / 1024 / NW, STEP = NW * 64 / PER;  // STEP: rows a round
   static constexpr int KINDS = STEP >= 16 ? 1 : 16 / STEP;  // rounds whose pieces lie differently: places repeat every 16 rows
   static_assert(ROUNDS % KINDS == 0, "");
-  const char *base;
-  int64_t stride_b;
-  int len, row_b, off[KINDS];
-  __device__ __forceinline__ Stager(const char *b, int64_t s, int n, int bytes, int wave, int lane) : base(b), stride_b(s), len(n), row_b(bytes) {
+  uint64_t at;    // first row of the next tile
+  int64_t left;   // bytes from there to the end of the prompt's last row
+  int64_t tile_b; // bytes from tile to tile
+  int step_b, off[KINDS];
+  // base: first row
+  __device__ __forceinline__ Stager(const char *base, int64_t stride_b, int len, int row_b, int wave, int lane)
+      : at(reinterpret_cast<uint64_t>(base)), left((len - 1) * stride_b + row_b), tile_b(KEYS * stride_b), step_b(KINDS * STEP * static_cast<int>(stride_b)) {
 #pragma unroll
     for (int k = 0; k < KINDS; ++k) {
-      const int at = (k * NW + wave) * 64 + lane, row = at / PER;
-      off[k] = row * static_cast<int>(stride_b) + min(Place::at(row, at % PER), row_b / 16 - 1) * 16;
+      const int n = (k * NW + wave) * 64 + lane, row = n / PER;
+      off[k] = row * static_cast<int>(stride_b) + min(Place::at(row, n % PER), row_b / 16 - 1) * 16;
     }
   }
-  // lds: of the wavefront's first round
-  __device__ __forceinline__ void tile(int t0, lds_char *lds) const {
-    const u32x4 rows = rows_from(base, stride_b, t0, len, row_b);
-    const int step_b = KINDS * STEP * static_cast<int>(stride_b);
+  // The next tile; lds: of the wavefront's first round
+  __device__ __forceinline__ void next(lds_char *lds) {
+    const u32x4 rows = {static_cast<uint32_t>(at), static_cast<uint32_t>(at >> 32) & 0xffffu,
+                        (left >> 31) != 0 ? 0x7fffffffu : static_cast<uint32_t>(left), 0x00020000u};
 #pragma unroll
     for (int i = 0; i < ROUNDS; ++i) copy_to_lds(rows, off[i % KINDS], i / KINDS * step_b, lds + i * NW * 1024);
+    at += tile_b;
+    left -= tile_b;
   }
 };
 template <int ROWB>
@@ -164,8 +163,8 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_k
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
   const RowSet rs = row_set<NW>(p, wave);
   const int pieces = p.D / 8;
-  const Stager<64, ROWB, NW, PlaceB<ROWB>> ks(static_cast<const char *>(p.k) + (rs.row0 * p.k_stride + rs.kv * p.D) * 2, p.k_stride * 2, rs.len, p.D * 2, wave, lane);
-  const Stager<64, ROWB, NW, PlaceB<ROWB>> vs(static_cast<const char *>(p.v) + (rs.row0 * p.v_stride + rs.kv * p.D) * 2, p.v_stride * 2, rs.len, p.D * 2, wave, lane);
+  Stager<64, ROWB, NW, PlaceB<ROWB>> ks(static_cast<const char *>(p.k) + (rs.row0 * p.k_stride + rs.kv * p.D) * 2, p.k_stride * 2, rs.len, p.D * 2, wave, lane);
+  Stager<64, ROWB, NW, PlaceB<ROWB>> vs(static_cast<const char *>(p.v) + (rs.row0 * p.v_stride + rs.kv * p.D) * 2, p.v_stride * 2, rs.len, p.D * 2, wave, lane);
   const int tiles = rs.last / 64 + 1, mine = rs.live ? min(rs.q0 + kPromptRows - 1, rs.len - 1) / 64 + 1 : 0;
   lds_char *const mine_at = lds + wave * 1024;  // where this wavefront's copies into the first buffer go
   // Queries and results cross LDS, so that memory sees whole rows: as the operands lie a load or store has 32 or 16 bytes of
@@ -174,11 +173,11 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_k
   auto rows_at = [&](int buffer) { return lds + ((wave >> 1) * 2 + buffer) * TILE + (wave & 1) * (TILE / 2); };
   const int64_t row = rs.row0 + rs.q0, head0 = static_cast<int64_t>(rs.live ? rs.head : 0) * p.D;
   if (rs.live) {
-    const Stager<32, ROWB, 1, PlaceB<ROWB>> qs(static_cast<const char *>(p.q) + (row * p.q_stride + head0) * 2, p.q_stride * 2, rs.len - rs.q0, p.D * 2, 0, lane);
-    qs.tile(0, rows_at(1));
+    Stager<32, ROWB, 1, PlaceB<ROWB>> qs(static_cast<const char *>(p.q) + (row * p.q_stride + head0) * 2, p.q_stride * 2, rs.len - rs.q0, p.D * 2, 0, lane);
+    qs.next(rows_at(1));
   }
-  ks.tile(0, mine_at);
-  vs.tile(0, mine_at + 2 * TILE);
+  ks.next(mine_at);
+  vs.next(mine_at + 2 * TILE);
   // Places of the operand pieces in a tile; the other keys of the tile lie at constant distances.
   int koff[KS], voff[DT][2];
 #pragma unroll
@@ -206,7 +205,8 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_k
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
-  float m = kMInit, l = 0.f;
+  float m = kMInit, l = 0.f, limit = -__builtin_huge_valf();  // limit: scores up to here need no other reference point
+  const float inv_scale = 1.0f / p.scale_log2;
   const int qpos = rs.q0 + col;
 
   for (int t = 0; t < tiles; ++t) {
@@ -214,8 +214,8 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_k
     lds_char *kt = lds + (t & 1) * TILE, *vt = lds + (2 + (t & 1)) * TILE;
     if (t + 1 < tiles) {
       lds_char *to = mine_at + (~t & 1) * TILE;
-      ks.tile((t + 1) * 64, to);
-      vs.tile((t + 1) * 64, to + 2 * TILE);
+      ks.next(to);
+      vs.next(to + 2 * TILE);
     }
     if (t >= mine) continue;
     f32x16 s[2];
@@ -239,10 +239,10 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_k
     float mx = s[0][0];
 #pragma unroll
     for (int r = 1; r < 32; ++r) mx = fmaxf(mx, s[r / 16][r % 16]);
-    mx = fmaxf(mx, other_half(mx)) * p.scale_log2;
-    if (__any(mx > m + kSlack)) {
-      const float mn = fmaxf(m, mx), f = fast_exp2(m - mn);
+    if (__any(mx > limit)) {
+      const float mn = fmaxf(m, fmaxf(mx, other_half(mx)) * p.scale_log2), f = fast_exp2(m - mn);
       m = mn;
+      limit = (m + kSlack) * inv_scale;
       l *= f;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
@@ -301,12 +301,12 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_f32_ke
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
   const RowSet rs = row_set<NW>(p, wave);
   const int pieces = p.D / 4;
-  const Stager<32, ROWB, NW, PlaceF> ks(static_cast<const char *>(p.k) + (rs.row0 * p.k_stride + rs.kv * p.D) * 4, p.k_stride * 4, rs.len, p.D * 4, wave, lane);
-  const Stager<32, ROWB, NW, PlaceF> vs(static_cast<const char *>(p.v) + (rs.row0 * p.v_stride + rs.kv * p.D) * 4, p.v_stride * 4, rs.len, p.D * 4, wave, lane);
+  Stager<32, ROWB, NW, PlaceF> ks(static_cast<const char *>(p.k) + (rs.row0 * p.k_stride + rs.kv * p.D) * 4, p.k_stride * 4, rs.len, p.D * 4, wave, lane);
+  Stager<32, ROWB, NW, PlaceF> vs(static_cast<const char *>(p.v) + (rs.row0 * p.v_stride + rs.kv * p.D) * 4, p.v_stride * 4, rs.len, p.D * 4, wave, lane);
   const int tiles = rs.last / 32 + 1, mine = rs.live ? min(rs.q0 + kPromptRows - 1, rs.len - 1) / 32 + 1 : 0;
   lds_char *const mine_at = lds + wave * 1024;  // where this wavefront's copies into the first buffer go
-  ks.tile(0, mine_at);
-  vs.tile(0, mine_at + 2 * TILE);
+  ks.next(mine_at);
+  vs.next(mine_at + 2 * TILE);
   f32x4 qf[KS];
   {
     const char *qrow = static_cast<const char *>(p.q) +
@@ -334,8 +334,8 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_f32_ke
     lds_char *kt = lds + (t & 1) * TILE, *vt = lds + (2 + (t & 1)) * TILE;
     if (t + 1 < tiles) {
       lds_char *to = mine_at + (~t & 1) * TILE;
-      ks.tile((t + 1) * 32, to);
-      vs.tile((t + 1) * 32, to + 2 * TILE);
+      ks.next(to);
+      vs.next(to + 2 * TILE);
     }
     if (t >= mine) continue;
     f32x16 s;
