@@ -35,11 +35,14 @@ extern "C" spex_status_t spex_prompt_attention(const spex_prompt_config_t *cfg, 
   if (strides[0] < q_row || strides[1] < kv_row || strides[2] < kv_row || strides[3] < q_row) return SPEX_ERR_INVALID_ARG;
   for (int64_t s : strides)
     if (s > INT32_MAX) return SPEX_ERR_UNSUPPORTED;
-  int64_t total = 0;
+  int64_t total = 0, row_sets = 0;
+  int32_t longest = 0;
   for (int32_t i = 0; i < n_prompts; ++i) {
     if (lens[i] < 0) return SPEX_ERR_INVALID_ARG;
     if (lens[i] > kMaxPromptTokens) return SPEX_ERR_UNSUPPORTED;
     total += lens[i];
+    longest = std::max(longest, lens[i]);
+    row_sets += (lens[i] + spex::kPromptRows - 1) / spex::kPromptRows;
   }
   if (total > INT32_MAX) return SPEX_ERR_UNSUPPORTED;
   if (total == 0) return SPEX_OK;
@@ -50,7 +53,7 @@ extern "C" spex_status_t spex_prompt_attention(const spex_prompt_config_t *cfg, 
   for (int64_t s : strides) wide = wide && s % per16 == 0;
   // offsets inside a tile of up to 64 tokens are 32 bits
   wide = wide && std::max({strides[0], strides[1], strides[2]}) * (16 / per16) < (int64_t(1) << 24);
-  const spex::PromptKernel kernel = spex::prompt_kernel(cfg->dtype == SPEX_F32, wide);
+  const spex::PromptKernel kernel = spex::prompt_kernel(cfg->dtype == SPEX_F32, wide, cfg->head_dim, row_sets * cfg->num_q_heads, longest);
   const int32_t G = cfg->num_q_heads / cfg->num_kv_heads;
 
   struct Prompt {

@@ -6,6 +6,9 @@
 //       wavefronts share the K and V tiles they stage in LDS, however many query heads a kv head has.
 //   spex_prompt_f32_kernel
 //       The same with the fp32 MFMA.
+//   spex_prompt_split_kernel
+//       The same for launches of few rows: a workgroup takes one set of 32 rows, its wavefronts every NW-th 32 keys each,
+//       and joins their states in the end.
 //   spex_prompt_generic_kernel
 //       Same contract without matrix cores, for rows that are not made of 16-byte pieces.
 //
@@ -17,6 +20,7 @@
 #include "prompt.hpp"
 
 #include <climits>
+#include <type_traits>
 
 namespace spex {
 namespace {
@@ -128,9 +132,10 @@ struct Stager {
   int64_t left;   // bytes from there to the end of the prompt's last row
   int64_t tile_b; // bytes from tile to tile
   int step_b, off[KINDS];
-  // base: first row
-  __device__ __forceinline__ Stager(const char *base, int64_t stride_b, int len, int row_b, int wave, int lane)
-      : at(reinterpret_cast<uint64_t>(base)), left((len - 1) * stride_b + row_b), tile_b(KEYS * stride_b), step_b(KINDS * STEP * static_cast<int>(stride_b)) {
+  // base: first row; tile number `first` comes first, then every `every`-th
+  __device__ __forceinline__ Stager(const char *base, int64_t stride_b, int len, int row_b, int wave, int lane, int first = 0, int every = 1)
+      : at(reinterpret_cast<uint64_t>(base) + first * (KEYS * stride_b)), left((len - 1 - first * KEYS) * stride_b + row_b),
+        tile_b(every * (KEYS * stride_b)), step_b(KINDS * STEP * static_cast<int>(stride_b)) {
 #pragma unroll
     for (int k = 0; k < KINDS; ++k) {
       const int n = (k * NW + wave) * 64 + lane, row = n / PER;
@@ -395,6 +400,171 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_f32_ke
   if (p.lse && h == 0) p.lse[row * (static_cast<int64_t>(p.Hkv) * p.G) + rs.head] = (m + __builtin_log2f(l)) * 0.6931471805599453f;
 }
 
+// ---- few rows ------------------------------------------------------------------------------------
+// A workgroup takes 32 rows of one query head; wavefront w units w, w + NW, .. of 32 keys, which it copies into LDS of its own and
+// waits for alone.  In the end the wavefronts' states go through LDS: with M the largest m of a row,
+// l = sum_w l_w 2^(m_w - M), out = sum_w O_w 2^(m_w - M) / l.
+// What bounds such launches is the way of the longest row set from launch to store; its keys are worked on NW at a time here.
+template <bool F32, int DP, int NW>
+__global__ __launch_bounds__(64 * NW, 2 * NW * 32 * (F32 ? DP * 4 : TileB<DP>::kRowB) <= 65536 ? 2 : 1) void spex_prompt_split_kernel(PromptArgs p) {
+  constexpr int ESZ = F32 ? 4 : 2, ROWB = F32 ? DP * 4 : TileB<DP>::kRowB, UNIT = 32 * ROWB, DT = DP / 32;
+  constexpr int KS = F32 ? DP / 8 : DP / 16;  // steps of 16 bytes a lane
+  typedef typename std::conditional<F32, PlaceF, PlaceB<ROWB>>::type Place;
+  constexpr int CP = UNIT / 1024;             // copies of a unit
+  constexpr int PER = DP / 4;                 // pieces of four dims of a row of results
+  static_assert(32 * DP * 4 <= 2 * UNIT, "a wavefront's results fit its own LDS");
+  __shared__ __attribute__((aligned(1024))) char lds_[2 * NW * UNIT];
+  __shared__ float ml[NW][2][32];
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
+  lds_char *const kt = (lds_char *)lds_ + wave * (2 * UNIT), *const vt = kt + UNIT;
+  const RowSet rs = row_set<1>(p, 0);
+  const int units = rs.q0 / 32 + 1, pieces = p.D * ESZ / 16;
+  const int64_t row = rs.row0 + rs.q0, head0 = static_cast<int64_t>(rs.head) * p.D, kv0 = static_cast<int64_t>(rs.kv) * p.D;
+  Stager<32, ROWB, 1, Place> ks(static_cast<const char *>(p.k) + (rs.row0 * p.k_stride + kv0) * ESZ, p.k_stride * ESZ, rs.len, p.D * ESZ, 0, lane, wave, NW);
+  Stager<32, ROWB, 1, Place> vs(static_cast<const char *>(p.v) + (rs.row0 * p.v_stride + kv0) * ESZ, p.v_stride * ESZ, rs.len, p.D * ESZ, 0, lane, wave, NW);
+  // Places of the operand pieces, as in the other kernels.
+  int koff[KS], voff[F32 ? 4 : 2 * DT];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) koff[s] = col * ROWB + Place::at(col, 2 * s + h) * 16;
+  if (F32) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) voff[i] = (4 * h + i) * ROWB + ((col >> 2) ^ (4 * h + i)) * 16 + (col & 3) * 4;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2 * DT; ++i) {
+      const int t = 8 * (i & 1) + 4 * h + ((lane & 15) >> 2), c = 4 * (i >> 1) + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      voff[i] = t * ROWB + Place::at(t, c) * 16 + (lane & 1) * 8;
+    }
+  }
+  f32x16 o[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
+  float m = kMInit, l = 0.f;
+  if (wave < units) {
+    // the queries by way of the room for values
+    Stager<32, ROWB, 1, Place> qs(static_cast<const char *>(p.q) + (row * p.q_stride + head0) * ESZ, p.q_stride * ESZ, rs.len - rs.q0, p.D * ESZ, 0, lane);
+    qs.next(vt);
+    ks.next(kt);
+    u32x4 qf[KS];
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CP) : "memory");
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      qf[s] = *(const lds_u32x4 *)(vt + koff[s]);
+      if (2 * s + h >= pieces) qf[s] = u32x4{0, 0, 0, 0};
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    vs.next(vt);
+    for (int u = wave; u < units; u += NW) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CP) : "memory");  // the keys have landed, the values may be under way
+      f32x16 s;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        const u32x4 kf = *(const lds_u32x4 *)(kt + koff[i]);
+        if (F32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(f32x4, kf)[e], __builtin_bit_cast(f32x4, qf[i])[e], s, 0, 0, 0);
+        } else {
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[i]), s, 0, 0, 0);
+        }
+      }
+      // No branch between the products and the first use of their results: the compiler has left out the wait states on the
+      // shorter of two ways here.
+      const bool more = u + NW < units;
+      const int seen = u == units - 1 ? col - 4 * h : 32;  // keys behind a row's own token lie in the last unit
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (8 * (r / 4) + r % 4 > seen) s[r] = -__builtin_huge_valf();
+      float mx = s[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+      const float mn = fmaxf(m, fmaxf(mx, other_half(mx)) * p.scale_log2);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the keys have been read
+      if (more) ks.next(kt);
+      if (__any(mn > m)) {
+        const float f = fast_exp2(m - mn);
+        m = mn;
+        l *= f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[dt][r] *= f;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] = fast_exp2(__builtin_fmaf(s[r], p.scale_log2, -m));
+        l += s[r];
+      }
+      if (more)
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CP) : "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if (F32) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(*(const lds_float *)(vt + voff[r % 4] + r / 4 * 8 * ROWB + (dt ^ (r / 4 & 1)) * 128), s[r], o[dt], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int sl = 0; sl < 2; ++sl) {
+          const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(s[8 * sl], s[8 * sl + 1]), pack_bf16(s[8 * sl + 2], s[8 * sl + 3]),
+                                                             pack_bf16(s[8 * sl + 4], s[8 * sl + 5]), pack_bf16(s[8 * sl + 6], s[8 * sl + 7])});
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            const u32x2 a0 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + voff[(2 * dt) % (F32 ? 4 : 2 * DT)] + sl * 16 * ROWB)));
+            const u32x2 a1 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + voff[(2 * dt + 1) % (F32 ? 4 : 2 * DT)] + sl * 16 * ROWB)));
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u32x4{a0[0], a0[1], a1[0], a1[1]}), pf, o[dt], 0, 0, 0);
+          }
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the values have been read
+      if (more) vs.next(vt);
+    }
+    l += other_half(l);
+  }
+  // Results into this wavefront's LDS: piece c of row r at place c ^ (r & 7), so that rows do not fall on the same banks.
+  if (h == 0) {
+    ml[wave][0][col] = m;
+    ml[wave][1][col] = l;
+  }
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *(__attribute__((address_space(3))) f32x4 *)(kt + col * (DP * 4) + ((8 * dt + 2 * j + h) ^ (col & 7)) * 16) =
+          f32x4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * PER; i += 64 * NW) {
+    const int r = i / PER, c = i % PER, d = 4 * c;
+    float top = kMInit;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, ml[w][0][r]);
+    float sum = 0.f;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = fast_exp2(ml[w][0][r] - top);
+      sum += ml[w][1][r] * f;
+      const f32x4 y = *(const __attribute__((address_space(3))) f32x4 *)((const lds_char *)lds_ + w * (2 * UNIT) + r * (DP * 4) + (c ^ (r & 7)) * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += y[e] * f;
+    }
+    if (rs.q0 + r >= rs.len || d >= p.D) continue;
+    const float inv = 1.0f / sum;
+    char *out = static_cast<char *>(p.out) + ((row + r) * p.out_stride + head0 + d) * ESZ;
+    if (F32)
+      *reinterpret_cast<f32x4 *>(out) = f32x4{x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
+    else
+      *reinterpret_cast<u32x2 *>(out) = u32x2{pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv)};
+    if (p.lse && c == 0) p.lse[(row + r) * (static_cast<int64_t>(p.Hkv) * p.G) + rs.head] = (top + __builtin_log2f(sum)) * 0.6931471805599453f;
+  }
+}
+
 // ---- any rows ------------------------------------------------------------------------------------
 template <bool F32>
 __device__ __forceinline__ float load(const void *p, int64_t i) {
@@ -454,11 +624,32 @@ constexpr int kWaves = 4;
 
 }  // namespace
 
-PromptKernel prompt_kernel(bool f32, bool wide) { return {f32, wide, wide ? kWaves : 1}; }
+PromptKernel prompt_kernel(bool f32, bool wide, int32_t D, int64_t row_sets, int32_t longest) {
+  PromptKernel k{f32, wide, false, wide ? kWaves : 1};
+  if (!wide || (f32 && D > 128)) return k;
+  // Keys are split over the wavefronts of a workgroup where all row sets run at once that way (by LDS), or where the way of the
+  // longest, in units of 32 keys, is shorter by enough: a workgroup has some other work as long as `fixed` units, and keys
+  // and values are then not shared by four row sets.  us, whole / split; heads 32/8/128, one prompt of 1: 4.9 / 4.1, 256: 8.6 / 6.8,
+  // 512 (512 row sets): 13.0 / 9.9, 768: 17.7 / 18.0, 1024: 22.2 / 23.1, 2048: 45.9 / 61.3; 8/2/128, 2048: 37.4 / 21.9, 4096 (1024):
+  // 70.7 / 57.7, 8192: 164 / 194; 8 of 128, 32/8/128 (1024): 7.3 / 12.1; 16/2/64, 2048 (1024): 32.7 / 20.3; 16/4/256, 512 (256): 27.2 / 16.9,
+  // 1500 (752): 69 / 65; fp32 8/2/64, 256: 23.1 / 9.1, 32/8/128, 256 (256): 38.7 / 15.8, 512: 71.7 / 34.3, 32 of 64 (2048): 29 / 67.
+  const int32_t row_b = f32 ? (D <= 64 ? 256 : 512) : (D <= 64 ? 128 : (D <= 128 ? 256 : 512));
+  const int64_t at_once = 256 * (512 / row_b), rounds = (row_sets + at_once - 1) / at_once;
+  const double units = (longest + 31) / 32, fixed = f32 ? 0.5 : 3.0, shared = f32 ? 1.3 : 1.5;
+  k.split = rounds <= 1 || shared * static_cast<double>(rounds) * (units / kWaves + fixed) < units;
+  if (k.split) k.sets = 1;
+  return k;
+}
 
 int64_t prompt_items(const PromptKernel &k, int32_t heads_per_kv, int32_t len) {
   const int64_t pairs = (static_cast<int64_t>(len) + kPromptRows - 1) / kPromptRows * heads_per_kv;
-  return (pairs + k.waves - 1) / k.waves;
+  return (pairs + k.sets - 1) / k.sets;
+}
+
+template <int DP>
+static void (*bf16_kernel(const PromptKernel &k))(PromptArgs) {
+  if (k.split) return spex_prompt_split_kernel<false, DP, kWaves>;
+  return spex_prompt_bf16_kernel<DP, kWaves>;
 }
 
 hipError_t launch_prompt(const PromptKernel &k, const PromptArgs &a, int64_t items, hipStream_t stream) {
@@ -466,14 +657,13 @@ hipError_t launch_prompt(const PromptKernel &k, const PromptArgs &a, int64_t ite
   void (*kernel)(PromptArgs) = nullptr;
   if (!k.wide)
     kernel = k.f32 ? spex_prompt_generic_kernel<true> : spex_prompt_generic_kernel<false>;
+  else if (k.f32 && k.split)
+    kernel = a.D <= 64 ? spex_prompt_split_kernel<true, 64, kWaves> : spex_prompt_split_kernel<true, 128, kWaves>;
   else if (k.f32)
     kernel = a.D <= 64 ? spex_prompt_f32_kernel<64, kWaves> : (a.D <= 128 ? spex_prompt_f32_kernel<128, kWaves> : spex_prompt_f32_kernel<256, kWaves>);
   else
-    kernel = a.D <= 64 ? spex_prompt_bf16_kernel<64, kWaves>
-                       : (a.D <= 96 ? spex_prompt_bf16_kernel<96, kWaves>
-                                    : (a.D <= 128 ? spex_prompt_bf16_kernel<128, kWaves>
-                                                  : (a.D <= 192 ? spex_prompt_bf16_kernel<192, kWaves> : spex_prompt_bf16_kernel<256, kWaves>)));
-  hipLaunchKernelGGL(kernel, grid, dim3(static_cast<unsigned>(64 * k.waves)), 0, stream, a);
+    kernel = a.D <= 64 ? bf16_kernel<64>(k) : (a.D <= 96 ? bf16_kernel<96>(k) : (a.D <= 128 ? bf16_kernel<128>(k) : (a.D <= 192 ? bf16_kernel<192>(k) : bf16_kernel<256>(k))));
+  hipLaunchKernelGGL(kernel, grid, dim3(k.wide ? 64 * kWaves : 64), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -26,12 +26,14 @@ struct PromptArgs {
   int32_t len[kMaxPromptsPerLaunch];        // tokens
 };
 
-// A kernel for the launches of one call.
+// The kernel for the launches of one call.
 struct PromptKernel {
   bool f32, wide;  // type; rows of 16-byte pieces (else element by element)
-  int32_t waves;   // row sets of kPromptRows rows a workgroup takes (wide)
+  bool split;      // a workgroup splits the keys of its rows
+  int32_t sets;    // row sets of kPromptRows rows a work item has
 };
-PromptKernel prompt_kernel(bool f32, bool wide);
+// row_sets: of all prompts and query heads; longest: tokens of the longest prompt
+PromptKernel prompt_kernel(bool f32, bool wide, int32_t head_dim, int64_t row_sets, int32_t longest);
 // Work items of one kv head that a prompt of `len` tokens makes.
 int64_t prompt_items(const PromptKernel &k, int32_t heads_per_kv, int32_t len);
 // a.first / start / len filled for a.n prompts, `items` of them together for one kv head.
