@@ -887,14 +887,20 @@ static spex_status_t append_rotated_impl(spex_tree_t *t, const spex_node_t *node
 
   const spex_status_t us = upload_rotation(t);
   if (us != SPEX_OK) return us;
-  // Ring: the records, the positions where they are given, and room for length patches of the cached plan as in
-  // append_tokens_impl.
+  // The lists go into the kernel arguments if they fit, with some room for length patches of the cached plan, and else into
+  // the ring, with room for 32 patches a node as in append_tokens_impl.  A call through the ring takes 5 us more on the host (an event
+  // behind the kernel) and 2 us more on the GPU (the kernel reads its records over the bus).
   const size_t rec_ints = static_cast<size_t>(visits) * spex::kVisitInts;
-  const size_t pos_ints = positions ? static_cast<size_t>(tokens) : 0;
-  const size_t patch_room = static_cast<size_t>(n_nodes) * 32;
-  int32_t *h = nullptr;
-  const spex_status_t rs = ring_reserve(t, (rec_ints + pos_ints + 2 * patch_room) * sizeof(int32_t), &h);
-  if (rs != SPEX_OK) return rs;
+  const size_t pos_ints = positions ? static_cast<size_t>(tokens) : 0, patch_at = rec_ints + pos_ints;
+  const bool plan_follows = t->plan.valid && t->plan_on_device;
+  const bool ring = patch_at + (plan_follows ? 8 * static_cast<size_t>(n_nodes) : 0) > spex::kInlineInts;
+  const size_t patch_room = ring ? static_cast<size_t>(n_nodes) * 32 : (spex::kInlineInts - patch_at) / 2;
+  spex::RotateLists lists;
+  int32_t *h = lists.ints;
+  if (ring) {
+    const spex_status_t rs = ring_reserve(t, (patch_at + 2 * patch_room) * sizeof(int32_t), &h);
+    if (rs != SPEX_OK) return rs;
+  }
   int32_t *rec = h, most = 0;
   int32_t token = 0, started = 0;
   for (int32_t i = 0; i < n_nodes; ++i) {
@@ -912,7 +918,6 @@ static spex_status_t append_rotated_impl(spex_tree_t *t, const spex_node_t *node
       rec[2] = token;
       rec[3] = positions ? 0 : before[i] + at - old_tokens;
       rec[4] = is_new ? started++ : 0;
-      rec[5] = rec[6] = rec[7] = 0;
       rec += spex::kVisitInts;
       most = std::max(most, n);
       token += n;
@@ -920,8 +925,7 @@ static spex_status_t append_rotated_impl(spex_tree_t *t, const spex_node_t *node
     }
   }
   if (positions) std::memcpy(h + rec_ints, positions, pos_ints * sizeof(int32_t));
-  int32_t *hp = h + rec_ints + pos_ints;
-  const size_t n_patch = follow_append(t, hp, patch_room);
+  const size_t n_patch = follow_append(t, h + patch_at, patch_room);
 
   spex::RotateArgs a{};
   a.k_pool = t->cfg.k_pool;
@@ -941,18 +945,18 @@ static spex_status_t append_rotated_impl(spex_tree_t *t, const spex_node_t *node
   a.k_scale_src = data->k_scales;
   a.v_scale_src = data->v_scales;
   a.freq = static_cast<const spex::Turns *>(t->d_freq);
-  a.recs = h;
-  a.positions = positions ? h + rec_ints : nullptr;
+  a.lists = ring ? h : nullptr;
+  a.has_positions = positions != nullptr;
   a.n_recs = static_cast<int32_t>(visits);
   a.rotary_dim = t->rotary_dim;
   a.interleaved = t->interleaved;
   a.most_tokens = most;
   a.plan = static_cast<int32_t *>(t->d_plan);
-  a.patches = hp;
+  a.patches = static_cast<int32_t>(patch_at);
   a.n_patches = static_cast<int32_t>(n_patch);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  HIP_TRY(spex::launch_append_rotated(t->shape, a, stream));
-  return ring_commit(t, (rec_ints + pos_ints + 2 * n_patch) * sizeof(int32_t), stream);
+  HIP_TRY(spex::launch_append_rotated(t->shape, a, lists, stream));
+  return ring ? ring_commit(t, (patch_at + 2 * n_patch) * sizeof(int32_t), stream) : SPEX_OK;
 }
 
 spex_status_t spex_tree_append_rotated(spex_tree_t *t, const spex_node_t *nodes, const int32_t *counts, int32_t n_nodes,

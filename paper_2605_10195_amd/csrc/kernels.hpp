@@ -115,10 +115,15 @@ struct AppendTokensArgs {
   int32_t n_patches;
 };
 
-// Tokens of many nodes, rotated on the way (spex_tree_append_rotated).  A record per page that the call writes to:
+// Tokens of many nodes, rotated on the way (spex_tree_append_rotated).  The lists: a record per page that the call writes to,
 // {page id, first slot | slot behind the last << 8 | (page is new) << 16, index of the first token in the call, its
-// position, index of the page among those the call starts, 0, 0, 0}.
-constexpr int kVisitInts = 8;
+// position, index of the page among those the call starts}; then, where they are given, the positions of the tokens;
+// then {index, value} patches of the cached plan.
+constexpr int kVisitInts = 5;
+constexpr int kInlineInts = 704;  // with the rest 3 KB of kernel arguments
+struct RotateLists {
+  int32_t ints[kInlineInts];
+};
 struct Turns {
   double hi, lo;  // a pair turns hi + lo whole turns a position: inv_freq / (2 pi)
 };
@@ -130,14 +135,12 @@ struct RotateArgs {
   int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;  // elements between tokens
   const float *k_scale_src, *v_scale_src;  // [pages the call starts][Hkv] or null (fp8)
   const Turns *freq;                       // [rotary_dim / 2]
-  const int32_t *recs;                     // pinned host memory
-  const int32_t *positions;                // pinned host memory, one per token, or null
+  const int32_t *lists;                    // pinned host memory, or null: RotateLists
   int32_t n_recs, rotary_dim, most_tokens; // most_tokens: of a record
-  bool interleaved;
+  bool interleaved, has_positions;
   int32_t parts;                           // set by launch_append_rotated
-  int32_t *plan;                           // length patches of the cached plan, as in AppendTokensArgs
-  const int32_t *patches;
-  int32_t n_patches;
+  int32_t *plan;                           // the device copy of the cached plan
+  int32_t patches, n_patches;              // where the patches begin in the lists, and how many there are
 };
 
 struct GatherArgs {
@@ -170,7 +173,7 @@ hipError_t launch_scatter(const Shape &sh, const ScatterArgs &a, hipStream_t str
 hipError_t launch_scatter_quantise(const Shape &sh, const ScatterArgs &a, hipStream_t stream);
 hipError_t launch_gather(const Shape &sh, const GatherArgs &a, hipStream_t stream);
 hipError_t launch_append_tokens(const Shape &sh, const AppendTokensArgs &a, hipStream_t stream);
-hipError_t launch_append_rotated(const Shape &sh, const RotateArgs &a, hipStream_t stream);
+hipError_t launch_append_rotated(const Shape &sh, const RotateArgs &a, const RotateLists &in, hipStream_t stream);
 // blob[pairs[2i]] = pairs[2i+1] for i < n (all DEVICE): patches the device copy of a plan.
 hipError_t launch_patch(int32_t *blob, const int32_t *pairs, int32_t n, hipStream_t stream);
 // Tree-walk kernel; ntw in {1, 2, 4} = 16-row tiles per wavefront and waves in {2, 4, 8} = wavefronts

@@ -47,31 +47,56 @@ __device__ __forceinline__ f32x2 turned(float x1, float x2, f32x2 cs) {
   return f32x2{x1 * cs[0] - x2 * cs[1], x2 * cs[0] + x1 * cs[1]};
 }
 
-// A record of a.recs: tokens tok0 .. tok0 + hi - lo - 1 of the call go to slots [lo, hi) of the page.
+// A record: tokens tok0 .. tok0 + hi - lo - 1 of the call go to slots [lo, hi) of the page.
 struct PageVisit {
   int page, lo, hi, fill, tok0, pos0, new_index;
   bool is_new;  // this call starts the page: slots up to fill = P are written, zeros behind the tokens
 };
-__device__ __forceinline__ PageVisit page_visit(const RotateArgs &a, int P) {
-  const int32_t *r = a.recs + static_cast<int64_t>(blockIdx.x) * kVisitInts;
-  const u32x4 x = *reinterpret_cast<const u32x4 *>(r);
+// Lists of up to kInlineInts travel in the kernel arguments; longer ones are read where the host wrote them, in pinned memory.
+__device__ __forceinline__ PageVisit page_visit(const RotateArgs &a, const RotateLists &in, int P) {
+  int r[kVisitInts];
+  const int at = static_cast<int>(blockIdx.x) * kVisitInts;
+  if (a.lists) {  // one access a wavefront: the lanes read an int each
+    const int x = a.lists[at + min(static_cast<int>(threadIdx.x) & 63, kVisitInts - 1)];
+#pragma unroll
+    for (int i = 0; i < kVisitInts; ++i) r[i] = __builtin_amdgcn_readlane(x, i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVisitInts; ++i) r[i] = uniform(in.ints[at + i]);
+  }
   PageVisit v;
-  v.page = uniform(static_cast<int>(x[0]));
-  const int flags = uniform(static_cast<int>(x[1]));
-  v.tok0 = uniform(static_cast<int>(x[2]));
-  v.pos0 = uniform(static_cast<int>(x[3]));
-  v.new_index = uniform(r[4]);
-  v.lo = flags & 0xff;
-  v.hi = (flags >> 8) & 0xff;
-  v.is_new = (flags >> 16) != 0;
+  v.page = r[0];
+  v.tok0 = r[2];
+  v.pos0 = r[3];
+  v.new_index = r[4];
+  v.lo = r[1] & 0xff;
+  v.hi = (r[1] >> 8) & 0xff;
+  v.is_new = (r[1] >> 16) != 0;
   v.fill = v.is_new ? P : v.hi;
   return v;
 }
+// Position of token t of a record.
+__device__ __forceinline__ int position(const RotateArgs &a, const RotateLists &in, const PageVisit &v, int t) {
+  if (!a.has_positions) return v.pos0 + t;
+  const int at = a.n_recs * kVisitInts + v.tok0 + t;
+  return a.lists ? a.lists[at] : in.ints[at];
+}
 
-__device__ __forceinline__ void apply_patches(const RotateArgs &a) {
+// Where token t begins; strides are below 2^31.
+__device__ __forceinline__ int64_t token_at(int t, int64_t stride) {
+  return static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(t)) * static_cast<uint32_t>(stride));
+}
+__device__ __forceinline__ uint16_t half_of(uint32_t w, int i) { return static_cast<uint16_t>(w >> (16 * i)); }
+
+__device__ __forceinline__ void apply_patches(const RotateArgs &a, const RotateLists &in) {
   if (blockIdx.y != 0) return;
-  for (int i = static_cast<int>(blockIdx.x * 256 + threadIdx.x); i < a.n_patches; i += static_cast<int>(gridDim.x) * 256)
-    a.plan[a.patches[2 * i]] = a.patches[2 * i + 1];
+  for (int i = static_cast<int>(blockIdx.x * 256 + threadIdx.x); i < a.n_patches; i += static_cast<int>(gridDim.x) * 256) {
+    const int at = a.patches + 2 * i;
+    if (a.lists)
+      a.plan[a.lists[at]] = a.lists[at + 1];
+    else
+      a.plan[in.ints[at]] = in.ints[at + 1];
+  }
 }
 
 // Eight dims of a row.
@@ -138,6 +163,10 @@ struct Unit {
     e[0] = load_eight<F32>(base, row + d[0]);
     e[1] = two ? load_eight<F32>(base, row + d[1]) : e[0];
   }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[0].x[j] = e[1].x[j] = 0.f;
+  }
   // cs: cosines and sines of the token's pairs.
   __device__ __forceinline__ void turn(const f32x2 *cs) {
     if (INTER) {
@@ -167,11 +196,19 @@ struct Unit {
   __device__ __forceinline__ float top() const { return fmaxf(largest(e[0]), two ? largest(e[1]) : 0.f); }
 };
 
+// e4m3 codes of a, b, c, d, as encode_e4m3 gives them: values clamped to +-448, then converted to nearest even two at a time.
+// The clamp would take a NaN to a number, so four values with one among them are encoded one by one.
+__device__ __forceinline__ uint32_t encode_four(float a, float b, float c, float d) {
+  const uint32_t top = max(max(__builtin_bit_cast(uint32_t, a) & 0x7fffffffu, __builtin_bit_cast(uint32_t, b) & 0x7fffffffu),
+                           max(__builtin_bit_cast(uint32_t, c) & 0x7fffffffu, __builtin_bit_cast(uint32_t, d) & 0x7fffffffu));
+  if (top > 0x7f800000u) return encode_e4m3(a) | encode_e4m3(b) << 8 | encode_e4m3(c) << 16 | encode_e4m3(d) << 24;
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_fmed3f(a, -448.f, 448.f), __builtin_amdgcn_fmed3f(b, -448.f, 448.f), 0, false);
+  r = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_fmed3f(c, -448.f, 448.f), __builtin_amdgcn_fmed3f(d, -448.f, 448.f), r, true);
+  return static_cast<uint32_t>(r);
+}
 __device__ __forceinline__ u32x2 encode_eight(const Eight &e, float inv) {
-  u32x2 r = {0, 0};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) r[i >> 2] |= encode_e4m3(e.x[i] * inv) << (8 * (i & 3));
-  return r;
+  return u32x2{encode_four(e.x[0] * inv, e.x[1] * inv, e.x[2] * inv, e.x[3] * inv),
+               encode_four(e.x[4] * inv, e.x[5] * inv, e.x[6] * inv, e.x[7] * inv)};
 }
 // Eight dims of a token into a tile.
 template <int KV>
@@ -182,22 +219,198 @@ __device__ __forceinline__ void put_eight(char *tile, int at, const Eight &e, fl
     store_eight<KV == kF32>(tile, at, e);
 }
 
-// DT: head_dim of tiled pools, else 0.
-template <int KV, int DT, bool INTER>
-__global__ __launch_bounds__(256) void spex_append_rotated_kernel(RotateArgs a, Shape sh) {
-  constexpr bool F32 = KV == kF32, FP8 = KV == kFP8, TILED = DT > 0;
-  constexpr int LAYOUT = TILED ? kMfmaTiled : kRowMajor, ESZ = F32 ? 4 : (FP8 ? 1 : 2);
+// Tiled pools.  A workgroup's work is cut into jobs of a wavefront, dealt to its four wavefronts in turn: a kv head's values (D 64:
+// two heads'; of a few tokens, rows), a page's worth of units of keys, two units of queries a lane.  Loads of a job are all under way before the first is used.
+template <int KV, int D, bool INTER>
+__global__ __launch_bounds__(256) void spex_append_rotated_kernel(RotateArgs a, Shape sh, RotateLists in) {
+  constexpr bool FP8 = KV == kFP8;
+  constexpr int P = 16, U = D / 16, N = P * U / 64, ESZ = FP8 ? 1 : 2;
   extern __shared__ __attribute__((aligned(16))) char lds_[];
   f32x2 *cs = reinterpret_cast<f32x2 *>(lds_);  // [token][R / 2]
-  const int D = TILED ? DT : sh.D, P = TILED ? 16 : sh.P, U = (D + 15) / 16, R = a.rotary_dim;
+  const int R = a.rotary_dim, half = R / 2, tid = threadIdx.x, lane = tid & 63;
+  const PageVisit pv = page_visit(a, in, P);
+  apply_patches(a, in);
+  const int n = pv.hi - pv.lo;  // tokens
+  for (int i = tid; i < n * half; i += 256) {
+    const int t = i / half, pair = i - t * half;
+    cs[i] = cos_sin_turns(position(a, in, pv, t), a.freq[pair]);
+  }
+  __syncthreads();
+  const int g0 = static_cast<int>(blockIdx.y) * sh.Hkv / a.parts, ng = (static_cast<int>(blockIdx.y) + 1) * sh.Hkv / a.parts - g0;
+  const int nq = ng * sh.G, slots = pv.fill - pv.lo, n_q = a.q ? n * nq * U : 0, n_k = slots * ng * U;
+  const int64_t tile0 = static_cast<int64_t>(pv.page) * sh.page_tiles + g0;
+  constexpr int64_t kTileBytes = static_cast<int64_t>(P) * D * ESZ;
+  constexpr int kHeadLanes = D / 2;  // values
+  // Values of a few tokens behind others have no eight slots that can be written at once: a lane takes eight dims of a token.
+  const bool few = !pv.is_new && n < 8;
+  const int n_v = few ? n * ng * (D / 8) : ng * kHeadLanes, v_jobs = (n_v + 63) / 64, k_jobs = (n_k + 64 * N - 1) / (64 * N), q_jobs = (n_q + 127) / 128;
+  for (int j = uniform(tid >> 6); j < v_jobs + k_jobs + q_jobs; j += 4) {
+    if (j < v_jobs && few) {
+      const int i = j * 64 + lane, r = i / (D / 8), t = r / ng, gi = r - t * ng, d = i % (D / 8) * 8;
+      if (i >= n_v) continue;
+      const Eight e = load_eight<false>(a.v, token_at(pv.tok0 + t, a.v_stride) + (g0 + gi) * D + d);
+      const float inv = FP8 ? inverse_scale(a.v_scale[pv.page * sh.Hkv + g0 + gi]) : 1.f;
+      char *tile = static_cast<char *>(a.v_pool) + (tile0 + gi) * kTileBytes;
+      const u32x2 c = encode_eight(e, inv);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int at = v_offset<KV, kMfmaTiled>(pv.lo + t, d + k, D);
+        if (FP8)
+          tile[at] = static_cast<char>(c[k >> 2] >> (8 * (k & 3)));
+        else
+          reinterpret_cast<uint16_t *>(tile)[at] = static_cast<uint16_t>(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(e.x[k], 0.f)));
+      }
+    } else if (j < v_jobs) {
+      // Values lie token-minor: a lane takes two dims of all tokens.
+      const int gi = (j * 64 + lane) / kHeadLanes, d = lane % kHeadLanes * 2;
+      if (gi >= ng) continue;
+      const char *src = static_cast<const char *>(a.v) + 2 * (token_at(pv.tok0, a.v_stride) + (g0 + gi) * D + d);
+      uint32_t w[P];
+#pragma unroll
+      for (int s = 0; s < P; ++s) {
+        w[s] = 0;
+        if (s >= pv.lo && s < pv.hi) w[s] = *reinterpret_cast<const uint32_t *>(src + 2 * token_at(s - pv.lo, a.v_stride));
+      }
+      float inv = 1.f;
+      if (FP8) {
+        const int at = pv.page * sh.Hkv + g0 + gi;
+        float s;
+        if (!pv.is_new) {
+          s = a.v_scale[at];
+        } else {
+          if (a.v_scale_src) {
+            s = a.v_scale_src[static_cast<int64_t>(pv.new_index) * sh.Hkv + g0 + gi];
+          } else {
+            float top = 0.f;
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+              top = fmaxf(top, fmaxf(__builtin_fabsf(bf16_bits_to_float(half_of(w[i], 0))), __builtin_fabsf(bf16_bits_to_float(half_of(w[i], 1)))));
+#pragma unroll
+            for (int o = kHeadLanes / 2; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+            s = page_scale(top);
+          }
+          if (d == 0) a.v_scale[at] = s;
+        }
+        inv = inverse_scale(s);
+      }
+      char *tile = static_cast<char *>(a.v_pool) + (tile0 + gi) * kTileBytes;
+#pragma unroll
+      for (int t0 = 0; t0 < P; t0 += 8) {
+        if (t0 + 8 <= pv.lo || t0 >= pv.fill) continue;
+        const bool whole = t0 >= pv.lo && t0 + 8 <= pv.fill;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          char *dst = tile + ESZ * v_offset<KV, kMfmaTiled>(t0, d + k, D);
+          float x[8];
+#pragma unroll
+          for (int s = 0; s < 8; ++s) x[s] = bf16_bits_to_float(half_of(w[t0 + s], k));
+          if (FP8) {
+            const u32x2 c = {encode_four(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv), encode_four(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv)};
+            if (whole) {
+              *reinterpret_cast<u32x2 *>(dst) = c;
+            } else {
+#pragma unroll
+              for (int s = 0; s < 8; ++s)
+                if (t0 + s >= pv.lo && t0 + s < pv.fill) dst[s] = static_cast<char>(c[s >> 2] >> (8 * (s & 3)));
+            }
+          } else {
+            u32x4 h;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) h[s] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x[2 * s], x[2 * s + 1]));
+            if (whole) {
+              *reinterpret_cast<u32x4 *>(dst) = h;
+            } else {
+#pragma unroll
+              for (int s = 0; s < 8; ++s)
+                if (t0 + s >= pv.lo && t0 + s < pv.fill) *reinterpret_cast<uint16_t *>(dst + 2 * s) = static_cast<uint16_t>(h[s >> 1] >> (16 * (s & 1)));
+            }
+          }
+        }
+      }
+    } else if (j < v_jobs + k_jobs) {
+      // Keys.  Of a page the call starts a job has one head; four lanes beside each other have four tokens, which lie beside each
+      // other in the tile.
+      Unit<false, INTER> un[N];
+      int t[N], gi[N];
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const int i = ((j - v_jobs) * N + k) * 64 + lane;
+        int u;
+        if (pv.is_new) {
+          gi[k] = j - v_jobs;
+          t[k] = (k * 64 + lane) / (4 * U) * 4 + (lane & 3);
+          u = lane / 4 % U;
+        } else {
+          const int r = i / U;
+          u = i - r * U;
+          gi[k] = r / slots;
+          t[k] = r - gi[k] * slots;
+        }
+        un[k].place(u, D, R);
+        un[k].clear();
+        if (i >= n_k) gi[k] = -1;
+        if (gi[k] >= 0 && t[k] < n) un[k].load(a.k, token_at(pv.tok0 + t[k], a.k_stride) + (g0 + gi[k]) * D);
+      }
+      float top = 0.f;
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        if (gi[k] < 0 || t[k] >= n) continue;
+        un[k].turn(cs + t[k] * half);
+        if (a.k_out) un[k].store(a.k_out, token_at(pv.tok0 + t[k], a.k_out_stride) + (g0 + gi[k]) * D);
+        if (FP8) top = fmaxf(top, un[k].top());
+      }
+      float started = 1.f;
+      if (FP8 && pv.is_new) {
+        const int g = g0 + j - v_jobs;
+        started = a.k_scale_src ? a.k_scale_src[static_cast<int64_t>(pv.new_index) * sh.Hkv + g] : page_scale(wave_max(top));
+        if (lane == 0) a.k_scale[pv.page * sh.Hkv + g] = started;
+        started = inverse_scale(started);
+      }
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        if (gi[k] < 0) continue;
+        float inv = started;
+        if (FP8 && !pv.is_new) inv = inverse_scale(a.k_scale[pv.page * sh.Hkv + g0 + gi[k]]);
+        char *tile = static_cast<char *>(a.k_pool) + (tile0 + gi[k]) * kTileBytes;
+        put_eight<KV>(tile, k_offset<KV, kMfmaTiled>(pv.lo + t[k], un[k].d[0], D), un[k].e[0], inv);
+        put_eight<KV>(tile, k_offset<KV, kMfmaTiled>(pv.lo + t[k], un[k].d[1], D), un[k].e[1], inv);
+      }
+    } else {
+      Unit<false, INTER> un[2];
+      int t[2], at[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int i = (j - v_jobs - k_jobs) * 128 + k * 64 + lane, r = i / U;
+        t[k] = i < n_q ? r / nq : -1;
+        at[k] = (g0 * sh.G + r - t[k] * nq) * D;
+        un[k].place(i - r * U, D, R);
+        if (t[k] >= 0) un[k].load(a.q, token_at(pv.tok0 + t[k], a.q_stride) + at[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (t[k] < 0) continue;
+        un[k].turn(cs + t[k] * half);
+        un[k].store(a.q_out, token_at(pv.tok0 + t[k], a.q_out_stride) + at[k]);
+      }
+    }
+  }
+}
+
+// Row-major pools.
+template <int KV, bool INTER>
+__global__ __launch_bounds__(256) void spex_append_rotated_rows_kernel(RotateArgs a, Shape sh, RotateLists in) {
+  constexpr bool F32 = KV == kF32, FP8 = KV == kFP8;
+  constexpr int ESZ = F32 ? 4 : (FP8 ? 1 : 2);
+  extern __shared__ __attribute__((aligned(16))) char lds_[];
+  f32x2 *cs = reinterpret_cast<f32x2 *>(lds_);  // [token][R / 2]
+  const int D = sh.D, P = sh.P, U = (D + 15) / 16, R = a.rotary_dim;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const PageVisit pv = page_visit(a, P);
-  apply_patches(a);
+  const PageVisit pv = page_visit(a, in, P);
+  apply_patches(a, in);
   const int n = pv.hi - pv.lo;  // tokens
   for (int i = tid; i < n * (R / 2); i += 256) {
     const int t = i / (R / 2), pair = i - t * (R / 2);
-    const int pos = a.positions ? a.positions[pv.tok0 + t] : pv.pos0 + t;
-    cs[i] = cos_sin_turns(pos, a.freq[pair]);
+    cs[i] = cos_sin_turns(position(a, in, pv, t), a.freq[pair]);
   }
   __syncthreads();
   const int g0 = static_cast<int>(blockIdx.y) * sh.Hkv / a.parts, g1 = (static_cast<int>(blockIdx.y) + 1) * sh.Hkv / a.parts, ng = g1 - g0;
@@ -207,14 +420,14 @@ __global__ __launch_bounds__(256) void spex_append_rotated_kernel(RotateArgs a, 
     for (int i = tid; i < n * nq * U; i += 256) {
       const int r = i / U, t = r / nq, head = g0 * sh.G + r - t * nq;
       un.place(i - r * U, D, R);
-      un.load(a.q, (pv.tok0 + t) * a.q_stride + static_cast<int64_t>(head) * D);
+      un.load(a.q, token_at(pv.tok0 + t, a.q_stride) + static_cast<int64_t>(head) * D);
       un.turn(cs + t * (R / 2));
-      un.store(a.q_out, (pv.tok0 + t) * a.q_out_stride + static_cast<int64_t>(head) * D);
+      un.store(a.q_out, token_at(pv.tok0 + t, a.q_out_stride) + static_cast<int64_t>(head) * D);
     }
   }
   const int64_t tile0 = static_cast<int64_t>(pv.page) * sh.page_tiles, tile_bytes = static_cast<int64_t>(P) * D * ESZ;
   const int slots = pv.fill - pv.lo;
-  // Keys: rows of the tile's layout.  fp8: a wavefront a kv head, because the page's scale comes from all of its tokens.
+  // Keys.  fp8: a wavefront a kv head, because the page's scale comes from all of its tokens.
   const int first = FP8 ? lane : tid, step = FP8 ? 64 : 256;
   for (int gi = FP8 ? wave : 0; gi < (FP8 ? ng : 1); gi += FP8 ? 4 : 1) {
     const int heads = FP8 ? 1 : ng;
@@ -231,7 +444,7 @@ __global__ __launch_bounds__(256) void spex_append_rotated_kernel(RotateArgs a, 
         for (int i = lane; i < n * U; i += 64) {
           const int t = i / U;
           un.place(i - t * U, D, R);
-          un.load(a.k, (pv.tok0 + t) * a.k_stride + static_cast<int64_t>(g) * D);
+          un.load(a.k, token_at(pv.tok0 + t, a.k_stride) + static_cast<int64_t>(g) * D);
           un.turn(cs + t * (R / 2));
           top = fmaxf(top, un.top());
         }
@@ -245,65 +458,24 @@ __global__ __launch_bounds__(256) void spex_append_rotated_kernel(RotateArgs a, 
       const int slot = pv.lo + t;
       un.place(i - r * U, D, R);
       if (t < n) {
-        un.load(a.k, (pv.tok0 + t) * a.k_stride + static_cast<int64_t>(g) * D);
+        un.load(a.k, token_at(pv.tok0 + t, a.k_stride) + static_cast<int64_t>(g) * D);
         un.turn(cs + t * (R / 2));
-        if (a.k_out) un.store(a.k_out, (pv.tok0 + t) * a.k_out_stride + static_cast<int64_t>(g) * D);
+        if (a.k_out) un.store(a.k_out, token_at(pv.tok0 + t, a.k_out_stride) + static_cast<int64_t>(g) * D);
       } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) un.e[0].x[j] = un.e[1].x[j] = 0.f;
+        un.clear();
       }
       char *tile = static_cast<char *>(a.k_pool) + (tile0 + g) * tile_bytes;
-      put_eight<KV>(tile, k_offset<KV, LAYOUT>(slot, un.d[0], D), un.e[0], inv);
-      if (un.two) put_eight<KV>(tile, k_offset<KV, LAYOUT>(slot, un.d[1], D), un.e[1], inv);
+      put_eight<KV>(tile, k_offset<KV, kRowMajor>(slot, un.d[0], D), un.e[0], inv);
+      if (un.two) put_eight<KV>(tile, k_offset<KV, kRowMajor>(slot, un.d[1], D), un.e[1], inv);
     }
   }
-  // Values.  Row-major pools: as the keys, unturned.
-  if (!TILED) {
-    const int C = D / 8;
-    for (int gi = FP8 ? wave : 0; gi < (FP8 ? ng : 1); gi += FP8 ? 4 : 1) {
-      const int heads = FP8 ? 1 : ng;
-      float inv = 1.f;
-      if (FP8) {
-        const int g = g0 + gi, at = pv.page * sh.Hkv + g;
-        float s;
-        if (!pv.is_new) {
-          s = a.v_scale[at];
-        } else if (a.v_scale_src) {
-          s = a.v_scale_src[static_cast<int64_t>(pv.new_index) * sh.Hkv + g];
-        } else {
-          float top = 0.f;
-          for (int i = lane; i < n * C; i += 64)
-            top = fmaxf(top, largest(load_eight<F32>(a.v, (pv.tok0 + i / C) * a.v_stride + static_cast<int64_t>(g) * D + i % C * 8)));
-          s = page_scale(wave_max(top));
-        }
-        if (pv.is_new && lane == 0) a.v_scale[at] = s;
-        inv = inverse_scale(s);
-      }
-      for (int i = first; i < slots * heads * C; i += step) {
-        const int r = i / C, t = r / heads, g = g0 + (FP8 ? gi : r - t * heads), d = (i - r * C) * 8;
-        Eight e = {};
-        if (t < n) e = load_eight<F32>(a.v, (pv.tok0 + t) * a.v_stride + static_cast<int64_t>(g) * D + d);
-        put_eight<KV>(static_cast<char *>(a.v_pool) + (tile0 + g) * tile_bytes, (pv.lo + t) * D + d, e, inv);
-      }
-    }
-    return;
-  }
-  // Tiled pools hold values token-minor: a thread takes eight dims of eight tokens and turns them round in registers.  The threads of a
-  // kv head are 2 D / 8 lanes beside each other.
-  constexpr int C = TILED ? DT / 8 : 1;
-  for (int i = tid; i < ng * 2 * C; i += 256) {
-    const int g = g0 + i / (2 * C), t0 = i / C % 2 * 8, d = i % C * 8;
-    u32x4 w[8];
-#pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      w[s] = u32x4{0, 0, 0, 0};
-      const int t = t0 + s - pv.lo;
-      if (t >= 0 && t < n)
-        w[s] = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.v) + (pv.tok0 + t) * a.v_stride + static_cast<int64_t>(g) * D + d);
-    }
+  // Values: as the keys, unturned.
+  const int C = D / 8;
+  for (int gi = FP8 ? wave : 0; gi < (FP8 ? ng : 1); gi += FP8 ? 4 : 1) {
+    const int heads = FP8 ? 1 : ng;
     float inv = 1.f;
     if (FP8) {
-      const int at = pv.page * sh.Hkv + g;
+      const int g = g0 + gi, at = pv.page * sh.Hkv + g;
       float s;
       if (!pv.is_new) {
         s = a.v_scale[at];
@@ -311,59 +483,33 @@ __global__ __launch_bounds__(256) void spex_append_rotated_kernel(RotateArgs a, 
         s = a.v_scale_src[static_cast<int64_t>(pv.new_index) * sh.Hkv + g];
       } else {
         float top = 0.f;
-#pragma unroll
-        for (int s2 = 0; s2 < 8; ++s2) top = fmaxf(top, abs_max8(w[s2]));
-#pragma unroll
-        for (int o = C; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-        s = page_scale(top);
+        for (int i = lane; i < n * C; i += 64)
+          top = fmaxf(top, largest(load_eight<F32>(a.v, token_at(pv.tok0 + i / C, a.v_stride) + static_cast<int64_t>(g) * D + i % C * 8)));
+        s = page_scale(wave_max(top));
       }
-      if (pv.is_new && i % (2 * C) == 0) a.v_scale[at] = s;
+      if (pv.is_new && lane == 0) a.v_scale[at] = s;
       inv = inverse_scale(s);
     }
-    char *tile = static_cast<char *>(a.v_pool) + (tile0 + g) * tile_bytes;
-    const bool whole = t0 >= pv.lo && t0 + 8 <= pv.fill;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {  // dim d + k of the eight tokens
-      char *dst = tile + ESZ * v_offset<KV, kMfmaTiled>(t0, d + k, D);
-      if (FP8) {
-        u32x2 c = {0, 0};
-#pragma unroll
-        for (int s = 0; s < 8; ++s) c[s >> 2] |= encode_e4m3(bf16_bits_to_float(half_word(w[s], k)) * inv) << (8 * (s & 3));
-        if (whole) {
-          *reinterpret_cast<u32x2 *>(dst) = c;
-        } else {
-#pragma unroll
-          for (int s = 0; s < 8; ++s)
-            if (t0 + s >= pv.lo && t0 + s < pv.fill) dst[s] = static_cast<char>(c[s >> 2] >> (8 * (s & 3)));
-        }
-      } else {
-        u32x4 h;
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-          h[s] = bf16_bits_to_f16_bits(half_word(w[2 * s], k)) | static_cast<uint32_t>(bf16_bits_to_f16_bits(half_word(w[2 * s + 1], k))) << 16;
-        if (whole) {
-          *reinterpret_cast<u32x4 *>(dst) = h;
-        } else {
-#pragma unroll
-          for (int s = 0; s < 8; ++s)
-            if (t0 + s >= pv.lo && t0 + s < pv.fill) *reinterpret_cast<uint16_t *>(dst + 2 * s) = static_cast<uint16_t>(h[s >> 1] >> (16 * (s & 1)));
-        }
-      }
+    for (int i = first; i < slots * heads * C; i += step) {
+      const int r = i / C, t = r / heads, g = g0 + (FP8 ? gi : r - t * heads), d = (i - r * C) * 8;
+      Eight e = {};
+      if (t < n) e = load_eight<F32>(a.v, token_at(pv.tok0 + t, a.v_stride) + static_cast<int64_t>(g) * D + d);
+      put_eight<KV>(static_cast<char *>(a.v_pool) + (tile0 + g) * tile_bytes, (pv.lo + t) * D + d, e, inv);
     }
   }
 }
 
 // Element by element: a workgroup per (page, kv head), with the query heads of the kv head; a thread turns whole pairs.
 template <int KV, int LAYOUT>
-__global__ __launch_bounds__(256) void spex_append_rotated_any_kernel(RotateArgs a, Shape sh) {
+__global__ __launch_bounds__(256) void spex_append_rotated_any_kernel(RotateArgs a, Shape sh, RotateLists in) {
   typedef typename std::conditional<KV == kF32, float, typename std::conditional<KV == kBF16, uint16_t, uint8_t>::type>::type T;
   typedef typename std::conditional<KV == kF32, float, uint16_t>::type S;
   constexpr bool FP8 = KV == kFP8;
   __shared__ float red[2][4];
   const int D = sh.D, P = sh.P, R = a.rotary_dim, half = R / 2, per = half + D - R;  // per: pairs and single dims of a row
   const int tid = threadIdx.x, g = blockIdx.y;
-  const PageVisit pv = page_visit(a, P);
-  apply_patches(a);
+  const PageVisit pv = page_visit(a, in, P);
+  apply_patches(a, in);
   const int n = pv.hi - pv.lo, slots = pv.fill - pv.lo;
   auto widen = [](S x) { return KV == kF32 ? static_cast<float>(x) : bf16_bits_to_float(static_cast<uint16_t>(x)); };
   auto narrow = [](float x) {
@@ -382,7 +528,7 @@ __global__ __launch_bounds__(256) void spex_append_rotated_any_kernel(RotateArgs
     e.x[0] = widen(static_cast<const S *>(base)[row + e.d[0]]);
     e.x[1] = widen(static_cast<const S *>(base)[row + e.d[1]]);
     if (j < half) {
-      const f32x2 y = turned(e.x[0], e.x[1], cos_sin_turns(a.positions ? a.positions[pv.tok0 + t] : pv.pos0 + t, a.freq[j]));
+      const f32x2 y = turned(e.x[0], e.x[1], cos_sin_turns(position(a, in, pv, t), a.freq[j]));
       e.x[0] = y[0];
       e.x[1] = y[1];
     }
