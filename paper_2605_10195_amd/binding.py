@@ -360,27 +360,31 @@ class SpexTree:
         na = _i32(nodes)
         ca = None if counts is None else _i32(counts)
         pa = None if positions is None else _i32(positions)
-        total = len(na) if ca is None else int(ca.sum(dtype=np.int64))
-        want = torch.float32 if self.kv_dtype == F32 else torch.bfloat16
+        total = len(na) if ca is None else _total(ca)
+        want, device = torch.float32 if self.kv_dtype == F32 else torch.bfloat16, _device()
         assert ca is None or len(ca) == len(na)
         assert pa is None or pa.shape == (total,)
-        assert k.shape[0] == total and v.shape[0] == total and (q is None or q.shape[0] == total)
-        if q_out is None and q is not None:
-            q_out = torch.empty((total, self.Hq, self.D), dtype=want, device=q.device)
+        d = Rotated()
+        d.k, d.k_stride = k.data_ptr(), _token_stride(k, total, self.Hkv, self.D, want, device)
+        d.v, d.v_stride = v.data_ptr(), _token_stride(v, total, self.Hkv, self.D, want, device)
+        if q is not None:
+            d.q, d.q_stride = q.data_ptr(), _token_stride(q, total, self.Hq, self.D, want, device)
+            if q_out is None:
+                q_out = torch.empty((total, self.Hq, self.D), dtype=want, device=q.device)
+            d.q_out, d.q_out_stride = q_out.data_ptr(), _token_stride(q_out, total, self.Hq, self.D, want, device)
+        else:
+            assert q_out is None
         if k_out is None and want_k:
             k_out = torch.empty((total, self.Hkv, self.D), dtype=want, device=k.device)
-        assert all(t is None or t.dtype == want for t in (q, k, v, q_out, k_out))
-        assert (q is None) == (q_out is None) and (q_out is None or q_out.shape == q.shape) and (k_out is None or k_out.shape == k.shape)
-        assert _on_current_device(q, k, v, q_out, k_out, k_scales, v_scales), "all tensors must lie on the current device"
+        if k_out is not None:
+            d.k_out, d.k_out_stride = k_out.data_ptr(), _token_stride(k_out, total, self.Hkv, self.D, want, device)
         if k_scales is not None:
-            assert k_scales.dtype == torch.float32 and v_scales.dtype == torch.float32
-            assert k_scales.is_contiguous() and v_scales.is_contiguous() and k_scales.shape == v_scales.shape
-            assert k_scales.dim() == 2 and k_scales.shape[1] == self.Hkv
-        d = Rotated(_dev(q), _dev(k), _dev(v), _dev(q_out), _dev(k_out),
-                    0 if q is None else _token_stride(q, self.Hq, self.D), _token_stride(k, self.Hkv, self.D),
-                    _token_stride(v, self.Hkv, self.D), 0 if q is None else _token_stride(q_out, self.Hq, self.D),
-                    0 if k_out is None else _token_stride(k_out, self.Hkv, self.D), _dev(k_scales), _dev(v_scales),
-                    0 if k_scales is None else k_scales.shape[0])
+            for x in (k_scales, v_scales):
+                assert x.dtype is torch.float32 and x.dim() == 2 and x.shape[1] == self.Hkv and x.is_contiguous() and x.get_device() == device
+            assert k_scales.shape == v_scales.shape
+            d.k_scales, d.v_scales, d.n_scales = k_scales.data_ptr(), v_scales.data_ptr(), k_scales.shape[0]
+        else:
+            assert v_scales is None
         _check(lib.spex_tree_append_rotated(self._h, _addr(na), _addr(ca), len(na), _addr(pa), C.byref(d), _stream()))
         return q_out, k_out
 
@@ -584,20 +588,28 @@ def spex_tree_append_tokens_quantize(tree: SpexTree, nodes, k, v, k_scales, v_sc
 
 
 # ---- spex_prompt.h -------------------------------------------------------------------------
-def _token_stride(t: torch.Tensor, heads: int, dim: int) -> int:
-    """Elements between tokens of [tokens, heads, dim]; the heads of a token must be dense."""
-    assert t.dim() == 3 and t.shape[1:] == (heads, dim), t.shape
-    assert (dim == 1 or t.stride(2) == 1) and (heads == 1 or t.stride(1) == dim), "the heads of a token must be contiguous"
-    if t.shape[0] <= 1:
+def _total(counts: np.ndarray) -> int:
+    return sum(counts.tolist()) if len(counts) < 64 else int(counts.sum(dtype=np.int64))
+
+
+def _device() -> int:
+    """The calls run on the current stream of the current device; -2 is no tensor's device."""
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
+
+
+def _token_stride(t: torch.Tensor, total: int, heads: int, dim: int, dtype: torch.dtype, device: int) -> int:
+    """Elements between tokens of [total, heads, dim] (0: no second one); the heads of a token must be dense.  Checks the rest too:
+    four tensors a call, 1 us each through torch's attributes asked one by one."""
+    shape = t.shape
+    assert len(shape) == 3 and shape[0] == total and shape[1] == heads and shape[2] == dim, shape
+    assert t.dtype is dtype, t.dtype
+    assert t.get_device() == device, "all tensors must lie on the current device"
+    s0, s1, s2 = t.stride()
+    assert (s2 == 1 or dim == 1) and (s1 == dim or heads == 1), "the heads of a token must be contiguous"
+    if total <= 1:
         return 0
-    assert t.stride(0) >= heads * dim, "tokens must not overlap"
-    return t.stride(0)
-
-
-def _on_current_device(*tensors: Optional[torch.Tensor]) -> bool:
-    """The calls run on the current stream of the current device."""
-    here = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None
-    return all(t is None or (t.is_cuda and t.get_device() == here) for t in tensors)
+    assert s0 >= heads * dim, "tokens must not overlap"
+    return s0
 
 
 def spex_prompt_attention(lens: Sequence[int], q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sm_scale: float,
@@ -606,20 +618,21 @@ def spex_prompt_attention(lens: Sequence[int], q: torch.Tensor, k: torch.Tensor,
     a stride between tokens (parts of one projection); out has q's shape and type.  Returns (out, lse)."""
     la = _i32(lens)
     total, hq, dim = q.shape
-    hkv = k.shape[1]
-    assert q.dtype in (torch.float32, torch.bfloat16) and k.dtype == q.dtype and v.dtype == q.dtype
-    assert k.shape[0] == total and v.shape[0] == total and int(la.sum(dtype=np.int64)) == total
+    hkv, dtype, device = k.shape[1], q.dtype, _device()
+    assert dtype in (torch.float32, torch.bfloat16), dtype
+    assert _total(la) == total
+    cfg = PromptConfig(hq, hkv, dim, F32 if dtype is torch.float32 else BF16, _token_stride(q, total, hq, dim, dtype, device),
+                       _token_stride(k, total, hkv, dim, dtype, device), _token_stride(v, total, hkv, dim, dtype, device), 0)
     if out is None:
-        out = torch.empty((total, hq, dim), dtype=q.dtype, device=q.device)
-    assert out.dtype == q.dtype and out.shape == q.shape
-    if lse is None and want_lse:
+        out = torch.empty((total, hq, dim), dtype=dtype, device=q.device)
+    else:
+        cfg.out_stride = _token_stride(out, total, hq, dim, dtype, device)
+    if lse is not None:
+        assert lse.dtype is torch.float32 and lse.shape == (total, hq) and lse.is_contiguous() and lse.get_device() == device
+    elif want_lse:
         lse = torch.empty((total, hq), dtype=torch.float32, device=q.device)
-    assert lse is None or (lse.dtype == torch.float32 and lse.shape == (total, hq) and lse.is_contiguous())
-    assert _on_current_device(q, k, v, out, lse), "all tensors must lie on the current device"
-    cfg = PromptConfig(hq, hkv, dim, F32 if q.dtype == torch.float32 else BF16, _token_stride(q, hq, dim), _token_stride(k, hkv, dim),
-                       _token_stride(v, hkv, dim), _token_stride(out, hq, dim))
-    _check(lib.spex_prompt_attention(C.byref(cfg), _addr(la), len(la), _dev(q), _dev(k), _dev(v), _dev(out), _dev(lse),
-                                     float(sm_scale), _stream()))
+    _check(lib.spex_prompt_attention(C.byref(cfg), _addr(la), len(la), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+                                     _dev(lse), float(sm_scale), _stream()))
     return out, lse
 
 

@@ -838,7 +838,7 @@ static spex_status_t append_rotated_impl(spex_tree_t *t, const spex_node_t *node
     return SPEX_ERR_INVALID_ARG;
 
   // Check everything before touching the table: the call is all or nothing.
-  const int32_t P = t->cfg.page_size;
+  const int32_t P = t->cfg.page_size, shift = __builtin_ctz(P);  // a division takes as long as the rest of a node's work
   int64_t need = 0, visits = 0, tokens = 0;
   bool ascending = true;
   for (int32_t i = 0; i < n_nodes; ++i) {
@@ -851,8 +851,9 @@ static spex_status_t append_rotated_impl(spex_tree_t *t, const spex_node_t *node
     ascending = ascending && (i == 0 || nodes[i - 1] < u);
     tokens += c;
     if (c == 0) continue;
-    need += t->pt->new_pages_needed(u, c);
-    visits += (static_cast<int64_t>(nd.n_tokens) + c - 1) / P - nd.n_tokens / P + 1;
+    const int32_t last = (nd.n_tokens + c - 1) >> shift;
+    need += last + 1 - static_cast<int64_t>(nd.pages.size());
+    visits += last - (nd.n_tokens >> shift) + 1;
   }
   std::vector<int32_t> sorted;
   if (!ascending) {
@@ -911,7 +912,7 @@ static spex_status_t append_rotated_impl(spex_tree_t *t, const spex_node_t *node
     t->pt->append(u, c, &first_new);  // cannot fail: the pages were counted above
     const spex::Node &nd = t->pt->node(u);
     for (int32_t at = old_tokens; at < old_tokens + c;) {
-      const int32_t page = at / P, lo = at % P, n = std::min(P - lo, old_tokens + c - at);
+      const int32_t page = at >> shift, lo = at & (P - 1), n = std::min(P - lo, old_tokens + c - at);
       const bool is_new = page >= first_new;
       rec[0] = nd.pages[page];
       rec[1] = lo | (lo + n) << 8 | (is_new ? 1 << 16 : 0);

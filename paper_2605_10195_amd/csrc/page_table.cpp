@@ -3,7 +3,7 @@
 namespace spex {
 
 PageTable::PageTable(int64_t num_pages, int32_t page_size, const int32_t *free_order)
-    : num_pages_(num_pages), page_size_(page_size) {
+    : num_pages_(num_pages), page_size_(page_size), page_shift_(__builtin_ctz(static_cast<uint32_t>(page_size))) {
   free_.resize(static_cast<size_t>(num_pages));
   // free_order[0] must be popped first, so it goes to the back of the stack vector.
   for (int64_t i = 0; i < num_pages; ++i) {
@@ -30,7 +30,7 @@ int32_t PageTable::fork(int32_t parent, int32_t n) {
 int32_t PageTable::new_pages_needed(int32_t u, int32_t n_tokens) const {
   const Node &nd = nodes_[u];
   const int64_t total = static_cast<int64_t>(nd.n_tokens) + n_tokens;
-  const int64_t pages = (total + page_size_ - 1) / page_size_;
+  const int64_t pages = (total + page_size_ - 1) >> page_shift_;
   return static_cast<int32_t>(pages - static_cast<int64_t>(nd.pages.size()));
 }
 

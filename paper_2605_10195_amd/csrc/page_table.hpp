@@ -65,7 +65,7 @@ class PageTable {
 
  private:
   int64_t num_pages_;
-  int32_t page_size_;
+  int32_t page_size_, page_shift_;  // a power of two and its logarithm
   std::vector<Node> nodes_;
   std::vector<int32_t> free_;  // stack, top = back()
   int64_t live_nodes_ = 0;
