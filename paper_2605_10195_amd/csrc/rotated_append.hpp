@@ -433,7 +433,8 @@ __global__ __launch_bounds__(256) void spex_append_rotated_rows_kernel(RotateArg
     const int heads = FP8 ? 1 : ng;
     float inv = 1.f;
     if (FP8) {
-      const int g = g0 + gi, at = pv.page * sh.Hkv + g;
+      const int g = g0 + gi;
+      const int64_t at = static_cast<int64_t>(pv.page) * sh.Hkv + g;
       float s;
       if (!pv.is_new) {
         s = a.k_scale[at];
@@ -475,7 +476,8 @@ __global__ __launch_bounds__(256) void spex_append_rotated_rows_kernel(RotateArg
     const int heads = FP8 ? 1 : ng;
     float inv = 1.f;
     if (FP8) {
-      const int g = g0 + gi, at = pv.page * sh.Hkv + g;
+      const int g = g0 + gi;
+      const int64_t at = static_cast<int64_t>(pv.page) * sh.Hkv + g;
       float s;
       if (!pv.is_new) {
         s = a.v_scale[at];
@@ -548,7 +550,7 @@ __global__ __launch_bounds__(256) void spex_append_rotated_any_kernel(RotateArgs
   auto v_row = [&](int t) { return (pv.tok0 + t) * a.v_stride + static_cast<int64_t>(g) * D; };
   float kinv = 1.f, vinv = 1.f;
   if (FP8) {
-    const int at = pv.page * sh.Hkv + g;
+    const int64_t at = static_cast<int64_t>(pv.page) * sh.Hkv + g;
     float ks, vs;
     if (!pv.is_new) {
       ks = a.k_scale[at];

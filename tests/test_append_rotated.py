@@ -460,3 +460,56 @@ def test_a_search_from_its_prompts_on(kv):
                 assert float((out[i].double().cpu() - want).abs().max()) <= 2e-3
     assert states.count(2) >= 17 and states[0] == 1                # patched in the append's own launch, planned afresh at most now and then
     t.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3", "f32"])
+@pytest.mark.parametrize("heads,page,rotary", [((8, 2, 128), 16, 128), ((6, 3, 64), 16, 32), ((4, 2, 40), 8, 16), ((3, 3, 20), 4, 20)], ids=str)
+def test_any_cut_into_calls_stores_the_same(kv, heads, page, rotary):
+    """The tokens of 150 nodes in one call, whose lists are long, or in many with few tokens each, that start pages, end inside them and go on
+    there: the same results bit by bit.  fp8 pages get given scales, since those of their tokens would depend on the cut."""
+    per, nodes = 37, 150
+    q, k, v = draw(nodes * per, heads, kv, 12)
+    pages = -(-per // page)
+    scales = 0.004 + 0.004 * torch.rand((2, nodes, pages, heads[1]), device="cuda")
+    rows = torch.arange(nodes * per, device="cuda").view(nodes, per)
+    results = []
+    for cuts in ([37], [1, 3, 8, 2, 12, 7, 4], [1] * 37, [20, 17], [9, 9, 9, 10]):
+        some = list(range(nodes)) if len(cuts) < 20 else list(range(0, nodes, 10))
+        t = tree_of(heads, page, kv, nodes * pages, rotary, False)
+        ids = t.fork(-1, len(some))
+        q_out, k_out, at = torch.empty_like(q), torch.empty_like(k), 0
+        for n in cuts:
+            new = slice(-(-at // page), -(-(at + n) // page))
+            s = [None if kv != "fp8_e4m3" else x[some, new].reshape(-1, heads[1]).contiguous() for x in scales]
+            r = rows[some, at:at + n].reshape(-1)
+            a, b = t.append_rotated(ids, [n] * len(ids), q[r], k[r], v[r], k_scales=s[0], v_scales=s[1], want_k=True)
+            q_out[r], k_out[r], at = a, b, at + n
+        results.append((some, q_out, k_out, [t.gather_kv(u, 0, per) for u in ids]))
+        t.close()
+    _, q0, k0, g0 = results[0]
+    for some, q1, k1, g1 in results[1:]:
+        r = rows[some].reshape(-1)
+        assert torch.equal(q0[r], q1[r]) and torch.equal(k0[r], k1[r])
+        for i, u in enumerate(some):
+            for j in range(4 if kv == "fp8_e4m3" else 2):
+                assert torch.equal(g0[u][j], g1[i][j]), (len(some), u, j)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("head_dim", [8, 7])
+def test_page_scales_behind_two_to_the_31(head_dim):
+    """255 kv heads on pages of one token: the scales of the pool's last pages have indexes that 32 bits do not hold."""
+    heads, num_pages = (255, 255, head_dim), (1 << 31) // 255 + 100
+    t = tree_of(heads, 1, "fp8_e4m3", num_pages, head_dim // 2 * 2, False, free_order=np.arange(num_pages, dtype=np.int32)[::-1].copy())
+    (u,) = t.fork(-1, 1)
+    q, k, v = draw(3, heads, "fp8_e4m3", 13)
+    t.append_rotated([u], [3], q, k, v)
+    assert min(t.path_pages(u)[0]) * 255 >= 1 << 31
+    freq = FREQ(head_dim // 2 * 2)
+    ks, vs = (x[:num_pages * 255].view(num_pages, 255)[t.path_pages(u)[0]] for x in (t.k_scale, t.v_scale))
+    for s, x in ((ks, turned(k, np.arange(3), freq, head_dim // 2 * 2, False)), (vs, v.double().cpu())):
+        want = x.abs().amax(-1) / 448
+        # as in test_page_scales_computed_and_given
+        assert bool(((s.double().cpu() - want).abs() <= 8 * 2.0 ** -24 * want * 1.5).all())
+    t.close()
