@@ -2,7 +2,6 @@
 #include "../../include/spex_prompt.h"
 
 #include <algorithm>
-#include <cmath>
 #include <new>
 #include <vector>
 
@@ -27,7 +26,7 @@ extern "C" spex_status_t spex_prompt_attention(const spex_prompt_config_t *cfg, 
       cfg->head_dim < 1 || cfg->head_dim > 256)
     return SPEX_ERR_INVALID_ARG;
   if (cfg->dtype != SPEX_F32 && cfg->dtype != SPEX_BF16) return SPEX_ERR_UNSUPPORTED;
-  if (!(sm_scale > 0.f) || std::isinf(sm_scale)) return SPEX_ERR_INVALID_ARG;
+  if (!(sm_scale >= 1e-38f && sm_scale <= 1e37f)) return SPEX_ERR_INVALID_ARG;  // times log2(e) it has a reciprocal in fp32
   const int64_t q_row = static_cast<int64_t>(cfg->num_q_heads) * cfg->head_dim;
   const int64_t kv_row = static_cast<int64_t>(cfg->num_kv_heads) * cfg->head_dim;
   const int64_t strides[4] = {cfg->q_stride ? cfg->q_stride : q_row, cfg->k_stride ? cfg->k_stride : kv_row,

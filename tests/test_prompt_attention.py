@@ -240,3 +240,19 @@ def test_equals_decode_attention_over_the_appended_prompt():
     bound = 2.0 ** -8 * 1.01 * (torch.as_tensor(reference(lens, q, k, v, d ** -0.5)[2], device="cuda") + ref.abs().double()) + 2e-3
     assert bool(((out.double() - ref.double()).abs() <= bound).all()) and float((lse - ref_lse).abs().max()) <= 2e-3
     tree.close()
+
+
+@pytest.mark.parametrize("scale,want", [(1e-38, True), (1e37, True), (1e-42, False), (3e38, False)])
+def test_scales_whose_reciprocal_fp32_does_not_hold(scale, want):
+    assert call([0], scale=scale) == (0 if want else INVALID)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [1e-38, 1e4])
+def test_scales_at_the_ends(dtype, scale):
+    """Scores of about nothing (all weights equal) and of tens of thousands (one key takes all the weight)."""
+    lens = [1, 40, 300]
+    q, k, v = inputs(lens, (4, 2, 64), dtype, 31)
+    out, lse = spex.prompt_attention(lens, q, k, v, scale)
+    check(lens, q, k, v, out, lse, scale)
