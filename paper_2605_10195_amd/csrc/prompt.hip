@@ -103,7 +103,7 @@ __device__ __forceinline__ void copy_to_lds(const u32x4 rows, int lane_off, int 
 __device__ __forceinline__ void tile_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // ---- bf16 ----------------------------------------------------------------------------------------
-// LDS tiles: 64 keys, rows of ROWB bytes (128, 256 or 512), 16-byte piece c of row t at place c ^ swz(t).  A K operand read
+// LDS tiles: rows of ROWB bytes (128, 256 or 512), 16-byte piece c of row t at place c ^ swz(t).  A K operand read
 // has 32 rows at one piece, a V read four rows at two neighbouring pieces: with the bits of t in this order both
 // spread over all banks.
 template <int ROWB>
@@ -112,9 +112,11 @@ __device__ __forceinline__ int swz(int t) {
   return ((t & 3) << 2) | (((t >> 2) & 1) << 1) | ((t >> 3) & 1);
 }
 
+// 64 keys a tile, 32 where a row has 512 bytes: two workgroups then fit into a CU.  8 prompts of 4096, 16/4/192: 1115 us
+// with 64 keys, 825 with 32 (1.0 PFLOP/s); 4 of 4096, 16/4/256: 850 and 611 (0.9).
 template <int DP>
 struct TileB {
-  static constexpr int kKeys = 64;
+  static constexpr int kKeys = DP <= 128 ? 64 : 32;
   static constexpr int kRowB = DP <= 64 ? 128 : (DP <= 128 ? 256 : 512);
   static constexpr int kBytes = kKeys * kRowB;
 };
@@ -161,49 +163,59 @@ struct PlaceF {
 };
 
 template <int DP, int NW>
-__global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_kernel(PromptArgs p) {
-  constexpr int ROWB = TileB<DP>::kRowB, TILE = TileB<DP>::kBytes, KS = DP / 16, DT = DP / 32;
+__global__ __launch_bounds__(64 * NW, 2) void spex_prompt_bf16_kernel(PromptArgs p) {
+  constexpr int ROWB = TileB<DP>::kRowB, TILE = TileB<DP>::kBytes, KS = DP / 16, DT = DP / 32, KEYS = TileB<DP>::kKeys, HALVES = KEYS / 32;
   __shared__ __attribute__((aligned(1024))) char lds_[4 * TILE];
   lds_char *lds = (lds_char *)lds_;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
   const RowSet rs = row_set<NW>(p, wave);
   const int pieces = p.D / 8;
-  Stager<64, ROWB, NW, PlaceB<ROWB>> ks(static_cast<const char *>(p.k) + (rs.row0 * p.k_stride + rs.kv * p.D) * 2, p.k_stride * 2, rs.len, p.D * 2, wave, lane);
-  Stager<64, ROWB, NW, PlaceB<ROWB>> vs(static_cast<const char *>(p.v) + (rs.row0 * p.v_stride + rs.kv * p.D) * 2, p.v_stride * 2, rs.len, p.D * 2, wave, lane);
-  const int tiles = rs.last / 64 + 1, mine = rs.live ? min(rs.q0 + kPromptRows - 1, rs.len - 1) / 64 + 1 : 0;
+  Stager<KEYS, ROWB, NW, PlaceB<ROWB>> ks(static_cast<const char *>(p.k) + (rs.row0 * p.k_stride + rs.kv * p.D) * 2, p.k_stride * 2, rs.len, p.D * 2, wave, lane);
+  Stager<KEYS, ROWB, NW, PlaceB<ROWB>> vs(static_cast<const char *>(p.v) + (rs.row0 * p.v_stride + rs.kv * p.D) * 2, p.v_stride * 2, rs.len, p.D * 2, wave, lane);
+  const int tiles = rs.last / KEYS + 1, mine = rs.live ? min(rs.q0 + kPromptRows - 1, rs.len - 1) / KEYS + 1 : 0;
   lds_char *const mine_at = lds + wave * 1024;  // where this wavefront's copies into the first buffer go
   // Queries and results cross LDS, so that memory sees whole rows: as the operands lie a load or store has 32 or 16 bytes of
-  // each of 32 rows.  Every wavefront has 32 rows of the buffer that is free then: a quarter of a tile of K and one of V.
+  // each of 32 rows.  Every wavefront has 32 rows of the buffer that is free then, half a tile; tiles of 32 keys leave no room beside a
+  // buffer in use, so all of them are free at those times.
   static_assert(NW == 4, "");
-  auto rows_at = [&](int buffer) { return lds + ((wave >> 1) * 2 + buffer) * TILE + (wave & 1) * (TILE / 2); };
+  auto rows_at = [&](int buffer) { return HALVES == 2 ? lds + ((wave >> 1) * 2 + buffer) * TILE + (wave & 1) * (TILE / 2) : lds + wave * TILE; };
   const int64_t row = rs.row0 + rs.q0, head0 = static_cast<int64_t>(rs.live ? rs.head : 0) * p.D;
   if (rs.live) {
     Stager<32, ROWB, 1, PlaceB<ROWB>> qs(static_cast<const char *>(p.q) + (row * p.q_stride + head0) * 2, p.q_stride * 2, rs.len - rs.q0, p.D * 2, 0, lane);
     qs.next(rows_at(1));
   }
-  ks.next(mine_at);
-  vs.next(mine_at + 2 * TILE);
-  // Places of the operand pieces in a tile; the other keys of the tile lie at constant distances.
-  int koff[KS], voff[DT][2];
+  if (HALVES == 2) {
+    ks.next(mine_at);
+    vs.next(mine_at + 2 * TILE);
+  }
+  // Places of the operand pieces in a tile; the other keys of the tile and the other half of a row of 512 bytes lie at constant
+  // distances.
+  constexpr int KO = KS < 8 ? KS : 8, VO = DT < 4 ? DT : 4;
+  int koff[KO], voff[VO][2];
 #pragma unroll
-  for (int s = 0; s < KS; ++s) koff[s] = col * ROWB + ((2 * s + h) ^ swz<ROWB>(col)) * 16;
+  for (int s = 0; s < KO; ++s) koff[s] = col * ROWB + ((2 * s + h) ^ swz<ROWB>(col)) * 16;
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
+  for (int dt = 0; dt < VO; ++dt)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int t = 8 * j + 4 * h + ((lane & 15) >> 2), c = 4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
       voff[dt][j] = t * ROWB + (c ^ swz<ROWB>(t)) * 16 + (lane & 1) * 8;
     }
   bf16x8 qf[KS];
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * TILE / 1024 / NW) : "memory");  // the copies of K and V are younger
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(HALVES == 2 ? 2 * TILE / 1024 / NW : 0) : "memory");  // the copies of K and V are younger
   {
     const lds_char *rows = rows_at(1);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      u32x4 x = *(const lds_u32x4 *)(rows + koff[s]);
+      u32x4 x = *(const lds_u32x4 *)(rows + koff[s % KO] + s / KO * 256);
       if (2 * s + h >= pieces) x = u32x4{0, 0, 0, 0};
       qf[s] = __builtin_bit_cast(bf16x8, x);
     }
+  }
+  if (HALVES == 1) {
+    tile_barrier();
+    ks.next(mine_at);
+    vs.next(mine_at + 2 * TILE);
   }
   f32x16 o[DT];
 #pragma unroll
@@ -223,27 +235,27 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_k
       vs.next(to + 2 * TILE);
     }
     if (t >= mine) continue;
-    f32x16 s[2];
+    f32x16 s[HALVES];
 #pragma unroll
-    for (int kt2 = 0; kt2 < 2; ++kt2) {
+    for (int kt2 = 0; kt2 < HALVES; ++kt2) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[kt2][r] = 0.f;
 #pragma unroll
       for (int i = 0; i < KS; ++i) {
-        const bf16x8 kf = __builtin_bit_cast(bf16x8, *(const lds_u32x4 *)(kt + koff[i] + kt2 * 32 * ROWB));
+        const bf16x8 kf = __builtin_bit_cast(bf16x8, *(const lds_u32x4 *)(kt + koff[i % KO] + i / KO * 256 + kt2 * 32 * ROWB));
         s[kt2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[kt2], 0, 0, 0);
       }
     }
-    if (t * 64 + 63 > rs.q0) {
+    if (t * KEYS + KEYS - 1 > rs.q0) {
 #pragma unroll
-      for (int kt2 = 0; kt2 < 2; ++kt2)
+      for (int kt2 = 0; kt2 < HALVES; ++kt2)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (t * 64 + kt2 * 32 + 8 * (r / 4) + 4 * h + r % 4 > qpos) s[kt2][r] = -__builtin_huge_valf();
+          if (t * KEYS + kt2 * 32 + 8 * (r / 4) + 4 * h + r % 4 > qpos) s[kt2][r] = -__builtin_huge_valf();
     }
     float mx = s[0][0];
 #pragma unroll
-    for (int r = 1; r < 32; ++r) mx = fmaxf(mx, s[r / 16][r % 16]);
+    for (int r = 1; r < KEYS / 2; ++r) mx = fmaxf(mx, s[r / 16][r % 16]);
     if (__any(mx > limit)) {
       const float mn = fmaxf(m, fmaxf(mx, other_half(mx)) * p.scale_log2), f = fast_exp2(m - mn);
       m = mn;
@@ -254,26 +266,27 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_bf16_k
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] *= f;
     }
-    uint32_t pw[16];
+    uint32_t pw[KEYS / 4];
 #pragma unroll
-    for (int r = 0; r < 32; r += 2) {
+    for (int r = 0; r < KEYS / 2; r += 2) {
       const float a = fast_exp2(__builtin_fmaf(s[r / 16][r % 16], p.scale_log2, -m));
       const float b = fast_exp2(__builtin_fmaf(s[r / 16][r % 16 + 1], p.scale_log2, -m));
       l += a + b;
       pw[r / 2] = pack_bf16(a, b);
     }
 #pragma unroll
-    for (int sl = 0; sl < 4; ++sl) {
+    for (int sl = 0; sl < KEYS / 16; ++sl) {
       const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pw[4 * sl], pw[4 * sl + 1], pw[4 * sl + 2], pw[4 * sl + 3]});
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
-        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + voff[dt][0] + sl * 16 * ROWB));
-        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + voff[dt][1] + sl * 16 * ROWB));
+        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + voff[dt % VO][0] + dt / VO * 256 + sl * 16 * ROWB));
+        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + voff[dt % VO][1] + dt / VO * 256 + sl * 16 * ROWB));
         const u32x2 a0 = __builtin_bit_cast(u32x2, v0), a1 = __builtin_bit_cast(u32x2, v1);
         o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u32x4{a0[0], a0[1], a1[0], a1[1]}), pf, o[dt], 0, 0, 0);
       }
     }
   }
+  if (HALVES == 1) tile_barrier();
   if (!rs.live) return;
   l += other_half(l);
   const float inv = 1.0f / l;
@@ -631,11 +644,11 @@ PromptKernel prompt_kernel(bool f32, bool wide, int32_t D, int64_t row_sets, int
   // longest, in units of 32 keys, is shorter by enough: a workgroup has some other work as long as `fixed` units, and keys
   // and values are then not shared by four row sets.  us, whole / split; heads 32/8/128, one prompt of 1: 4.9 / 4.1, 256: 8.6 / 6.8,
   // 512 (512 row sets): 13.0 / 9.9, 768: 17.7 / 18.0, 1024: 22.2 / 23.1, 2048: 45.9 / 61.3; 8/2/128, 2048: 37.4 / 21.9, 4096 (1024):
-  // 70.7 / 57.7, 8192: 164 / 194; 8 of 128, 32/8/128 (1024): 7.3 / 12.1; 16/2/64, 2048 (1024): 32.7 / 20.3; 16/4/256, 512 (256): 27.2 / 16.9,
-  // 1500 (752): 69 / 65; fp32 8/2/64, 256: 23.1 / 9.1, 32/8/128, 256 (256): 38.7 / 15.8, 512: 71.7 / 34.3, 32 of 64 (2048): 29 / 67.
+  // 70.7 / 57.7, 8192: 164 / 194; 8 of 128, 32/8/128 (1024): 7.3 / 12.1; 16/2/64, 2048 (1024): 32.7 / 20.3; 16/4/256, 512 (256): 27.4 / 17.0,
+  // 1024 (512): 49 / 34, 1500 (752): 68 / 65, 2048 (1024): 93 / 100, 16/4/192, 1500 (752): 44 / 54; fp32 8/2/64, 256: 23.1 / 9.1, 32/8/128, 256 (256): 38.7 / 15.8, 512: 71.7 / 34.3, 32 of 64 (2048): 29 / 67.
   const int32_t row_b = f32 ? (D <= 64 ? 256 : 512) : (D <= 64 ? 128 : (D <= 128 ? 256 : 512));
   const int64_t at_once = 256 * (512 / row_b), rounds = (row_sets + at_once - 1) / at_once;
-  const double units = (longest + 31) / 32, fixed = f32 ? 0.5 : 3.0, shared = f32 ? 1.3 : 1.5;
+  const double units = (longest + 31) / 32, fixed = f32 ? 0.5 : 3.0, shared = f32 ? 1.3 : (D <= 128 ? 1.5 : 1.2);
   k.split = rounds <= 1 || shared * static_cast<double>(rounds) * (units / kWaves + fixed) < units;
   if (k.split) k.sets = 1;
   return k;

@@ -256,3 +256,12 @@ def test_scales_at_the_ends(dtype, scale):
     q, k, v = inputs(lens, (4, 2, 64), dtype, 31)
     out, lse = spex.prompt_attention(lens, q, k, v, scale)
     check(lens, q, k, v, out, lse, scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [(8, 2, 256), (8, 4, 224), (8, 2, 192), (8, 1, 160)], ids=str)
+def test_wide_heads_with_rows_enough_for_whole_workgroups(heads):
+    lens = [1100, 700, 333, 0, 1]
+    q, k, v = inputs(lens, heads, "bf16", 32, fused=heads[1] == 2)
+    out, lse = spex.prompt_attention(lens, q, k, v, heads[2] ** -0.5)
+    check(lens, q, k, v, out, lse, heads[2] ** -0.5)
