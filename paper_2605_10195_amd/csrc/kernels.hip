@@ -32,8 +32,6 @@
 //       The same element by element, for rows or buffers that are not 16-byte aligned.
 //   spex_append_tokens_kernel
 //       One token for each of many nodes.
-//   spex_append_rotated_kernel / spex_append_rotated_any_kernel (rotated_append.hpp)
-//       Tokens of many nodes, queries and keys turned by their positions on the way.
 //   spex_patch_plan_kernel
 //       Applies {index, value} patches to the device copy of the cached launch lists.
 #include "kernels.hpp"
@@ -2902,8 +2900,6 @@ __global__ __launch_bounds__(256) void spex_append_tokens_kernel(AppendTokensArg
   }
 }
 
-#include "rotated_append.hpp"
-
 template <int KV, int LAYOUT>
 __global__ __launch_bounds__(256) void spex_gather_kv_kernel(GatherArgs a, Shape sh) {
   typedef typename std::conditional<KV == kF32, float,
@@ -3308,66 +3304,6 @@ hipError_t launch_append_tokens(const Shape &sh, const AppendTokensArgs &a, hipS
     case kF32: return append_tokens_layout<kF32, false>(sh, a, stream);
     case kBF16: return append_tokens_layout<kBF16, false>(sh, a, stream);
     case kFP8: return append_tokens_layout<kFP8, false>(sh, a, stream);
-  }
-  return hipErrorInvalidValue;
-}
-
-// DT: head_dim of tiled pools, else 0.
-template <int KV, int DT, bool INTER>
-static void append_rotated_wide(const Shape &sh, const RotateArgs &a, const RotateLists &in, hipStream_t stream) {
-  const dim3 grid(static_cast<unsigned>(a.n_recs), static_cast<unsigned>(a.parts)), block(256);
-  const size_t lds = static_cast<size_t>(a.most_tokens) * (a.rotary_dim / 2) * sizeof(float) * 2;
-  if constexpr (DT > 0)
-    hipLaunchKernelGGL((spex_append_rotated_kernel<KV, DT, INTER>), grid, block, lds, stream, a, sh, in);
-  else
-    hipLaunchKernelGGL((spex_append_rotated_rows_kernel<KV, INTER>), grid, block, lds, stream, a, sh, in);
-}
-template <int KV, int DT>
-static void append_rotated_wide(const Shape &sh, const RotateArgs &a, const RotateLists &in, hipStream_t stream) {
-  if (a.interleaved)
-    append_rotated_wide<KV, DT, true>(sh, a, in, stream);
-  else
-    append_rotated_wide<KV, DT, false>(sh, a, in, stream);
-}
-
-template <int KV>
-static hipError_t append_rotated(const Shape &sh, const RotateArgs &args, const RotateLists &in, hipStream_t stream) {
-  RotateArgs a = args;
-  const bool tiled = sh.layout == kMfmaTiled;
-  const int64_t per16 = KV == kF32 ? 4 : 8;
-  bool wide = sh.D % 8 == 0 && a.rotary_dim % (a.interleaved ? 8 : 16) == 0;
-  for (const void *x : {a.q, a.k, a.v, static_cast<const void *>(a.q_out), static_cast<const void *>(a.k_out),
-                        static_cast<const void *>(a.k_pool), static_cast<const void *>(a.v_pool)})
-    wide = wide && aligned16(x);
-  for (int64_t s : {a.q_stride, a.k_stride, a.v_stride, a.q_out_stride, a.k_out_stride}) wide = wide && s % per16 == 0;
-  if (!wide) {
-    const dim3 grid(static_cast<unsigned>(a.n_recs), static_cast<unsigned>(sh.Hkv)), block(256);
-    a.parts = sh.Hkv;
-    if (tiled)
-      hipLaunchKernelGGL((spex_append_rotated_any_kernel<KV, KV == kF32 ? kRowMajor : kMfmaTiled>), grid, block, 0, stream, a, sh, in);
-    else
-      hipLaunchKernelGGL((spex_append_rotated_any_kernel<KV, kRowMajor>), grid, block, 0, stream, a, sh, in);
-    return hipGetLastError();
-  }
-  // Pages few in number are shared by several workgroups, each with some kv heads, up to as many as the card holds at once (four
-  // a CU).  16 tokens of 8 kv heads: 5.0 us against 7.7 with a workgroup a page; 512 pages of 6 tokens, fp8: 26.3 us with 1024
-  // workgroups, 31.8 with 512, 30.4 with 2048, 35.2 with 4096.
-  a.parts = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(sh.Hkv, 1024 / a.n_recs)));
-  if (KV != kF32 && tiled && sh.D == 64)
-    append_rotated_wide<KV, KV == kF32 ? 0 : 64>(sh, a, in, stream);
-  else if (KV != kF32 && tiled)
-    append_rotated_wide<KV, KV == kF32 ? 0 : 128>(sh, a, in, stream);
-  else
-    append_rotated_wide<KV, 0>(sh, a, in, stream);
-  return hipGetLastError();
-}
-
-hipError_t launch_append_rotated(const Shape &sh, const RotateArgs &a, const RotateLists &in, hipStream_t stream) {
-  if (a.n_recs <= 0) return hipSuccess;
-  switch (sh.kv_dtype) {
-    case kF32: return append_rotated<kF32>(sh, a, in, stream);
-    case kBF16: return append_rotated<kBF16>(sh, a, in, stream);
-    case kFP8: return append_rotated<kFP8>(sh, a, in, stream);
   }
   return hipErrorInvalidValue;
 }

@@ -1,17 +1,91 @@
-// Kernels of spex_tree_append_rotated; part of kernels.hip, whose helpers they use.
+// HIP kernels of spex_tree_append_rotated on gfx950.
 //
 //   spex_append_rotated_kernel
-//       One workgroup per (page that the call writes to, range of kv heads): the cosines and sines of its tokens into LDS,
-//       then queries, keys and values 16 bytes at a time.
+//       Tiled pools.  One workgroup per (page that the call writes to, range of kv heads): the cosines and sines of its tokens into
+//       LDS, then queries, keys and values in jobs of a wavefront.
+//   spex_append_rotated_rows_kernel
+//       Row-major pools: the same, 16 bytes of a row at a time.
 //   spex_append_rotated_any_kernel
 //       The same element by element, for rows, buffers or rotated parts that are not made of 16-byte pieces.
+//
+// Bound: memory.  Runs of prompts move at the rate of a large copy (5 TB/s here): 211 MB of bf16 prompts take 40 us, 1.08 GB into
+// an fp8 cache 254 us (4.3 TB/s, encoding beside it), 92 MB of drafts, six tokens a page, 25 us.  Steps of one token are bound
+// by latency, a launch, the angles, one round of loads and stores: 16 branches of 32/8/128 take 4.9 us, 1024 of 28/4/128 13.5
+// (21 MB, 4 us by bytes; 3 us go to lists read over the bus, 8 to the one round of every workgroup).
 //
 // Mathematics: the pair (x1, x2) number i of a head at position p turns by the angle p * inv_freq[i],
 //   y1 = x1 cos - x2 sin,  y2 = x2 cos + x1 sin.
 // The angle is taken in 64 bits, as turns, so that whole turns can be dropped exactly however far the position; cosine
 // and sine are rounded to fp32, products and sums are fp32 operations rounded one by one, and the result is rounded once to the
 // type it is stored in.
-#pragma once
+#include <algorithm>
+#include <type_traits>
+
+#include "kernels.hpp"
+
+namespace spex {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+__device__ __forceinline__ float bf16_bits_to_float(uint16_t b) {
+  return __builtin_bit_cast(float, static_cast<uint32_t>(b) << 16);
+}
+__device__ __forceinline__ uint16_t half_word(const u32x4 &v, int i) {
+  return static_cast<uint16_t>(v[i >> 1] >> (16 * (i & 1)));
+}
+
+// Where the attention kernels expect token t, dim d of a tile.
+template <int KV, int LAYOUT>
+__device__ __forceinline__ int k_offset(int t, int d, int D) {
+  if (LAYOUT == kRowMajor) return t * D + d;
+  const int tt = 4 * (t >> 3) + (t & 3);
+  if (KV == kFP8)
+    return ((t >> 2) & 1) * 8 * D + (d >> 6) * 512 + ((d & 31) >> 3) * 128 + tt * 16 +
+           ((d >> 5) & 1) * 8 + (d & 7);
+  return ((t >> 2) & 1) * 8 * D + (d >> 5) * 256 + ((d & 31) >> 3) * 64 + tt * 8 + (d & 7);
+}
+template <int KV, int LAYOUT>
+__device__ __forceinline__ int v_offset(int t, int d, int D) {
+  if (LAYOUT == kRowMajor) return t * D + d;
+  if (KV == kFP8)
+    return (d >> 5) * 512 + (t >> 3) * 256 + (d & 15) * 16 + ((d >> 4) & 1) * 8 + (t & 7);
+  return (d >> 4) * 256 + (t >> 3) * 128 + (d & 15) * 8 + (t & 7);
+}
+// Tiled bf16 pools hold V in IEEE half precision, rounded toward zero.
+template <int KV, int LAYOUT>
+__device__ __forceinline__ constexpr bool v_is_f16() {
+  return KV == kBF16 && LAYOUT == kMfmaTiled;
+}
+__device__ __forceinline__ uint16_t bf16_bits_to_f16_bits(uint16_t b) {
+  return static_cast<uint16_t>(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(bf16_bits_to_float(b), 0.f)));
+}
+// fp32 -> e4m3: to nearest even, saturating, NaN kept, by integer arithmetic.
+__device__ __forceinline__ uint32_t encode_e4m3(float y) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, y);
+  const uint32_t sign = (u >> 24) & 0x80u, a = u & 0x7fffffffu;
+  uint32_t code;
+  if (a > 0x7f800000u) {
+    code = 0x7fu;
+  } else if (a >= 0x43e00000u) {  // 448.0f and above (infinity included)
+    code = 0x7eu;
+  } else if (a >= 0x3c800000u) {  // 2^-6
+    const uint32_t r = a + 0x7ffffu + ((a >> 20) & 1u);
+    code = (((r >> 23) - 120u) << 3) | ((r >> 20) & 7u);
+  } else {
+    code = static_cast<uint32_t>(__builtin_rintf(__builtin_bit_cast(float, a) * 512.0f));
+  }
+  return code | sign;
+}
 
 // Cosine and sine of 2 pi p (f.hi + f.lo).  p f.hi is split exactly into its rounded value and the rest; after whole turns and
 // quarter turns at most an eighth of a turn is left, where the Taylor series to the 13th and 14th power are off by less than 3e-14.
@@ -617,3 +691,69 @@ __global__ __launch_bounds__(256) void spex_append_rotated_any_kernel(RotateArgs
     vp[v_offset<KV, LAYOUT>(pv.lo + t, d, D)] = x;
   }
 }
+
+}  // namespace
+
+static bool aligned16(const void *x) { return (reinterpret_cast<uintptr_t>(x) & 15) == 0; }
+
+// DT: head_dim of tiled pools, else 0.
+template <int KV, int DT, bool INTER>
+static void append_rotated_wide(const Shape &sh, const RotateArgs &a, const RotateLists &in, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(a.n_recs), static_cast<unsigned>(a.parts)), block(256);
+  const size_t lds = static_cast<size_t>(a.most_tokens) * (a.rotary_dim / 2) * sizeof(float) * 2;
+  if constexpr (DT > 0)
+    hipLaunchKernelGGL((spex_append_rotated_kernel<KV, DT, INTER>), grid, block, lds, stream, a, sh, in);
+  else
+    hipLaunchKernelGGL((spex_append_rotated_rows_kernel<KV, INTER>), grid, block, lds, stream, a, sh, in);
+}
+template <int KV, int DT>
+static void append_rotated_wide(const Shape &sh, const RotateArgs &a, const RotateLists &in, hipStream_t stream) {
+  if (a.interleaved)
+    append_rotated_wide<KV, DT, true>(sh, a, in, stream);
+  else
+    append_rotated_wide<KV, DT, false>(sh, a, in, stream);
+}
+
+template <int KV>
+static hipError_t append_rotated(const Shape &sh, const RotateArgs &args, const RotateLists &in, hipStream_t stream) {
+  RotateArgs a = args;
+  const bool tiled = sh.layout == kMfmaTiled;
+  const int64_t per16 = KV == kF32 ? 4 : 8;
+  bool wide = sh.D % 8 == 0 && a.rotary_dim % (a.interleaved ? 8 : 16) == 0;
+  for (const void *x : {a.q, a.k, a.v, static_cast<const void *>(a.q_out), static_cast<const void *>(a.k_out),
+                        static_cast<const void *>(a.k_pool), static_cast<const void *>(a.v_pool)})
+    wide = wide && aligned16(x);
+  for (int64_t s : {a.q_stride, a.k_stride, a.v_stride, a.q_out_stride, a.k_out_stride}) wide = wide && s % per16 == 0;
+  if (!wide) {
+    const dim3 grid(static_cast<unsigned>(a.n_recs), static_cast<unsigned>(sh.Hkv)), block(256);
+    a.parts = sh.Hkv;
+    if (tiled)
+      hipLaunchKernelGGL((spex_append_rotated_any_kernel<KV, KV == kF32 ? kRowMajor : kMfmaTiled>), grid, block, 0, stream, a, sh, in);
+    else
+      hipLaunchKernelGGL((spex_append_rotated_any_kernel<KV, kRowMajor>), grid, block, 0, stream, a, sh, in);
+    return hipGetLastError();
+  }
+  // Pages few in number are shared by several workgroups, each with some kv heads, up to as many as the card holds at once (four
+  // a CU).  16 tokens of 8 kv heads: 5.0 us against 7.7 with a workgroup a page; 512 pages of 6 tokens, fp8: 26.3 us with 1024
+  // workgroups, 31.8 with 512, 30.4 with 2048, 35.2 with 4096.
+  a.parts = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(sh.Hkv, 1024 / a.n_recs)));
+  if (KV != kF32 && tiled && sh.D == 64)
+    append_rotated_wide<KV, KV == kF32 ? 0 : 64>(sh, a, in, stream);
+  else if (KV != kF32 && tiled)
+    append_rotated_wide<KV, KV == kF32 ? 0 : 128>(sh, a, in, stream);
+  else
+    append_rotated_wide<KV, 0>(sh, a, in, stream);
+  return hipGetLastError();
+}
+
+hipError_t launch_append_rotated(const Shape &sh, const RotateArgs &a, const RotateLists &in, hipStream_t stream) {
+  if (a.n_recs <= 0) return hipSuccess;
+  switch (sh.kv_dtype) {
+    case kF32: return append_rotated<kF32>(sh, a, in, stream);
+    case kBF16: return append_rotated<kBF16>(sh, a, in, stream);
+    case kFP8: return append_rotated<kFP8>(sh, a, in, stream);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace spex
