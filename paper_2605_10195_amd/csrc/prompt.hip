@@ -118,13 +118,9 @@ __device__ __forceinline__ int swz(int t) {
   return ((t & 3) << 2) | (((t >> 2) & 1) << 1) | ((t >> 3) & 1);
 }
 
-// 64 keys a tile, 32 where a row has 512 bytes: two workgroups then fit into a CU.  8 prompts of 4096, 16/4/192: 1115 us
-// with 64 keys, 825 with 32 (1.0 PFLOP/s); 4 of 4096, 16/4/256: 850 and 611 (0.9).
 template <int DP>
 struct TileB {
-  static constexpr int kKeys = DP <= 128 ? 64 : 32;
   static constexpr int kRowB = DP <= 64 ? 128 : (DP <= 128 ? 256 : 512);
-  static constexpr int kBytes = kKeys * kRowB;
 };
 
 // Copies tiles of KEYS tokens of one head, ROWB bytes a row in LDS, into LDS; Place::at(t, c) is where piece c of row t lies in its
@@ -168,9 +164,12 @@ struct PlaceF {
   static __device__ __forceinline__ int at(int t, int c) { return c ^ (t & 15); }
 };
 
-template <int DP, int NW>
+// KEYS: keys of a tile.  64 means half the barriers, 32 half the LDS: two workgroups then fit into a CU where a row has 512 bytes, three
+// where it has 256.  Rows of 512 bytes always take 32: 8 prompts of 4096, 16/4/192: 1115 us with 64 keys, 825 with 32 (1.0
+// PFLOP/s); 4 of 4096, 16/4/256: 850 and 611 (0.9).  The others: prompt_kernel.
+template <int DP, int KEYS, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void spex_prompt_bf16_kernel(PromptArgs p) {
-  constexpr int ROWB = TileB<DP>::kRowB, TILE = TileB<DP>::kBytes, KS = DP / 16, DT = DP / 32, KEYS = TileB<DP>::kKeys, HALVES = KEYS / 32;
+  constexpr int ROWB = TileB<DP>::kRowB, TILE = KEYS * ROWB, KS = DP / 16, DT = DP / 32, HALVES = KEYS / 32;
   __shared__ __attribute__((aligned(1024))) char lds_[4 * TILE];
   lds_char *lds = (lds_char *)lds_;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
@@ -644,7 +643,7 @@ constexpr int kWaves = 4;
 }  // namespace
 
 PromptKernel prompt_kernel(bool f32, bool wide, int32_t D, int64_t row_sets, int32_t longest) {
-  PromptKernel k{f32, wide, false, wide ? kWaves : 1};
+  PromptKernel k{f32, wide, false, false, wide ? kWaves : 1};
   if (!wide || (f32 && D > 128)) return k;
   // Keys are split over the wavefronts of a workgroup where all row sets run at once that way (by LDS), or where the way of the
   // longest, in units of 32 keys, is shorter by enough: a workgroup has some other work as long as `fixed` units, and keys
@@ -657,6 +656,12 @@ PromptKernel prompt_kernel(bool f32, bool wide, int32_t D, int64_t row_sets, int
   const double units = (longest + 31) / 32, fixed = f32 ? 0.5 : 3.0, shared = f32 ? 1.3 : (D <= 128 ? 1.5 : 1.2);
   k.split = rounds <= 1 || shared * static_cast<double>(rounds) * (units / kWaves + fixed) < units;
   if (k.split) k.sets = 1;
+  // Heads of 97 to 128 dims, tiles of 64 / 32 keys: a third workgroup on a CU pays once there are some rounds of them (3072 row sets
+  // each), and a single round is bound by the way of its longest.  us; 32/8/128, one prompt of 1024 (1024 row sets): 22.4 / 28.0, 2048:
+  // 47.9 / 56.4, 4096 (4096): 150.6 / 149.7; 12/4/128, 12 of 200 .. 1500 (3288): 40.8 / 46.6; 16/4/128, 4 of 2000 (4032): 86.6 / 90.0; 40/8/128,
+  // 4 of 900 (4640): 50.7 / 51.5; 28/4/128, 16 of 512 (7168): 52.9 / 51.9; 64 of 128 .. 1024 (32 thousand): 331 / 307; 64/8/128, 32 of 2048:
+  // 2394 / 2302.  96 dims: 8 of 4096 alike, 12 of 200 .. 1500 34.2 / 40.3; 64 dims: 8 of 4096 345 / 354.
+  k.short_tiles = !f32 && D > 96 && D <= 128 && row_sets > 2 * 3072;
   return k;
 }
 
@@ -668,7 +673,13 @@ int64_t prompt_items(const PromptKernel &k, int32_t heads_per_kv, int32_t len) {
 template <int DP>
 static void (*bf16_kernel(const PromptKernel &k))(PromptArgs) {
   if (k.split) return spex_prompt_split_kernel<false, DP, kWaves>;
-  return spex_prompt_bf16_kernel<DP, kWaves>;
+  if constexpr (DP > 128) {
+    return spex_prompt_bf16_kernel<DP, 32, kWaves>;
+  } else {
+    if constexpr (DP == 128)
+      if (k.short_tiles) return spex_prompt_bf16_kernel<DP, 32, kWaves>;
+    return spex_prompt_bf16_kernel<DP, 64, kWaves>;
+  }
 }
 
 hipError_t launch_prompt(const PromptKernel &k, const PromptArgs &a, int64_t items, hipStream_t stream) {

@@ -28,9 +28,10 @@ struct PromptArgs {
 
 // The kernel for the launches of one call.
 struct PromptKernel {
-  bool f32, wide;  // type; rows of 16-byte pieces (else element by element)
-  bool split;      // a workgroup splits the keys of its rows
-  int32_t sets;    // row sets of kPromptRows rows a work item has
+  bool f32, wide;    // type; rows of 16-byte pieces (else element by element)
+  bool split;        // a workgroup splits the keys of its rows
+  bool short_tiles;  // tiles of 32 keys instead of 64
+  int32_t sets;      // row sets of kPromptRows rows a work item has
 };
 // row_sets: of all prompts and query heads; longest: tokens of the longest prompt
 PromptKernel prompt_kernel(bool f32, bool wide, int32_t head_dim, int64_t row_sets, int32_t longest);

@@ -265,3 +265,14 @@ def test_wide_heads_with_rows_enough_for_whole_workgroups(heads):
     q, k, v = inputs(lens, heads, "bf16", 32, fused=heads[1] == 2)
     out, lse = spex.prompt_attention(lens, q, k, v, heads[2] ** -0.5)
     check(lens, q, k, v, out, lse, heads[2] ** -0.5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [(128, 8, 128), (130, 2, 104)], ids=str)
+def test_batches_of_many_row_sets(heads):
+    """More than 6144 sets of 32 rows."""
+    lens = [65, 1, 700, 257, 64, 33, 0, 500, 31, 96]
+    q, k, v = inputs(lens, heads, "bf16", 33, fused=heads[1] == 8)
+    assert heads[0] * sum(-(-n // 32) for n in lens) > 6144
+    out, lse = spex.prompt_attention(lens, q, k, v, heads[2] ** -0.5)
+    check(lens, q, k, v, out, lse, heads[2] ** -0.5)
