@@ -21,7 +21,7 @@
 // Bound: the matrix cores, and with them power (at 1.0 PFLOP/s the clock falls from 2.4 to 1.75 GHz; on zeros the same launch is a
 // third faster).  bf16, 8 prompts of 4096 tokens: D 64 0.82 PFLOP/s (the exponentials take a larger share), 96 0.87, 128 1.04, 192 1.0,
 // 256 (4 prompts) 0.9; one of 16000, 32/8/128: 1.1; a bf16 matrix product of 16384 reaches 1.35.  Prompts below 1000 tokens are bound by
-// the first loads and last stores of their workgroups: 64 of 128 .. 1024 tokens, 28/4/128: 318 us, 16 of 1024: 0.8 PFLOP/s.  fp32:
+// the first loads and last stores of their workgroups: 64 of 128 .. 1024 tokens, 28/4/128: 307 us, 16 of 1024: 0.8 PFLOP/s.  fp32:
 // 105 TFLOP/s at D 128 (matrix product: 154).  One prompt of a few hundred tokens: 10 us, launch and latency.
 #include "prompt.hpp"
 
