@@ -244,7 +244,7 @@ typedef struct {
  *   positions : HOST [sum(counts)], >= 0, or NULL: a token's position is the number of tokens before it on its path.  To be given
  *     where the two differ, as for the drafts of a token tree, whose position is their depth
  * fp8 pools are quantised on the way, from the rotated keys in fp32: code = e4m3fn(x * (1 / scale)), round to nearest even,
- * saturating.  A page the call starts takes its row of k_scales / v_scales (pages in the order of the nodes, within a node in token
+ * saturating; k and v must be finite there.  A page the call starts takes its row of k_scales / v_scales (pages in the order of the nodes, within a node in token
  * order) if they are given, and else scale = max(amax / 448, 2^-40) over the tokens the call puts into it, as
  * spex_tree_append_step_quantize; other pages keep the scale they have.
  * All or nothing, page order, structure version and patches of the cached launch lists as spex_tree_append_tokens; like it,

@@ -364,6 +364,7 @@ class SpexTree:
         want, device = torch.float32 if self.kv_dtype == F32 else torch.bfloat16, _device()
         assert ca is None or len(ca) == len(na)
         assert pa is None or pa.shape == (total,)
+        assert self.k_pool is None or self.k_pool.get_device() == device, "the tree's pools must lie on the current device"
         d = Rotated()
         d.k, d.k_stride = k.data_ptr(), _token_stride(k, total, self.Hkv, self.D, want, device)
         d.v, d.v_stride = v.data_ptr(), _token_stride(v, total, self.Hkv, self.D, want, device)

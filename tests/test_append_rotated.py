@@ -513,3 +513,17 @@ def test_page_scales_behind_two_to_the_31(head_dim):
         # as in test_page_scales_computed_and_given
         assert bool(((s.double().cpu() - want).abs() <= 8 * 2.0 ** -24 * want * 1.5).all())
     t.close()
+
+
+@pytest.mark.gpu
+def test_pools_on_another_device_are_refused():
+    t = tree_of((4, 2, 64), 16, "bf16", 4, 64, False)
+    (u,) = t.fork(-1, 1)
+    q, k, v = draw(1, (4, 2, 64), "bf16", 14)
+    here, t.k_pool = t.k_pool, torch.empty(4)
+    with pytest.raises(AssertionError, match="pools"):
+        t.append_rotated([u], None, q, k, v)
+    assert t.node_info(u)["n_tokens"] == 0
+    t.k_pool = here
+    t.append_rotated([u], None, q, k, v)
+    t.close()
