@@ -656,12 +656,12 @@ PromptKernel prompt_kernel(bool f32, bool wide, int32_t D, int64_t row_sets, int
   const double units = (longest + 31) / 32, fixed = f32 ? 0.5 : 3.0, shared = f32 ? 1.3 : (D <= 128 ? 1.5 : 1.2);
   k.split = rounds <= 1 || shared * static_cast<double>(rounds) * (units / kWaves + fixed) < units;
   if (k.split) k.sets = 1;
-  // Heads of 97 to 128 dims, tiles of 64 / 32 keys: a third workgroup on a CU pays once there are some rounds of them (3072 row sets
-  // each), and a single round is bound by the way of its longest.  us; 32/8/128, one prompt of 1024 (1024 row sets): 22.4 / 28.0, 2048:
+  // Heads of 97 to 128 dims, tiles of 64 / 32 keys: a third workgroup on a CU pays once there are some rounds of them, and a single
+  // round is bound by the way of its longest.  us; 32/8/128, one prompt of 1024 (1024 row sets): 22.4 / 28.0, 2048:
   // 47.9 / 56.4, 4096 (4096): 150.6 / 149.7; 12/4/128, 12 of 200 .. 1500 (3288): 40.8 / 46.6; 16/4/128, 4 of 2000 (4032): 86.6 / 90.0; 40/8/128,
   // 4 of 900 (4640): 50.7 / 51.5; 28/4/128, 16 of 512 (7168): 52.9 / 51.9; 64 of 128 .. 1024 (32 thousand): 331 / 307; 64/8/128, 32 of 2048:
   // 2394 / 2302.  96 dims: 8 of 4096 alike, 12 of 200 .. 1500 34.2 / 40.3; 64 dims: 8 of 4096 345 / 354.
-  k.short_tiles = !f32 && D > 96 && D <= 128 && row_sets > 2 * 3072;
+  k.short_tiles = !f32 && D > 96 && D <= 128 && row_sets > 2 * (3 * 256 * kWaves);
   return k;
 }
 
