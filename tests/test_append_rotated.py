@@ -2,6 +2,9 @@
 against the definition in 64 bits."""
 
 import ctypes as C
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -527,3 +530,25 @@ def test_pools_on_another_device_are_refused():
     t.k_pool = here
     t.append_rotated([u], None, q, k, v)
     t.close()
+
+
+def test_lists_of_a_launch_under_sanitizers(tmp_path):
+    """Random trees, nodes and counts with the HIP runtime and the launches replaced by the test's own: every launch has each token once, in
+    its slot and at its position, and its patches lie in the plan."""
+    include = "/opt/rocm/include"
+    if shutil.which("g++") is None or not os.path.exists(os.path.join(include, "hip", "hip_runtime.h")):
+        pytest.skip("needs g++ and the HIP headers")
+    here = os.path.dirname(os.path.abspath(__file__))
+    csrc = os.path.join(here, "..", "paper_2605_10195_amd", "csrc")
+    exe = str(tmp_path / "rotated_lists")
+    build = subprocess.run(
+        ["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-static-libasan", "-static-libubsan",
+         "-D__HIP_PLATFORM_AMD__", "-I" + include, "-D__align__(n)=__attribute__((aligned(n)))", "-DHIP_SYMBOL(x)=(&x)",
+         os.path.join(here, "rotated_lists.cpp")] +
+        [os.path.join(csrc, f) for f in ("api.cpp", "rotated_append.cpp", "planner.cpp", "page_table.cpp", "sched.cpp")] + ["-o", exe],
+        capture_output=True, text=True)
+    if build.returncode != 0 and "cannot find" in build.stderr and any(w in build.stderr for w in ("asan", "ubsan", "sanitize")):
+        pytest.skip("the sanitizer runtime is not installed")
+    assert build.returncode == 0, build.stderr[-2000:]
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=600)
+    assert run.returncode == 0 and run.stdout == "ok\n", (run.stdout[-2000:], run.stderr[-4000:])
