@@ -643,19 +643,25 @@ constexpr int kWaves = 4;
 }  // namespace
 
 PromptKernel prompt_kernel(bool f32, bool wide, int32_t D, int64_t row_sets, int32_t longest) {
-  PromptKernel k{f32, wide, false, false, wide ? kWaves : 1};
+  PromptKernel k{f32, wide, false, false, false, wide ? kWaves : 1};
   if (!wide || (f32 && D > 128)) return k;
   // Keys are split over the wavefronts of a workgroup where all row sets run at once that way (by LDS), or where the way of the
   // longest, in units of 32 keys, is shorter by enough: a workgroup has some other work as long as `fixed` units, and keys
   // and values are then not shared by four row sets.  us, whole / split; heads 32/8/128, one prompt of 1: 4.9 / 4.1, 256: 8.6 / 6.8,
   // 512 (512 row sets): 13.0 / 9.9, 768: 17.7 / 18.0, 1024: 22.2 / 23.1, 2048: 45.9 / 61.3; 8/2/128, 2048: 37.4 / 21.9, 4096 (1024):
   // 70.7 / 57.7, 8192: 164 / 194; 8 of 128, 32/8/128 (1024): 7.3 / 12.1; 16/2/64, 2048 (1024): 32.7 / 20.3; 16/4/256, 512 (256): 27.4 / 17.0,
-  // 1024 (512): 49 / 34, 1500 (752): 68 / 65, 2048 (1024): 93 / 100, 16/4/192, 1500 (752): 44 / 54; fp32 8/2/64, 256: 23.1 / 9.1, 32/8/128, 256 (256): 38.7 / 15.8, 512: 71.7 / 34.3, 32 of 64 (2048): 29 / 67.
+  // 1024 (512): 49 / 34, 1500 (752): 68 / 65, 2048 (1024): 93 / 100, 16/4/192, 1500 (752): 44 / 54; fp32 8/2/64, 256: 23.1 / 9.1,
+  // 32/8/128, 256 (256): 38.7 / 15.8, 512: 71.7 / 34.3, 32 of 64 (2048): 29 / 67.
   const int32_t row_b = f32 ? (D <= 64 ? 256 : 512) : (D <= 64 ? 128 : (D <= 128 ? 256 : 512));
   const int64_t at_once = 256 * (512 / row_b), rounds = (row_sets + at_once - 1) / at_once;
   const double units = (longest + 31) / 32, fixed = f32 ? 0.5 : 3.0, shared = f32 ? 1.3 : (D <= 128 ? 1.5 : 1.2);
   k.split = rounds <= 1 || shared * static_cast<double>(rounds) * (units / kWaves + fixed) < units;
   if (k.split) k.sets = 1;
+  // Eight wavefronts where their LDS (128 KB where a row has 256 bytes) still holds all row sets at once and the longest has more units than
+  // four of them take in one go, two of a bf16 head of more than 96 dims, where joining eight states costs more.  us, four / eight:
+  // 8/2/128, 256: 6.3 / 6.5, 512: 8.4 / 7.9, 1024: 12.3 / 10.7; 4/2/96, 2048: 19.4 / 14.7; 16/2/64, 256: 5.0 / 4.7, 1024: 10.1 / 9.2; 4 of 200, 8/2/128:
+  // 6.5 / 6.6; fp32 8/2/64, 160: 8.9 / 8.5, 256: 9.2 / 8.9, 1024: 25.3 / 22.8.
+  k.eight = k.split && row_b <= 256 && row_sets <= 256 * (256 / row_b) && longest > (f32 || D <= 96 ? 1 : 2) * 32 * kWaves;
   // Heads of 97 to 128 dims, tiles of 64 / 32 keys: a third workgroup on a CU pays once there are some rounds of them, and a single
   // round is bound by the way of its longest.  us; 32/8/128, one prompt of 1024 (1024 row sets): 22.4 / 28.0, 2048:
   // 47.9 / 56.4, 4096 (4096): 150.6 / 149.7; 12/4/128, 12 of 200 .. 1500 (3288): 40.8 / 46.6; 16/4/128, 4 of 2000 (4032): 86.6 / 90.0; 40/8/128,
@@ -672,6 +678,8 @@ int64_t prompt_items(const PromptKernel &k, int32_t heads_per_kv, int32_t len) {
 
 template <int DP>
 static void (*bf16_kernel(const PromptKernel &k))(PromptArgs) {
+  if constexpr (DP <= 128)
+    if (k.eight) return spex_prompt_split_kernel<false, DP, 2 * kWaves>;
   if (k.split) return spex_prompt_split_kernel<false, DP, kWaves>;
   if constexpr (DP > 128) {
     return spex_prompt_bf16_kernel<DP, 32, kWaves>;
@@ -687,13 +695,15 @@ hipError_t launch_prompt(const PromptKernel &k, const PromptArgs &a, int64_t ite
   void (*kernel)(PromptArgs) = nullptr;
   if (!k.wide)
     kernel = k.f32 ? spex_prompt_generic_kernel<true> : spex_prompt_generic_kernel<false>;
+  else if (k.f32 && k.eight)
+    kernel = spex_prompt_split_kernel<true, 64, 2 * kWaves>;
   else if (k.f32 && k.split)
     kernel = a.D <= 64 ? spex_prompt_split_kernel<true, 64, kWaves> : spex_prompt_split_kernel<true, 128, kWaves>;
   else if (k.f32)
     kernel = a.D <= 64 ? spex_prompt_f32_kernel<64, kWaves> : (a.D <= 128 ? spex_prompt_f32_kernel<128, kWaves> : spex_prompt_f32_kernel<256, kWaves>);
   else
     kernel = a.D <= 64 ? bf16_kernel<64>(k) : (a.D <= 96 ? bf16_kernel<96>(k) : (a.D <= 128 ? bf16_kernel<128>(k) : (a.D <= 192 ? bf16_kernel<192>(k) : bf16_kernel<256>(k))));
-  hipLaunchKernelGGL(kernel, grid, dim3(k.wide ? 64 * kWaves : 64), 0, stream, a);
+  hipLaunchKernelGGL(kernel, grid, dim3(k.wide ? (k.eight ? 128 * kWaves : 64 * kWaves) : 64), 0, stream, a);
   return hipGetLastError();
 }
 

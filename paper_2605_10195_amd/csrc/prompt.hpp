@@ -29,7 +29,8 @@ struct PromptArgs {
 // The kernel for the launches of one call.
 struct PromptKernel {
   bool f32, wide;    // type; rows of 16-byte pieces (else element by element)
-  bool split;        // a workgroup splits the keys of its rows
+  bool split;        // a workgroup splits the keys of its rows over its wavefronts
+  bool eight;        // eight of them instead of four
   bool short_tiles;  // tiles of 32 keys instead of 64
   int32_t sets;      // row sets of kPromptRows rows a work item has
 };

@@ -276,3 +276,13 @@ def test_batches_of_many_row_sets(heads):
     assert heads[0] * sum(-(-n // 32) for n in lens) > 6144
     out, lse = spex.prompt_attention(lens, q, k, v, heads[2] ** -0.5)
     check(lens, q, k, v, out, lse, heads[2] ** -0.5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,lens", [((8, 2, 128), [1024]), ((4, 2, 96), [2048]), ((2, 1, 64), [129, 7, 1700]), ((8, 2, 40), [255, 0, 257]), ((1, 1, 128), [289])], ids=str)
+def test_few_rows_with_long_ways(dtype, heads, lens):
+    """Row sets few enough to share each over eight wavefronts, or four (fp32 above 64 dims)."""
+    q, k, v = inputs(lens, heads, dtype, 34)
+    out, lse = spex.prompt_attention(lens, q, k, v, heads[2] ** -0.5)
+    check(lens, q, k, v, out, lse, heads[2] ** -0.5)
