@@ -218,8 +218,8 @@ spex_status_t spex_tree_append_new_pages(const spex_tree_t *tree, spex_node_t no
  *   inv_freq : HOST [rotary_dim / 2], the f_i in radians a position (finite), copied; a scaled variant of the rotation is its
  *     frequencies
  *   rotary_dim : even, 2 .. head_dim; 0 (inv_freq then NULL) takes the setting away
- * The angle is evaluated in 64 bits with whole turns dropped exactly, cosine and sine are rounded to fp32, each product and sum
- * is rounded to fp32, and y is rounded once to the type it is stored in.  Host only; calls already made keep their setting.
+ * The angle is evaluated in 64 bits, to 2^-64 of p f_i before its whole turns are dropped, cosine and sine are rounded to fp32, each
+ * product and sum is rounded to fp32, and y is rounded once to the type it is stored in.  Host only; calls already made keep their setting.
  */
 spex_status_t spex_tree_set_rotation(spex_tree_t *tree, int32_t rotary_dim, const double *inv_freq, int32_t interleaved);
 

@@ -5,6 +5,7 @@ import ctypes as C
 import os
 import shutil
 import subprocess
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -306,6 +307,34 @@ def test_positions_given_and_far(kv, rotary, interleaved):
     for got, x in ((q_out, q), (k_out, k)):
         for i, row in enumerate(turns):                           # a rotation by `turns` at position 1
             assert_rotated(got[i:i + 1], x[i:i + 1], [1.0], 2 * np.pi * row, rotary, interleaved, int(pos[i]))
+    t.close()
+
+
+def turns_of(pos, freq):
+    """pos * freq / (2 pi) less its whole turns, exactly but for one rounding at the end; pi to 60 digits."""
+    two_pi = 2 * Fraction(314159265358979323846264338327950288419716939937510582097494, 10 ** 59)
+    return np.array([[float((int(p) * Fraction(float(f)) / two_pi + Fraction(1, 2)) % 1 - Fraction(1, 2)) for f in freq] for p in pos])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("base", [1e4, 1e6])
+def test_ordinary_frequencies_at_far_positions(base, shift):
+    """Cosines and sines themselves, as the rotation of (1, 0): 1 * cos - 0 * sin and 0 * cos + 1 * sin are exact, so a result is
+    off by half a step of fp32 (2^-25 of at most 1), and by the angle's error: the turns of a position are known to 2^-64 of them, 2^-35 at
+    positions below 2^31 and frequencies of at most 1, that is 2^-32 in radians, and the series to 3e-14."""
+    heads, rotary = (1, 1, 128), 128
+    t = tree_of(heads, 16, "f32", 20, rotary, False, FREQ(rotary, base))
+    (u,) = t.fork(-1, 1)
+    rng = np.random.default_rng(1)
+    pos = np.concatenate([rng.integers(1 << e, (1 << e) + (1 << e - 1), 4) for e in (20, 24, 26, 28, 29, 30)] + [[(1 << 31) - 1]]).astype(np.int32)
+    q, k, v = draw(len(pos), heads, "f32", 15, shift)
+    q[..., :64], q[..., 64:] = 1.0, 0.0
+    q_out, _ = t.append_rotated([u], [len(pos)], q, k, v, positions=pos)
+    angle = 2 * np.pi * turns_of(pos, FREQ(rotary, base))
+    got = q_out.double().cpu().numpy()[:, 0]
+    off = np.maximum(np.abs(got[:, :64] - np.cos(angle)), np.abs(got[:, 64:] - np.sin(angle))).max(1)
+    assert off.max() <= 2.0 ** -25 + 2.0 ** -32 + 1e-13, dict(zip(pos.tolist(), (off * 2 ** 25).tolist()))
     t.close()
 
 
