@@ -46,7 +46,8 @@ typedef struct {
  *   lse  : DEVICE fp32 [sum(lens)][num_q_heads] or NULL:  ln sum_s exp(sm_scale * <q_t, k_s>)
  * q, k and v must be finite, and so must the scores <q_t, k_s> in fp32 and, times sm_scale, stay within +-1e30; sm_scale in
  * 1e-38 .. 1e37 (else SPEX_ERR_INVALID_ARG).  out must not overlap q, k or v.  Nothing outside
- * the prompts' rows is read or written.  Scores, softmax statistics and sums are fp32; for bf16 the
+ * the prompts' rows is read or written.  Scores, softmax statistics and sums are fp32 (a weight's exponent is a difference of
+ * scores, also where the scores are so large that fp32 rounds their scaled values to many units); for bf16 the
  * softmax weights are rounded to bf16 (to nearest) for their product with v, so that an output is within
  * 2^-8 of the weighted mean of |v| besides its own rounding.
  * Rows whose address, stride or head_dim is no multiple of 16 bytes take a slower kernel.

@@ -45,14 +45,37 @@ typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
 typedef __attribute__((address_space(3))) float lds_float;
 
-// Start value of the running maximum: finite, and below any score that the rows can have.
-constexpr float kMInit = -1.0e30f;
+// Start value of the running maximum: finite, and far below any scaled score (+-1e30 log2(e)) that the rows can have.
+constexpr float kMInit = -3.0e38f;
 // A row's reference m stays while its scores are below m + 8: weights reach 2^8, sums stay far inside fp32, and the
 // accumulators are rescaled a few times a row instead of once a tile.
 constexpr float kSlack = 8.0f;
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The reference point of a row: its weights are 2^((s - base) scale_log2 - m).  A row near zero has base 0, so that a weight is one fma and
+// one exponential; the key that set m then has the weight 2^(what rounding the product to m left), not 1, which is of no account as long as that
+// is a few units.  Rows whose |m| reaches kFar -- where fp32 holds no fractions, and from 2^31 on no unit below 128 -- have m 0
+// and the score itself as base, subtracted from the scores of every tile before they are scaled.
+constexpr float kFar = 16777216.0f;
+struct Reference {
+  float m = kMInit, base = 0.f;
+  // Moves it up to `top`, the row's largest score of a tile (at least once before the first weight); the factor of the weights so far.
+  __device__ __forceinline__ float move(float top, float scale) {
+    const float ref = base != 0.f ? fmaxf(base, top) : top, scaled = ref * scale;
+    const float mn = base != 0.f ? scaled : fmaxf(m, scaled);
+    const bool far = __builtin_fabsf(mn) >= kFar;  // mn is then that of ref
+    const float new_base = far ? ref : 0.f, new_m = far ? 0.f : mn;
+    const float f = fast_exp2(__builtin_fmaf(base - new_base, scale, m - new_m));
+    base = new_base;
+    m = new_m;
+    return f;
+  }
+  __device__ __forceinline__ bool far() const { return base != 0.f; }
+  // In log2 units.
+  __device__ __forceinline__ float value(float scale) const { return __builtin_fmaf(base, scale, m); }
+};
 
 // The value of lane l ^ 32.
 __device__ __forceinline__ float other_half(float v) {
@@ -227,7 +250,8 @@ __global__ __launch_bounds__(64 * NW, 2) void spex_prompt_bf16_kernel(PromptArgs
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
-  float m = kMInit, l = 0.f, limit = -__builtin_huge_valf();  // limit: scores up to here need no other reference point
+  Reference ref;
+  float l = 0.f, limit = -__builtin_huge_valf();  // limit: scores up to here need no other reference point, of a far row none
   const float inv_scale = 1.0f / p.scale_log2;
   const int qpos = rs.q0 + col;
 
@@ -262,20 +286,23 @@ __global__ __launch_bounds__(64 * NW, 2) void spex_prompt_bf16_kernel(PromptArgs
 #pragma unroll
     for (int r = 1; r < KEYS / 2; ++r) mx = fmaxf(mx, s[r / 16][r % 16]);
     if (__any(mx > limit)) {
-      const float mn = fmaxf(m, fmaxf(mx, other_half(mx)) * p.scale_log2), f = fast_exp2(m - mn);
-      m = mn;
-      limit = (m + kSlack) * inv_scale;
+      const float f = ref.move(fmaxf(mx, other_half(mx)), p.scale_log2);
+      limit = ref.far() ? -__builtin_huge_valf() : (ref.m + kSlack) * inv_scale;
       l *= f;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] *= f;
+      if (__any(ref.far())) {
+#pragma unroll
+        for (int r = 0; r < KEYS / 2; ++r) s[r / 16][r % 16] -= ref.base;
+      }
     }
     uint32_t pw[KEYS / 4];
 #pragma unroll
     for (int r = 0; r < KEYS / 2; r += 2) {
-      const float a = fast_exp2(__builtin_fmaf(s[r / 16][r % 16], p.scale_log2, -m));
-      const float b = fast_exp2(__builtin_fmaf(s[r / 16][r % 16 + 1], p.scale_log2, -m));
+      const float a = fast_exp2(__builtin_fmaf(s[r / 16][r % 16], p.scale_log2, -ref.m));
+      const float b = fast_exp2(__builtin_fmaf(s[r / 16][r % 16 + 1], p.scale_log2, -ref.m));
       l += a + b;
       pw[r / 2] = pack_bf16(a, b);
     }
@@ -311,7 +338,7 @@ __global__ __launch_bounds__(64 * NW, 2) void spex_prompt_bf16_kernel(PromptArgs
     if (rs.q0 + r < rs.len && c < pieces) *reinterpret_cast<u32x4 *>(out + r * p.out_stride * 2 + c * 16) = x;
   }
   if (p.lse && h == 0 && qpos < rs.len)
-    p.lse[(row + col) * (static_cast<int64_t>(p.Hkv) * p.G) + rs.head] = (m + __builtin_log2f(l)) * 0.6931471805599453f;
+    p.lse[(row + col) * (static_cast<int64_t>(p.Hkv) * p.G) + rs.head] = (ref.value(p.scale_log2) + __builtin_log2f(l)) * 0.6931471805599453f;
 }
 
 // ---- fp32 ----------------------------------------------------------------------------------------
@@ -350,7 +377,8 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_f32_ke
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
-  float m = kMInit, l = 0.f;
+  Reference ref;
+  float l = 0.f;
   const int qpos = rs.q0 + col;
   for (int t = 0; t < tiles; ++t) {
     tile_barrier();
@@ -378,19 +406,22 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_f32_ke
     float mx = s[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-    mx = fmaxf(mx, other_half(mx)) * p.scale_log2;
-    if (__any(mx > m + kSlack)) {
-      const float mn = fmaxf(m, mx), f = fast_exp2(m - mn);
-      m = mn;
+    mx = fmaxf(mx, other_half(mx));
+    if (__any(mx * p.scale_log2 > ref.m + kSlack || ref.far())) {
+      const float f = ref.move(mx, p.scale_log2);
       l *= f;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] *= f;
+      if (__any(ref.far())) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] -= ref.base;
+      }
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      s[r] = fast_exp2(__builtin_fmaf(s[r], p.scale_log2, -m));
+      s[r] = fast_exp2(__builtin_fmaf(s[r], p.scale_log2, -ref.m));
       l += s[r];
     }
 #pragma unroll
@@ -415,13 +446,13 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void spex_prompt_f32_ke
       if (d < p.D)
         *reinterpret_cast<f32x4 *>(out + d) = f32x4{o[dt][4 * j] * inv, o[dt][4 * j + 1] * inv, o[dt][4 * j + 2] * inv, o[dt][4 * j + 3] * inv};
     }
-  if (p.lse && h == 0) p.lse[row * (static_cast<int64_t>(p.Hkv) * p.G) + rs.head] = (m + __builtin_log2f(l)) * 0.6931471805599453f;
+  if (p.lse && h == 0) p.lse[row * (static_cast<int64_t>(p.Hkv) * p.G) + rs.head] = (ref.value(p.scale_log2) + __builtin_log2f(l)) * 0.6931471805599453f;
 }
 
 // ---- few rows ------------------------------------------------------------------------------------
 // A workgroup takes 32 rows of one query head; wavefront w units w, w + NW, .. of 32 keys, which it copies into LDS of its own and
 // waits for alone.  In the end the wavefronts' states go through LDS: with M the largest m of a row,
-// l = sum_w l_w 2^(m_w - M), out = sum_w O_w 2^(m_w - M) / l.
+// l = sum_w l_w 2^(m_w - M), out = sum_w O_w 2^(m_w - M) / l.  Where M is far from zero the differences are those of the scores themselves.
 // What bounds such launches is the way of the longest row set from launch to store; its keys are worked on NW at a time here.
 template <bool F32, int DP, int NW>
 __global__ __launch_bounds__(64 * NW, 2 * NW * 32 * (F32 ? DP * 4 : TileB<DP>::kRowB) <= 65536 ? 2 : 1) void spex_prompt_split_kernel(PromptArgs p) {
@@ -432,7 +463,7 @@ __global__ __launch_bounds__(64 * NW, 2 * NW * 32 * (F32 ? DP * 4 : TileB<DP>::k
   constexpr int PER = DP / 4;                 // pieces of four dims of a row of results
   static_assert(32 * DP * 4 <= 2 * UNIT, "a wavefront's results fit its own LDS");
   __shared__ __attribute__((aligned(1024))) char lds_[2 * NW * UNIT];
-  __shared__ float ml[NW][2][32];
+  __shared__ float ml[NW][3][32];  // value and sum of a row, and its base where far
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
   lds_char *const kt = (lds_char *)lds_ + wave * (2 * UNIT), *const vt = kt + UNIT;
   const RowSet rs = row_set<1>(p, 0);
@@ -459,7 +490,8 @@ __global__ __launch_bounds__(64 * NW, 2 * NW * 32 * (F32 ? DP * 4 : TileB<DP>::k
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
-  float m = kMInit, l = 0.f;
+  Reference ref;
+  float l = 0.f;
   if (wave < units) {
     // the queries by way of the room for values
     Stager<32, ROWB, 1, Place> qs(static_cast<const char *>(p.q) + (row * p.q_stride + head0) * ESZ, p.q_stride * ESZ, rs.len - rs.q0, p.D * ESZ, 0, lane);
@@ -500,21 +532,24 @@ __global__ __launch_bounds__(64 * NW, 2 * NW * 32 * (F32 ? DP * 4 : TileB<DP>::k
       float mx = s[0];
 #pragma unroll
       for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-      const float mn = fmaxf(m, fmaxf(mx, other_half(mx)) * p.scale_log2);
+      mx = fmaxf(mx, other_half(mx));
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the keys have been read
       if (more) ks.next(kt);
-      if (__any(mn > m)) {
-        const float f = fast_exp2(m - mn);
-        m = mn;
+      if (__any(mx * p.scale_log2 > ref.m || ref.far())) {
+        const float f = ref.move(mx, p.scale_log2);
         l *= f;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[dt][r] *= f;
+        if (__any(ref.far())) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] -= ref.base;
+        }
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        s[r] = fast_exp2(__builtin_fmaf(s[r], p.scale_log2, -m));
+        s[r] = fast_exp2(__builtin_fmaf(s[r], p.scale_log2, -ref.m));
         l += s[r];
       }
       if (more)
@@ -547,8 +582,9 @@ __global__ __launch_bounds__(64 * NW, 2 * NW * 32 * (F32 ? DP * 4 : TileB<DP>::k
   }
   // Results into this wavefront's LDS: piece c of row r at place c ^ (r & 7), so that rows do not fall on the same banks.
   if (h == 0) {
-    ml[wave][0][col] = m;
+    ml[wave][0][col] = ref.value(p.scale_log2);
     ml[wave][1][col] = l;
+    ml[wave][2][col] = wave < units ? ref.base : -__FLT_MAX__;
   }
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
@@ -562,11 +598,19 @@ __global__ __launch_bounds__(64 * NW, 2 * NW * 32 * (F32 ? DP * 4 : TileB<DP>::k
     float top = kMInit;
 #pragma unroll
     for (int w = 0; w < NW; ++w) top = fmaxf(top, ml[w][0][r]);
+    const bool far = __builtin_fabsf(top) >= kFar;
+    float base = -__FLT_MAX__;  // the largest of the far rows'
+    if (far) {
+#pragma unroll
+      for (int w = 0; w < NW; ++w) base = fmaxf(base, ml[w][2][r]);
+    }
     float sum = 0.f;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const float f = fast_exp2(ml[w][0][r] - top);
+      float x2 = ml[w][0][r] - top;
+      if (far) x2 = ml[w][2][r] != 0.f ? (ml[w][2][r] - base) * p.scale_log2 : __builtin_fmaf(-base, p.scale_log2, ml[w][0][r]);
+      const float f = fast_exp2(x2);
       sum += ml[w][1][r] * f;
       const f32x4 y = *(const __attribute__((address_space(3))) f32x4 *)((const lds_char *)lds_ + w * (2 * UNIT) + r * (DP * 4) + (c ^ (r & 7)) * 16);
 #pragma unroll
@@ -600,16 +644,16 @@ __global__ __launch_bounds__(64) void spex_prompt_generic_kernel(PromptArgs p) {
     if (qpos >= rs.len) return;
     const int64_t q = (rs.row0 + qpos) * p.q_stride + static_cast<int64_t>(rs.head) * D, k = rs.row0 * p.k_stride + rs.kv * D,
                   v = rs.row0 * p.v_stride + rs.kv * D;
-    float m = kMInit, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    float m = -__FLT_MAX__, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};  // m: as a score, not scaled
     for (int t0 = 0; t0 <= qpos; t0 += 64) {
       const int t = min(t0 + lane, qpos);
       float x = 0.f;
       for (int d = 0; d < D; ++d) x = __builtin_fmaf(load<F32>(p.q, q + d), load<F32>(p.k, k + t * p.k_stride + d), x);
-      x = t0 + lane <= qpos ? x * p.scale_log2 : -__builtin_huge_valf();
+      if (t0 + lane > qpos) x = -__builtin_huge_valf();
       float mx = x;
 #pragma unroll
       for (int w = 32; w >= 1; w >>= 1) mx = fmaxf(mx, __shfl_xor(mx, w));
-      const float mn = fmaxf(m, mx), f = fast_exp2(m - mn), w = fast_exp2(x - mn);
+      const float mn = fmaxf(m, mx), f = fast_exp2((m - mn) * p.scale_log2), w = fast_exp2((x - mn) * p.scale_log2);
       m = mn;
       l = l * f + w;
 #pragma unroll
@@ -634,7 +678,7 @@ __global__ __launch_bounds__(64) void spex_prompt_generic_kernel(PromptArgs p) {
       else
         static_cast<__bf16 *>(p.out)[out + d] = static_cast<__bf16>(o[c] / l);
     }
-    if (p.lse && lane == 0) p.lse[row * (static_cast<int64_t>(p.Hkv) * p.G) + rs.head] = (m + __builtin_log2f(l)) * 0.6931471805599453f;
+    if (p.lse && lane == 0) p.lse[row * (static_cast<int64_t>(p.Hkv) * p.G) + rs.head] = __builtin_fmaf(m, p.scale_log2, __builtin_log2f(l)) * 0.6931471805599453f;
   }
 }
 

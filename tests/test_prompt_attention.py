@@ -286,3 +286,68 @@ def test_few_rows_with_long_ways(dtype, heads, lens):
     q, k, v = inputs(lens, heads, dtype, 34)
     out, lse = spex.prompt_attention(lens, q, k, v, heads[2] ** -0.5)
     check(lens, q, k, v, out, lse, heads[2] ** -0.5)
+
+
+# ---- every kernel ------------------------------------------------------------------------------
+# Heads whose calls with a prompt of some 400 tokens take each of the kernels.
+KERNELS = [("bf16", (96, 2, 64)), ("bf16", (60, 3, 96)), ("bf16", (64, 4, 128)), ("bf16", (480, 2, 128)),
+           ("bf16", (40, 4, 192)), ("bf16", (40, 2, 256)), ("f32", (96, 2, 64)), ("f32", (60, 3, 128)),
+           ("f32", (4, 2, 256)), ("bf16", (64, 2, 64)), ("bf16", (24, 2, 96)), ("bf16", (24, 4, 128)),
+           ("bf16", (16, 2, 192)), ("bf16", (8, 2, 256)), ("f32", (32, 2, 64)), ("f32", (8, 1, 128)),
+           ("bf16", (16, 2, 64)), ("bf16", (4, 2, 96)), ("bf16", (4, 2, 128)), ("f32", (4, 2, 64))]
+NAMES = [f"{d}-{h[0]}x{h[2]}" for d, h in KERNELS]
+
+
+def of_scores(levels, heads, dtype, seed):
+    """q, k, v of one prompt whose scores are exact: query t, head h and key s have levels[0][t % .., h % ..] * levels[1][s]."""
+    (hq, hkv, d), n = heads, len(levels[1])
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    q, k = torch.zeros((n, hq, d), device="cuda"), torch.zeros((n, hkv, d), device="cuda")
+    rows = torch.as_tensor(levels[0], dtype=torch.float64)
+    q[..., 0] = rows[torch.arange(n)[:, None] % rows.shape[0], torch.arange(hq)[None] % rows.shape[1]].float().cuda()
+    k[..., 0] = torch.as_tensor(levels[1], dtype=torch.float64).float().cuda()[:, None]
+    v = torch.randn((n, hkv, d), generator=g, device="cuda")
+    return [x.to(TYPES[dtype]) for x in (q, k, v)]
+
+
+N = 400
+LEVELS = {
+    "flat": ([[1.0, 3e4, 1e10, 1e25]], [1.1875] * N),
+    "steps": ([[2.0 ** 31, -2.0 ** 34, 2.0 ** 60]], [1.0 + (s * 5 % 7) / 64 for s in range(N)]),
+    "climb": ([[1.0, 1e-3, 1e3]], [np.sign(s - 200) * 2.0 ** (abs(s - 200) / 200 * 90) for s in range(N)]),
+    "fall": ([[1.0, 1e-3, 1e3]], [np.sign(200 - s) * 2.0 ** (abs(s - 200) / 200 * 90) for s in range(N)]),
+    "ends": ([[8.8e29, -8.8e29, 6.9e29, -7.1e29]], [1.0 + (s % 3) / 128 for s in range(N)]),
+    "border": ([[2.0 ** 23, 2.0 ** 24, -2.0 ** 24, 2.0 ** 25, -2.0 ** 23]], [1.0 + (s * 3 % 11) / 128 for s in range(N)]),
+    "fine": ([[2.0 ** 22, -2.0 ** 24, 2.0 ** 25, 2.0 ** 30]], [1.0 + (s * 3 % 5) * 2.0 ** -23 for s in range(N)]),
+    "mixed": ([[1.0, 2.0 ** 33], [-2.0 ** 80, 0.25], [2.0 ** 24, -2.0 ** 24], [0.0, 2.0 ** 10]], [(s * 7 % 13 - 6) / 8 for s in range(N)]),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("what,scale", [(what, scale) for what in LEVELS for scale in (1.0, 0.09) if (what, scale) != ("ends", 0.09)])
+@pytest.mark.parametrize("dtype,heads", KERNELS + [("bf16", (4, 2, 7)), ("f32", (4, 2, 7))], ids=NAMES + ["bf16-any", "f32-any"])
+def test_scores_far_from_zero(dtype, heads, scale, what):
+    """Scores up to the documented ends, times the scale +-1e30.  They are exact in fp32, so the definition in 64 bits knows the weights: keys
+    of the largest score share a row between them, and only keys within 150 / log2(e) of it count ("ends": those of scale 1).  A weight's exponent is a difference of
+    scores times the scale, rounded three times and the scale twice (5 * 2^-24 of at most 150), its power off by 2 steps; then as `check`."""
+    scale = float(np.float32(scale))
+    q, k, v = of_scores(LEVELS[what], heads, dtype, 41)
+    out, lse = spex.prompt_attention([N], q, k, v, scale)
+    hq, hkv, d = heads
+    half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    rel = 2 * (5 * 2.0 ** -24 * 150 * 0.7 + 4 * 2.0 ** -24 + N * 2.0 ** -24)
+    future = torch.ones(N, N, device="cuda").triu(1).bool()
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+    for h in range(hq):
+        kv = h * hkv // hq
+        x = (q[:, h, 0].double()[:, None] * k[:, kv, 0].double()[None] * scale).masked_fill(future, -torch.inf)
+        top = x.amax(-1, keepdim=True)
+        w = torch.exp(x - top)
+        total = w.sum(-1, keepdim=True)
+        ref, mean = (w @ v[:, kv].double()) / total, (w @ v[:, kv].double().abs()) / total
+        bound = rel * mean + half * ref.abs() * 1.01 + half * mean * (1.01 if dtype == "bf16" else 2)
+        worst = float(((out[:, h].double() - ref).abs() / bound).max())
+        assert worst <= 1.0, (h, worst)
+        ref_lse = (top + torch.log(total))[:, 0]
+        off = (lse[:, h].double() - ref_lse).abs() / (8 * 2.0 ** -24 * (ref_lse.abs() + 200) + (N + 4) * 2.0 ** -24)
+        assert float(off.max()) <= 1.0, (h, float(off.max()))
