@@ -58,6 +58,12 @@ spex_status_t spex_prompt_attention(const spex_prompt_config_t *cfg, const int32
                                     const void *q, const void *k, const void *v, void *out, float *lse,
                                     float sm_scale, void *hip_stream);
 
+/* The kernel that a call with these arguments launches, for tests: -1 = none (no tokens); 0 = element by element; 1 = workgroups that
+ * share tiles between their wavefronts, of 64 keys (fp32: 32); 2 = the same with tiles of 32 keys; 3, 4 = workgroups of four, eight
+ * wavefronts that split the keys of their rows.  The tensors are not touched. */
+spex_status_t spex_prompt_form(const spex_prompt_config_t *cfg, const int32_t *lens, int32_t n_prompts, const void *q,
+                               const void *k, const void *v, const void *out, int32_t *form);
+
 #ifdef __cplusplus
 }
 #endif

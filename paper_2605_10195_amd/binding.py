@@ -98,7 +98,7 @@ SCHED_EXPORTS = [
 ]
 
 # spex_prompt.h: attention over whole prompts
-PROMPT_EXPORTS = ["spex_prompt_attention"]
+PROMPT_EXPORTS = ["spex_prompt_attention", "spex_prompt_form"]
 
 
 class PromptConfig(C.Structure):
@@ -159,6 +159,7 @@ def _load():
     lib.spex_sched_early_termination.argtypes = [_I32P, _F64P, i32, i32, C.c_double, _I32P, _I32P]
     lib.spex_tree_path_kv_bytes.argtypes = [vp, i32, _F64P]
     lib.spex_prompt_attention.argtypes = [C.POINTER(PromptConfig), ip, i32, vp, vp, vp, vp, vp, f32, vp]
+    lib.spex_prompt_form.argtypes = [C.POINTER(PromptConfig), ip, i32, vp, vp, vp, vp, _I32P]
     for name in EXPORTS + SCHED_EXPORTS + PROMPT_EXPORTS:
         fn = getattr(lib, name)
         if name not in ("spex_status_string", "spex_last_device_error", "spex_tree_destroy"):

@@ -711,7 +711,7 @@ PromptKernel prompt_kernel(bool f32, bool wide, int32_t D, int64_t row_sets, int
   // 47.9 / 56.4, 4096 (4096): 150.6 / 149.7; 12/4/128, 12 of 200 .. 1500 (3288): 40.8 / 46.6; 16/4/128, 4 of 2000 (4032): 86.6 / 90.0; 40/8/128,
   // 4 of 900 (4640): 50.7 / 51.5; 28/4/128, 16 of 512 (7168): 52.9 / 51.9; 64 of 128 .. 1024 (32 thousand): 331 / 307; 64/8/128, 32 of 2048:
   // 2394 / 2302.  96 dims: 8 of 4096 alike, 12 of 200 .. 1500 34.2 / 40.3; 64 dims: 8 of 4096 345 / 354.
-  k.short_tiles = !f32 && D > 96 && D <= 128 && row_sets > 2 * (3 * 256 * kWaves);
+  k.short_tiles = !f32 && (D > 128 || (D > 96 && row_sets > 2 * (3 * 256 * kWaves)));
   return k;
 }
 
@@ -725,13 +725,9 @@ static void (*bf16_kernel(const PromptKernel &k))(PromptArgs) {
   if constexpr (DP <= 128)
     if (k.eight) return spex_prompt_split_kernel<false, DP, 2 * kWaves>;
   if (k.split) return spex_prompt_split_kernel<false, DP, kWaves>;
-  if constexpr (DP > 128) {
-    return spex_prompt_bf16_kernel<DP, 32, kWaves>;
-  } else {
-    if constexpr (DP == 128)
-      if (k.short_tiles) return spex_prompt_bf16_kernel<DP, 32, kWaves>;
-    return spex_prompt_bf16_kernel<DP, 64, kWaves>;
-  }
+  if constexpr (DP >= 128)
+    if (DP > 128 || k.short_tiles) return spex_prompt_bf16_kernel<DP, 32, kWaves>;
+  if constexpr (DP <= 128) return spex_prompt_bf16_kernel<DP, 64, kWaves>;
 }
 
 hipError_t launch_prompt(const PromptKernel &k, const PromptArgs &a, int64_t items, hipStream_t stream) {

@@ -288,14 +288,126 @@ def test_few_rows_with_long_ways(dtype, heads, lens):
     check(lens, q, k, v, out, lse, heads[2] ** -0.5)
 
 
-# ---- every kernel ------------------------------------------------------------------------------
-# Heads whose calls with a prompt of some 400 tokens take each of the kernels.
-KERNELS = [("bf16", (96, 2, 64)), ("bf16", (60, 3, 96)), ("bf16", (64, 4, 128)), ("bf16", (480, 2, 128)),
-           ("bf16", (40, 4, 192)), ("bf16", (40, 2, 256)), ("f32", (96, 2, 64)), ("f32", (60, 3, 128)),
-           ("f32", (4, 2, 256)), ("bf16", (64, 2, 64)), ("bf16", (24, 2, 96)), ("bf16", (24, 4, 128)),
-           ("bf16", (16, 2, 192)), ("bf16", (8, 2, 256)), ("f32", (32, 2, 64)), ("f32", (8, 1, 128)),
-           ("bf16", (16, 2, 64)), ("bf16", (4, 2, 96)), ("bf16", (4, 2, 128)), ("f32", (4, 2, 64))]
-NAMES = [f"{d}-{h[0]}x{h[2]}" for d, h in KERNELS]
+# ---- every kernel by name ----------------------------------------------------------------------
+# Kernels that spex_prompt_form tells apart, and heads whose calls with a prompt of some 400 tokens take them.
+ANY, WHOLE, SHORT_TILES, FOUR, EIGHT = range(5)
+KERNELS = [("bf16", (96, 2, 64), WHOLE), ("bf16", (60, 3, 96), WHOLE), ("bf16", (64, 4, 128), WHOLE), ("bf16", (480, 2, 128), SHORT_TILES),
+           ("bf16", (40, 4, 192), SHORT_TILES), ("bf16", (40, 2, 256), SHORT_TILES), ("f32", (96, 2, 64), WHOLE), ("f32", (60, 3, 128), WHOLE),
+           ("f32", (4, 2, 256), WHOLE), ("bf16", (64, 2, 64), FOUR), ("bf16", (24, 2, 96), FOUR), ("bf16", (24, 4, 128), FOUR),
+           ("bf16", (16, 2, 192), FOUR), ("bf16", (8, 2, 256), FOUR), ("f32", (32, 2, 64), FOUR), ("f32", (8, 1, 128), FOUR),
+           ("bf16", (16, 2, 64), EIGHT), ("bf16", (4, 2, 96), EIGHT), ("bf16", (4, 2, 128), EIGHT), ("f32", (4, 2, 64), EIGHT)]
+ODD = [("bf16", (4, 2, 7), ANY), ("f32", (4, 2, 7), ANY)]
+NAMES = [f"{d}-{h[0]}x{h[2]}" for d, h, _ in KERNELS]
+SHARING = [x for x in KERNELS if x[2] in (WHOLE, SHORT_TILES)]
+MIXED = [65, 0, 400, 1, 290, 32]
+
+
+def form(lens, heads, dtype, strides=(0, 0, 0, 0), pointers=(64, 64, 64, 64), out=True):
+    la, got = np.asarray(lens, dtype=np.int32), C.c_int32(-7)
+    c = binding.PromptConfig(*heads, {"bf16": binding.BF16, "f32": binding.F32}[dtype], *strides)
+    st = binding.lib.spex_prompt_form(C.byref(c), la.ctypes.data, len(la), *pointers, C.byref(got) if out else None)
+    return got.value if st == OK else ("error", st)
+
+
+@pytest.mark.parametrize("dtype,heads,kernel", KERNELS + ODD, ids=NAMES + ["bf16-any", "f32-any"])
+def test_the_kernel_that_each_case_is_for(dtype, heads, kernel):
+    """A changed rule that empties one of the tests below of the kernel it is for fails here."""
+    for n in (385, 400, 401, 415, 447):
+        assert form([n], heads, dtype) == kernel, n
+    if kernel in (WHOLE, SHORT_TILES):
+        assert form(MIXED, heads, dtype) == kernel
+
+
+def test_forms_of_other_calls():
+    assert form([], (4, 2, 64), "bf16") == form([0, 0], (4, 2, 64), "bf16", pointers=(None,) * 4) == -1
+    assert form([3], (4, 2, 64), "bf16") == FOUR and form([3], (4, 2, 64), "bf16", pointers=(64, 66, 64, 64)) == ANY
+    assert form([3], (4, 2, 64), "f32", strides=(0, 0, 129, 0)) == ANY
+    assert form([3], (4, 2, 64), "bf16", pointers=(64, None, 64, 64)) == form([-3], (4, 2, 64), "bf16") == ("error", INVALID)
+    assert form([3], (4, 2, 64), "bf16", strides=(1 << 31, 0, 0, 0)) == ("error", UNSUPPORTED)
+    assert form([3], (4, 2, 64), "bf16", out=False) == ("error", INVALID)
+
+
+def check_some_heads(lens, q, k, v, out, lse, scale):
+    """`check` on the first, the middle and the last query head of every kv head."""
+    hkv, g = k.shape[1], q.shape[1] // k.shape[1]
+    rows = torch.tensor([kv * g + i for kv in range(hkv) for i in (0, g // 2, g - 1)], device=q.device)
+    check(lens, q[:, rows], k, v, out[:, rows], lse[:, rows], scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fused", [False, True])
+@pytest.mark.parametrize("dtype,heads,kernel", SHARING, ids=NAMES[:len(SHARING)])
+def test_tiles_shared_by_wavefronts_against_the_definition(dtype, heads, kernel, fused):
+    q, k, v = inputs(MIXED, heads, dtype, seed=51, fused=fused)
+    out, lse = spex.prompt_attention(MIXED, q, k, v, heads[2] ** -0.5)
+    check_some_heads(MIXED, q, k, v, out, lse, heads[2] ** -0.5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("what", ["rising", "falling", "far", "flat", "huge"])
+@pytest.mark.parametrize("dtype,heads,kernel", KERNELS, ids=NAMES)
+def test_running_maximum_of_each_kernel(dtype, heads, kernel, what):
+    """As test_scores_that_move_the_running_maximum."""
+    q, k, v = (x.float() for x in inputs([400], heads, dtype, seed=52, spread=1.0))
+    if what == "flat":
+        k.zero_()
+    else:
+        q[..., 0] = 8.0
+        pos = torch.arange(400, device="cuda")[:, None].float()
+        k[..., 0] += {"rising": pos * 0.25, "falling": -pos * 0.25, "far": torch.full_like(pos, -200.0), "huge": 50.0 * (pos % 7)}[what]
+    q, k, v = (x.to(TYPES[dtype]) for x in (q, k, v))
+    out, lse = spex.prompt_attention([400], q, k, v, 0.5)
+    check_some_heads([400], q, k, v, out, lse, 0.5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [1e-38, 1e4])
+@pytest.mark.parametrize("dtype,heads,kernel", SHARING, ids=NAMES[:len(SHARING)])
+def test_scales_at_the_ends_of_shared_tiles(dtype, heads, kernel, scale):
+    q, k, v = inputs(MIXED, heads, dtype, 53)
+    out, lse = spex.prompt_attention(MIXED, q, k, v, scale)
+    check_some_heads(MIXED, q, k, v, out, lse, scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,heads,kernel", SHARING, ids=NAMES[:len(SHARING)])
+def test_windows_captured_and_replayed_with_shared_tiles(dtype, heads, kernel):
+    """out and lse are windows of larger tensors, whose other rows stay; the launch is recorded and replayed on new inputs."""
+    (hq, hkv, d), t = heads, sum(MIXED)
+    big, lse = torch.full((t + 7, hq + 2, d), 9.0, dtype=TYPES[dtype], device="cuda"), torch.full((t + 3, hq), 9.0, device="cuda")
+    out = big[3:3 + t, 1:1 + hq]
+    qkv = inputs(MIXED, heads, dtype, seed=54, fused=True)
+    spex.prompt_attention(MIXED, *qkv, 0.1, out=out, lse=lse[:t])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        spex.prompt_attention(MIXED, *qkv, 0.1, out=out, lse=lse[:t])
+    for seed in (55, 56, 57):
+        for x, y in zip(qkv, inputs(MIXED, heads, dtype, seed=seed)):
+            x.copy_(y)
+        graph.replay()
+        eager, eager_lse = spex.prompt_attention(MIXED, *qkv, 0.1)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager) and torch.equal(lse[:t], eager_lse)
+    check_some_heads(MIXED, *qkv, out, lse[:t], 0.1)
+    out.fill_(9.0)
+    assert bool((big == 9.0).all()) and bool((lse[t:] == 9.0).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [385, 401, 415, 447])
+@pytest.mark.parametrize("dtype,heads,kernel", KERNELS, ids=NAMES)
+def test_nothing_behind_a_prompt_is_read(dtype, heads, kernel, n):
+    """q, k and v are windows with NaN around them, and the prompt ends 1, 17, 31 and 63 keys into a tile."""
+    (hq, hkv, d), big = heads, []
+    for x, h in zip(inputs([n], heads, dtype, seed=n), (hq, hkv, hkv)):
+        y = torch.full((n + 140, h, d), float("nan"), dtype=x.dtype, device="cuda")
+        y[70:70 + n] = x
+        big.append(y[70:70 + n])
+    out, lse = spex.prompt_attention([n], *big, d ** -0.5)
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+    dense, dense_lse = spex.prompt_attention([n], *(x.clone() for x in big), d ** -0.5)
+    assert torch.equal(out, dense) and torch.equal(lse, dense_lse)
 
 
 def of_scores(levels, heads, dtype, seed):
@@ -325,8 +437,8 @@ LEVELS = {
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("what,scale", [(what, scale) for what in LEVELS for scale in (1.0, 0.09) if (what, scale) != ("ends", 0.09)])
-@pytest.mark.parametrize("dtype,heads", KERNELS + [("bf16", (4, 2, 7)), ("f32", (4, 2, 7))], ids=NAMES + ["bf16-any", "f32-any"])
-def test_scores_far_from_zero(dtype, heads, scale, what):
+@pytest.mark.parametrize("dtype,heads,kernel", KERNELS + ODD, ids=NAMES + ["bf16-any", "f32-any"])
+def test_scores_far_from_zero(dtype, heads, kernel, scale, what):
     """Scores up to the documented ends, times the scale +-1e30.  They are exact in fp32, so the definition in 64 bits knows the weights: keys
     of the largest score share a row between them, and only keys within 150 / log2(e) of it count ("ends": those of scale 1).  A weight's exponent is a difference of
     scores times the scale, rounded three times and the scale twice (5 * 2^-24 of at most 150), its power off by 2 steps; then as `check`."""
