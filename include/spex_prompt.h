@@ -51,7 +51,8 @@ typedef struct {
  * softmax weights are rounded to bf16 (to nearest) for their product with v, so that an output is within
  * 2^-8 of the weighted mean of |v| besides its own rounding.
  * Rows whose address, stride or head_dim is no multiple of 16 bytes take a slower kernel.
- * A prompt may have up to 2^24 tokens and all of them INT32_MAX (else SPEX_ERR_UNSUPPORTED).  SPEX_ERR_CAPACITY: no host memory
+ * A prompt may have up to 2^24 tokens, and up to 2^31 - 65 sets of 32 tokens of one of a kv head's query heads, and all prompts INT32_MAX
+ * tokens (else SPEX_ERR_UNSUPPORTED).  SPEX_ERR_CAPACITY: no host memory
  * for the list of the prompts.
  */
 spex_status_t spex_prompt_attention(const spex_prompt_config_t *cfg, const int32_t *lens, int32_t n_prompts,

@@ -48,7 +48,9 @@ spex_status_t check(const spex_prompt_config_t *cfg, const int32_t *lens, int32_
     longest = std::max(longest, lens[i]);
     row_sets += (lens[i] + spex::kPromptRows - 1) / spex::kPromptRows;
   }
-  if (total > INT32_MAX) return SPEX_ERR_UNSUPPORTED;
+  // the kernels count a prompt's row sets of one kv head in 32 bits, with a workgroup's to spare
+  const int64_t longest_sets = (static_cast<int64_t>(longest) + spex::kPromptRows - 1) / spex::kPromptRows;
+  if (total > INT32_MAX || longest_sets * (cfg->num_q_heads / cfg->num_kv_heads) > INT32_MAX - 64) return SPEX_ERR_UNSUPPORTED;
   call->total = total;
   if (total == 0) return SPEX_OK;
   if (!q || !k || !v || !out) return SPEX_ERR_INVALID_ARG;
@@ -110,7 +112,6 @@ extern "C" spex_status_t spex_prompt_attention(const spex_prompt_config_t *cfg, 
   for (int32_t i = 0; i < n_prompts; ++i) {
     if (lens[i] > 0) {
       list[n++] = {at, lens[i]};
-      if (spex::prompt_items(kernel, G, lens[i]) * cfg->num_kv_heads > kMaxLaunchGroups) return SPEX_ERR_UNSUPPORTED;
     }
     at += lens[i];
   }
@@ -131,16 +132,18 @@ extern "C" spex_status_t spex_prompt_attention(const spex_prompt_config_t *cfg, 
   a.Hkv = cfg->num_kv_heads;
   a.G = G;
   a.D = cfg->head_dim;
+  const int64_t room = kMaxLaunchGroups / cfg->num_kv_heads;
+  int64_t done = 0;  // items of prompt i that launches before have taken
   for (int32_t i = 0; i < n;) {
     int64_t items = 0;
-    a.n = 0;
-    for (; i < n && a.n < spex::kMaxPromptsPerLaunch; ++i, ++a.n) {
-      const int64_t more = spex::prompt_items(kernel, G, list[i].len);
-      if ((items + more) * cfg->num_kv_heads > kMaxLaunchGroups) break;
-      a.first[a.n] = static_cast<int32_t>(items);
+    for (a.n = 0; i < n && a.n < spex::kMaxPromptsPerLaunch && items < room; ++a.n) {
+      const int64_t left = spex::prompt_items(kernel, G, list[i].len) - done, take = std::min(left, room - items);
+      a.first[a.n] = static_cast<int32_t>(items - done);
       a.start[a.n] = list[i].start;
       a.len[a.n] = list[i].len;
-      items += more;
+      items += take;
+      done = take < left ? done + take : 0;
+      if (done == 0) ++i;
     }
     for (int32_t j = a.n; j < spex::kMaxPromptsPerLaunch; ++j) {
       a.first[j] = INT32_MAX;

@@ -21,7 +21,8 @@ struct PromptArgs {
   float scale_log2;
   int32_t Hkv, G, D;
   int32_t n;                                // prompts of this launch, longest first
-  int32_t first[kMaxPromptsPerLaunch];      // work items (of one kv head) before the prompt's; INT32_MAX behind the last
+  // work items (of one kv head) before the prompt's, less those of it that an earlier launch has taken; INT32_MAX behind the last
+  int32_t first[kMaxPromptsPerLaunch];
   int32_t start[kMaxPromptsPerLaunch];      // first token
   int32_t len[kMaxPromptsPerLaunch];        // tokens
 };

@@ -1,6 +1,9 @@
 """spex_prompt_attention: refusals on the CPU (nothing is launched), values on the GPU against the definition in 64 bits."""
 
 import ctypes as C
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -463,3 +466,56 @@ def test_scores_far_from_zero(dtype, heads, kernel, scale, what):
         ref_lse = (top + torch.log(total))[:, 0]
         off = (lse[:, h].double() - ref_lse).abs() / (8 * 2.0 ** -24 * (ref_lse.abs() + 200) + (N + 4) * 2.0 ** -24)
         assert float(off.max()) <= 1.0, (h, float(off.max()))
+
+
+# ---- launches ------------------------------------------------------------------------------------
+def test_lists_of_the_launches_under_sanitizers(tmp_path):
+    """Every row set exactly once, however many launches prompts and heads take."""
+    include = "/opt/rocm/include"
+    if shutil.which("g++") is None or not os.path.exists(os.path.join(include, "hip", "hip_runtime.h")):
+        pytest.skip("needs g++ and the HIP headers")
+    here = os.path.dirname(os.path.abspath(__file__))
+    exe = str(tmp_path / "prompt_lists")
+    build = subprocess.run(
+        ["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-static-libasan", "-static-libubsan",
+         "-D__HIP_PLATFORM_AMD__", "-I" + include, "-D__align__(n)=__attribute__((aligned(n)))", os.path.join(here, "prompt_lists.cpp"),
+         os.path.join(here, "..", "paper_2605_10195_amd", "csrc", "prompt.cpp"), "-o", exe], capture_output=True, text=True)
+    if build.returncode != 0 and "cannot find" in build.stderr and any(w in build.stderr for w in ("asan", "ubsan", "sanitize")):
+        pytest.skip("the sanitizer runtime is not installed")
+    assert build.returncode == 0, build.stderr[-2000:]
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=600)
+    assert run.returncode == 0 and run.stdout == "ok\n", (run.stdout[-2000:], run.stderr[-4000:])
+
+
+def test_most_row_sets_of_a_prompt():
+    assert form([1 << 24], (4095, 1, 1), "bf16") == ANY and form([1 << 24], (4096, 1, 1), "bf16") == ("error", UNSUPPORTED)
+    assert form([1 << 24], (1 << 20, 1 << 6, 1), "bf16") == ("error", UNSUPPORTED)
+
+
+@pytest.mark.gpu
+def test_a_prompt_that_takes_several_launches():
+    """8.4 million query heads: two prompts in four launches.  Values are the same for all tokens of a kv head, which is then what every row
+    returns; the first row's score is its log-sum-exp."""
+    lens, (hq, hkv) = [40, 3], (255 * 33000, 255)
+    g = torch.Generator(device="cuda").manual_seed(61)
+    q = torch.randn((43, hq, 1), generator=g, device="cuda").bfloat16()
+    k = torch.randn((43, hkv, 1), generator=g, device="cuda").bfloat16()
+    v = (1 + torch.arange(hkv, device="cuda") / 64).bfloat16()[None, :, None].expand(43, hkv, 1).contiguous()
+    out, lse = torch.full_like(q, float("nan")), torch.full((43, hq), float("nan"), device="cuda")
+    spex.prompt_attention(lens, q, k, v, 1.0, out=out, lse=lse)
+    # the mean is off by 2 * 41 roundings of fp32, 5e-6 of the value, far less than the 2^-9 to the next number that rounds elsewhere
+    assert torch.equal(out, v.repeat_interleave(hq // hkv, 1))
+    for row in (0, 40):
+        score = q[row, :, 0].float() * k[row].repeat_interleave(hq // hkv, 0)[:, 0].float()
+        # two products with log2(e) and ln 2 and their constants, relative 4 * 2^-24
+        assert bool(((lse[row] - score).abs() <= 4 * 2.0 ** -24 * score.abs()).all())
+    heads = torch.randint(0, hq, (300,), generator=g, device="cuda").sort().values
+    cols = torch.cat([heads, torch.tensor([0, hq - 1], device="cuda")])
+    kh, at = k[:, cols * hkv // hq, 0].double(), 0
+    for n in lens:
+        x = (q[at:at + n, cols, 0].double()[:, None] * kh[at:at + n][None]).masked_fill(torch.ones(n, n, device="cuda").triu(1).bool()[..., None], -torch.inf)
+        ref = torch.logsumexp(x, 1)
+        # scores are below 32 and off by 4 * 2^-24 of that, sums by n and the logarithm by a few steps more
+        assert float((lse[at:at + n, cols].double() - ref).abs().max()) <= (4 * 32 + n + 32 * 4) * 2.0 ** -24
+        assert float(x[x > -1e9].abs().max()) < 32
+        at += n
