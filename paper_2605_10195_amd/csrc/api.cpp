@@ -420,40 +420,35 @@ namespace spex {
 // The cached plan, if its copy is on the device and nothing else is waiting for it, follows an append
 // right in the append's launch: same request next time means no planning and no separate patch launch.  Writes up to
 // `room` {index, value} pairs for the launch to apply and returns their number; if a plan needs more, they wait for the next
-// decode_attention call.
+// decode_attention call.  The tokens are in the page table by now, so it does not throw: without host memory the plan is dropped.
 size_t follow_append(spex_tree *t, int32_t *hp, size_t room) {
-  size_t n_patch = 0;
-  if (t->plan.valid && t->plan_on_device && t->pending_patches.empty() &&
-      t->plan.table_version != t->pt->version()) {
-    std::vector<int32_t> &pp = t->pending_patches;
-    if (t->planner.patch_lengths(*t->pt, &t->plan, &pp)) {
-      bool fits = true;
-      for (size_t i = 0; i < pp.size() / 3 && fits; ++i) {
-        const int arr = kPatchTarget[pp[3 * i]];
-        const size_t idx = static_cast<size_t>(pp[3 * i + 1]);
-        if (idx >= t->blob_ints[arr]) continue;  // that list is not on the device
-        if (n_patch == room) {
-          fits = false;
-          break;
-        }
-        hp[2 * n_patch] = static_cast<int32_t>(t->blob_off[arr] / sizeof(int32_t) + idx);
-        hp[2 * n_patch + 1] = pp[3 * i + 2];
-        ++n_patch;
-      }
-      if (fits) {
-        pp.clear();
-        t->plan_patched_by_append = true;
-      } else {
-        n_patch = 0;  // too many for this launch: decode_attention sends them
-      }
-    } else {
-      // The lists cannot follow this append (and may be half changed): drop the plan, so that the
-      // next call plans afresh instead of trying the same patch again on arrays already touched.
-      pp.clear();
-      t->plan.valid = false;
-      t->plan_on_device = false;
-    }
+  if (!t->plan.valid || !t->plan_on_device || !t->pending_patches.empty() || t->plan.table_version == t->pt->version()) return 0;
+  std::vector<int32_t> &pp = t->pending_patches;
+  bool follows = false;
+  try {
+    follows = t->planner.patch_lengths(*t->pt, &t->plan, &pp);
+  } catch (const std::bad_alloc &) {
   }
+  if (!follows) {
+    // The lists cannot follow this append (and may be half changed): drop the plan, so that the
+    // next call plans afresh instead of trying the same patch again on arrays already touched.
+    pp.clear();
+    t->plan.valid = false;
+    t->plan_on_device = false;
+    return 0;
+  }
+  size_t n_patch = 0;
+  for (size_t i = 0; i < pp.size() / 3; ++i) {
+    const int arr = kPatchTarget[pp[3 * i]];
+    const size_t idx = static_cast<size_t>(pp[3 * i + 1]);
+    if (idx >= t->blob_ints[arr]) continue;  // that list is not on the device
+    if (n_patch == room) return 0;           // too many for this launch: decode_attention sends them
+    hp[2 * n_patch] = static_cast<int32_t>(t->blob_off[arr] / sizeof(int32_t) + idx);
+    hp[2 * n_patch + 1] = pp[3 * i + 2];
+    ++n_patch;
+  }
+  pp.clear();
+  t->plan_patched_by_append = true;
   return n_patch;
 }
 

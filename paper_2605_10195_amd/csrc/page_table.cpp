@@ -34,6 +34,12 @@ int32_t PageTable::new_pages_needed(int32_t u, int32_t n_tokens) const {
   return static_cast<int32_t>(pages - static_cast<int64_t>(nd.pages.size()));
 }
 
+void PageTable::reserve(int32_t u, int32_t n_tokens) {
+  std::vector<int32_t> &pages = nodes_[u].pages;
+  const size_t then = pages.size() + static_cast<size_t>(new_pages_needed(u, n_tokens));
+  if (then > pages.capacity()) pages.reserve(then > 2 * pages.capacity() ? then : 2 * pages.capacity());
+}
+
 bool PageTable::append(int32_t u, int32_t n_tokens, int32_t *first_new) {
   const int32_t need = new_pages_needed(u, n_tokens);
   if (need > free_pages()) return false;

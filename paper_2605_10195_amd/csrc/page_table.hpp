@@ -47,6 +47,8 @@ class PageTable {
   // Appends n_tokens; returns false (and changes nothing) if the pool is too small.
   // first_new receives the index, within the node's page run, of the first newly started page.
   bool append(int32_t u, int32_t n_tokens, int32_t *first_new);
+  // Host memory for the page run that such an append makes, so that the append itself cannot fail for want of it.
+  void reserve(int32_t u, int32_t n_tokens);
   // Removes the subtree of u: pre-order, children in creation order, pages in run order,
   // each pushed on the free stack.
   void prune(int32_t u);

@@ -93,6 +93,9 @@ spex_status_t append_rotated_impl(spex_tree_t *t, const spex_node_t *nodes, cons
     }
   }
 
+  if (need > 0)
+    for (int32_t i = 0; i < n_nodes; ++i) t->pt->reserve(nodes[i], counts ? counts[i] : 1);
+
   const spex_status_t us = upload_rotation(t);
   if (us != SPEX_OK) return us;
   // The lists go into the kernel arguments if they fit, with some room for length patches of the cached plan, and else into
@@ -116,7 +119,7 @@ spex_status_t append_rotated_impl(spex_tree_t *t, const spex_node_t *nodes, cons
     if (c == 0) continue;
     const int32_t old_tokens = t->pt->node(u).n_tokens;
     int32_t first_new = 0;
-    t->pt->append(u, c, &first_new);  // cannot fail: the pages were counted above
+    t->pt->append(u, c, &first_new);  // cannot fail: the pages were counted and their lists have room
     const spex::Node &nd = t->pt->node(u);
     for (int32_t at = old_tokens; at < old_tokens + c;) {
       const int32_t page = at >> shift, lo = at & (P - 1), n = std::min(P - lo, old_tokens + c - at);
