@@ -642,8 +642,8 @@ prompt_attention = spex_prompt_attention
 
 
 def spex_tree_append_rotated(tree: SpexTree, nodes, counts, q, k, v, q_out=None, k_out=None, positions=None, k_scales=None,
-                             v_scales=None):
-    return tree.append_rotated(nodes, counts, q, k, v, q_out, k_out, positions, k_scales, v_scales)
+                             v_scales=None, want_k=False):
+    return tree.append_rotated(nodes, counts, q, k, v, q_out, k_out, positions, k_scales, v_scales, want_k)
 
 
 # ---- spex_sched.h: argument marshalling only ------------------------------------------------

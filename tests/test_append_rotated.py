@@ -2,6 +2,7 @@
 against the definition in 64 bits."""
 
 import ctypes as C
+import inspect
 import os
 import shutil
 import subprocess
@@ -559,6 +560,17 @@ def test_pools_on_another_device_are_refused():
     t.k_pool = here
     t.append_rotated([u], None, q, k, v)
     t.close()
+
+
+def test_the_function_hands_on_all_that_the_method_takes():
+    names = list(inspect.signature(spex.SpexTree.append_rotated).parameters)[1:]
+    assert sorted(list(inspect.signature(binding.spex_tree_append_rotated).parameters)[1:]) == sorted(names)
+
+    class Tree:
+        def append_rotated(self, *args, **kw):
+            return inspect.signature(spex.SpexTree.append_rotated).bind(self, *args, **kw).arguments
+    got = binding.spex_tree_append_rotated(Tree(), **{n: n for n in names})
+    assert {n: got[n] for n in names} == {n: n for n in names}
 
 
 def test_lists_of_a_launch_under_sanitizers(tmp_path):
