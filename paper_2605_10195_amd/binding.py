@@ -363,6 +363,7 @@ class SpexTree:
         pa = None if positions is None else _i32(positions)
         total = len(na) if ca is None else _total(ca)
         want, device = torch.float32 if self.kv_dtype == F32 else torch.bfloat16, _device()
+        assert (k_scales is None) == (v_scales is None), "scales of keys and of values go together"
         assert ca is None or len(ca) == len(na)
         assert pa is None or pa.shape == (total,)
         assert self.k_pool is None or self.k_pool.get_device() == device, "the tree's pools must lie on the current device"
@@ -385,8 +386,6 @@ class SpexTree:
                 assert x.dtype is torch.float32 and x.dim() == 2 and x.shape[1] == self.Hkv and x.is_contiguous() and x.get_device() == device
             assert k_scales.shape == v_scales.shape
             d.k_scales, d.v_scales, d.n_scales = k_scales.data_ptr(), v_scales.data_ptr(), k_scales.shape[0]
-        else:
-            assert v_scales is None
         _check(lib.spex_tree_append_rotated(self._h, _addr(na), _addr(ca), len(na), _addr(pa), C.byref(d), _stream()))
         return q_out, k_out
 

@@ -573,6 +573,16 @@ def test_the_function_hands_on_all_that_the_method_takes():
     assert {n: got[n] for n in names} == {n: n for n in names}
 
 
+@pytest.mark.parametrize("one", ["k_scales", "v_scales"])
+def test_scales_of_keys_and_values_go_together(one):
+    t = spex.SpexTree(4, 2, 64, kv_dtype="fp8_e4m3", num_pages=4, device="cpu")
+    (u,) = t.fork(-1, 1)
+    x = torch.zeros(1, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(AssertionError, match="go together"):
+        t.append_rotated([u], None, None, x, x, **{one: torch.ones(1, 2)})
+    t.close()
+
+
 def test_lists_of_a_launch_under_sanitizers(tmp_path):
     """Random trees, nodes and counts with the HIP runtime and the launches replaced by the test's own: every launch has each token once, in
     its slot and at its position, and its patches lie in the plan."""
