@@ -251,7 +251,7 @@ typedef struct {
  * the call is not for recording in a HIP graph.  Rows, rotary_dim or buffers that are not made of 16-byte pieces take a slower
  * kernel.  More than 2^22 pages written by one call are SPEX_ERR_UNSUPPORTED, as is a position beyond INT32_MAX; SPEX_ERR_CAPACITY:
  * no host memory for the lists.
- * The first call after spex_tree_set_rotation copies the frequencies to the device (and synchronises it if it replaces others).
+ * The first call after spex_tree_set_rotation copies the frequencies to the device and waits for its stream (for the device, if it replaces others).
  */
 spex_status_t spex_tree_append_rotated(spex_tree_t *tree, const spex_node_t *nodes, const int32_t *counts, int32_t n_nodes,
                                        const int32_t *positions, const spex_rotated_t *data, void *hip_stream);

@@ -10,14 +10,16 @@
 
 namespace {
 
-// The frequencies to the device.  Launches that read others there are waited for.
-spex_status_t upload_rotation(spex_tree *t) {
+// The frequencies to the device.  Launches that read others there are waited for, and so is the copy, since later launches may come on
+// other streams.
+spex_status_t upload_rotation(spex_tree *t, hipStream_t stream) {
   if (t->freq_on_device) return SPEX_OK;
   if (t->d_freq)
     HIP_TRY(hipDeviceSynchronize());
   else
     HIP_TRY(hipMalloc(&t->d_freq, sizeof(t->freq)));
-  HIP_TRY(hipMemcpy(t->d_freq, t->freq, sizeof(t->freq), hipMemcpyHostToDevice));
+  HIP_TRY(hipMemcpyAsync(t->d_freq, t->freq, sizeof(t->freq), hipMemcpyHostToDevice, stream));
+  HIP_TRY(hipStreamSynchronize(stream));
   t->freq_on_device = true;
   return SPEX_OK;
 }
@@ -96,7 +98,8 @@ spex_status_t append_rotated_impl(spex_tree_t *t, const spex_node_t *nodes, cons
   if (need > 0)
     for (int32_t i = 0; i < n_nodes; ++i) t->pt->reserve(nodes[i], counts ? counts[i] : 1);
 
-  const spex_status_t us = upload_rotation(t);
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  const spex_status_t us = upload_rotation(t, stream);
   if (us != SPEX_OK) return us;
   // The lists go into the kernel arguments if they fit, with some room for length patches of the cached plan, and else into
   // the ring, with room for 32 patches a node as in append_tokens_impl.  A call through the ring takes 5 us more on the host (an event
@@ -165,7 +168,6 @@ spex_status_t append_rotated_impl(spex_tree_t *t, const spex_node_t *nodes, cons
   a.plan = static_cast<int32_t *>(t->d_plan);
   a.patches = static_cast<int32_t>(patch_at);
   a.n_patches = static_cast<int32_t>(n_patch);
-  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   HIP_TRY(spex::launch_append_rotated(t->shape, a, lists, stream));
   return ring ? spex::ring_commit(t, (patch_at + 2 * n_patch) * sizeof(int32_t), stream) : SPEX_OK;
 }

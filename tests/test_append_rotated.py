@@ -605,19 +605,29 @@ def test_lists_of_a_launch_under_sanitizers(tmp_path):
     assert run.returncode == 0 and run.stdout == "ok\n", (run.stdout[-2000:], run.stderr[-4000:])
 
 
-def test_a_call_without_host_memory_changes_nothing(tmp_path):
-    """Every allocation of a call fails in turn: all of the call, or nothing of it."""
+def host_program(tmp_path, name):
+    """tests/<name>.cpp over the library's host sources, run."""
     include = "/opt/rocm/include"
     if shutil.which("g++") is None or not os.path.exists(os.path.join(include, "hip", "hip_runtime.h")):
         pytest.skip("needs g++ and the HIP headers")
     here = os.path.dirname(os.path.abspath(__file__))
     csrc = os.path.join(here, "..", "paper_2605_10195_amd", "csrc")
-    exe = str(tmp_path / "rotated_out_of_memory")
+    exe = str(tmp_path / name)
     build = subprocess.run(
         ["g++", "-std=c++17", "-O1", "-g", "-D__HIP_PLATFORM_AMD__", "-I" + include, "-D__align__(n)=__attribute__((aligned(n)))", "-DHIP_SYMBOL(x)=(&x)",
-         os.path.join(here, "rotated_out_of_memory.cpp")] +
+         os.path.join(here, name + ".cpp")] +
         [os.path.join(csrc, f) for f in ("api.cpp", "rotated_append.cpp", "planner.cpp", "page_table.cpp", "sched.cpp")] + ["-o", exe],
         capture_output=True, text=True)
     assert build.returncode == 0, build.stderr[-2000:]
     run = subprocess.run([exe], capture_output=True, text=True, timeout=600)
     assert run.returncode == 0 and run.stdout == "ok\n", (run.stdout[-2000:], run.stderr[-4000:])
+
+
+def test_a_call_without_host_memory_changes_nothing(tmp_path):
+    """Every allocation of a call fails in turn: all of the call, or nothing of it."""
+    host_program(tmp_path, "rotated_out_of_memory")
+
+
+def test_frequencies_have_landed_before_a_launch_reads_them(tmp_path):
+    """On whatever stream, with copies that end when somebody waits for them, and not under launches that read those of the setting before."""
+    host_program(tmp_path, "rotated_frequencies")
