@@ -434,6 +434,8 @@ LEVELS = {
     "ends": ([[8.8e29, -8.8e29, 6.9e29, -7.1e29]], [1.0 + (s % 3) / 128 for s in range(N)]),
     "border": ([[2.0 ** 23, 2.0 ** 24, -2.0 ** 24, 2.0 ** 25, -2.0 ** 23]], [1.0 + (s * 3 % 11) / 128 for s in range(N)]),
     "fine": ([[2.0 ** 22, -2.0 ** 24, 2.0 ** 25, 2.0 ** 30]], [1.0 + (s * 3 % 5) * 2.0 ** -23 for s in range(N)]),
+    # the keys of one wavefront of a split launch far below zero, of others near, or near the border of the two
+    "states": ([[1.0], [2.0 ** -2]], [[-2.0 ** 40, -2.0 ** 24 - 64, -2.0 ** 24 + 130, (s % 5) * 1.5, 2.0 ** 24 - 60, 2.0 ** 24 + 32, 2.0 ** 27][s // 32 % 7] * (1 if s < 300 else -1) for s in range(N)]),
     "mixed": ([[1.0, 2.0 ** 33], [-2.0 ** 80, 0.25], [2.0 ** 24, -2.0 ** 24], [0.0, 2.0 ** 10]], [(s * 7 % 13 - 6) / 8 for s in range(N)]),
 }
 
