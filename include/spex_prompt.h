@@ -44,7 +44,7 @@ typedef struct {
  *   k, v : DEVICE [sum(lens)][num_kv_heads][head_dim]
  *   out  : DEVICE, shape of q:  sum_s softmax_s(sm_scale * <q_t, k_s>) v_s, rounded to nearest
  *   lse  : DEVICE fp32 [sum(lens)][num_q_heads] or NULL:  ln sum_s exp(sm_scale * <q_t, k_s>)
- * q, k and v must be finite, and so must the scores <q_t, k_s> in fp32 and, times sm_scale, stay within +-1e30; sm_scale in
+ * q, k and v must be finite (a value of v that is not may spoil rows of tokens before its own, too), and so must the scores <q_t, k_s> in fp32 and, times sm_scale, stay within +-1e30; sm_scale in
  * 1e-38 .. 1e37 (else SPEX_ERR_INVALID_ARG).  out must not overlap q, k or v.  Nothing outside
  * the prompts' rows is read or written.  Scores, softmax statistics and sums are fp32 (a weight's exponent is a difference of
  * scores, also where the scores are so large that fp32 rounds their scaled values to many units); for bf16 the

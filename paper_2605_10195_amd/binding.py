@@ -357,7 +357,7 @@ class SpexTree:
                        v_scales: Optional[torch.Tensor] = None, want_k: bool = False):
         """Rotate and append counts[i] tokens (None: one) to each of nodes, one launch.  q [tokens, Hq, D] or None, k and v
         [tokens, Hkv, D] in bfloat16 (float32 for fp32 pools), dense or with a stride between tokens.  Returns the rotated
-        queries and -- want_k, or k_out given -- keys; q_out=q and k_out=k rotate in place."""
+        queries and -- want_k, or k_out given -- keys; q_out=q and k_out=k rotate in place.  fp8 pools: k and v must be finite."""
         na = _i32(nodes)
         ca = None if counts is None else _i32(counts)
         pa = None if positions is None else _i32(positions)
@@ -616,7 +616,8 @@ def _token_stride(t: torch.Tensor, total: int, heads: int, dim: int, dtype: torc
 def spex_prompt_attention(lens: Sequence[int], q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sm_scale: float,
                           out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = True):
     """Causal attention over packed prompts: q [tokens, Hq, D], k and v [tokens, Hkv, D] in float32 or bfloat16, dense or with
-    a stride between tokens (parts of one projection); out has q's shape and type.  Returns (out, lse)."""
+    a stride between tokens (parts of one projection); out has q's shape and type.  Returns (out, lse).  q, k and v must be finite: a
+    value of v that is not may spoil rows of tokens before its own, too."""
     la = _i32(lens)
     total, hq, dim = q.shape
     hkv, dtype, device = k.shape[1], q.dtype, _device()

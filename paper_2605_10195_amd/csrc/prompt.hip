@@ -17,11 +17,13 @@
 // With the scores transposed a lane holds scores of one query row only (column lane % 32 of the MFMA result), so m and l
 // are one register each, and the weights of 16 keys are, as they lie, the B operand of the PV product for the
 // key order {8 j + 4 (lane / 32) + i}: V is read from LDS in that order by the transposing load.
+// bf16: the weights are rounded to bf16, half a step of 2^-8 each, because the product with V takes its operands so; two parts of a weight
+// would keep 16 bits and double that product's matrix instructions.  l sums them as they were before.
 //
 // Bound: the matrix cores, and with them power (at 1.0 PFLOP/s the clock falls from 2.4 to 1.75 GHz; on zeros the same launch is a
 // third faster).  bf16, 8 prompts of 4096 tokens: D 64 0.82 PFLOP/s (the exponentials take a larger share), 96 0.87, 128 1.04, 192 1.0,
 // 256 (4 prompts) 0.9; one of 16000, 32/8/128: 1.1; a bf16 matrix product of 16384 reaches 1.35.  Prompts below 1000 tokens are bound by
-// the first loads and last stores of their workgroups: 64 of 128 .. 1024 tokens, 28/4/128: 307 us, 16 of 1024: 0.8 PFLOP/s.  fp32:
+// the first loads and last stores of their workgroups: 64 of 128 .. 1024 tokens, 28/4/128: 294 us, 16 of 1024: 0.8 PFLOP/s.  fp32:
 // 105 TFLOP/s at D 128 (matrix product: 154).  One prompt of a few hundred tokens: 10 us, launch and latency.
 #include "prompt.hpp"
 
