@@ -101,8 +101,8 @@ spex_status_t spex_sched_allocate_budget(const int32_t *capacity, const double *
 
 /*
  * S_KV(q) of Eq. 1 read from the page table: bytes of K and V held by the tokens on the
- * root-to-node path of `node` (tokens * 2 * num_kv_heads * head_dim * element size; fp8: plus
- * 8 * num_kv_heads bytes of scales for every page on the path), i.e. the cache every branch
+ * root-to-node path of `node` (tokens * 2 * num_kv_heads * head_dim * element size; MXFP4: 17 / 32
+ * of a byte an element; fp8: plus 8 * num_kv_heads bytes of scales for every page on the path), i.e. the cache every branch
  * forked below `node` reuses instead of recomputing.  SPEX_ERR_BAD_NODE for an unknown or pruned
  * node.  HOST call, no GPU work.
  */

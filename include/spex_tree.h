@@ -45,7 +45,7 @@ typedef enum {
   SPEX_ERR_CAPACITY = 8     /* caller-provided output array too small */
 } spex_status_t;
 
-typedef enum { SPEX_F32 = 0, SPEX_BF16 = 1, SPEX_FP8_E4M3 = 2 } spex_dtype_t;
+typedef enum { SPEX_F32 = 0, SPEX_BF16 = 1, SPEX_FP8_E4M3 = 2, SPEX_MXFP4 = 3 /* pools only */ } spex_dtype_t;
 
 /*
  * Pool layout.  k_pool and v_pool are caller-owned DEVICE buffers of (page, kv head) tiles of
@@ -69,6 +69,21 @@ typedef enum { SPEX_F32 = 0, SPEX_BF16 = 1, SPEX_FP8_E4M3 = 2 } spex_dtype_t;
  *     V, fp8 :  (d/32)*512 + (t/8)*256 + (d%16)*16 + ((d/16)&1)*8 + t%8
  *  Use spex_tree_gather_kv to read tokens back in logical order.
  *
+ *  MXFP4      (kv_dtype MXFP4; page_size 16, head_dim a multiple of 32, pools 16-byte aligned, else SPEX_ERR_UNSUPPORTED):
+ *     microscaled 4-bit floating point, 4.25 bits an element.  32 consecutive dims of one token and kv head are a block: they share
+ *     a scale 2^E and hold e2m1 numbers (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), value = number * 2^E.  Only the
+ *     quantising appends write such a pool.  With amax the largest magnitude of a block of what they are given (keys of
+ *     spex_tree_append_rotated: rotated, in fp32),
+ *         E = floor(log2 amax) - 2, bounded to -126 .. 125 for keys and to -23 .. 13 for values,
+ *     a number is the nearest to x * 2^-E, ties to the one whose last bit is 0, at most 6 in magnitude.  So a key or value
+ *     is off by at most 2 * 2^E, a value of V beyond 49152 is held as 49152, one of 2^-25 or less may be held as 0.
+ *     A tile is 17 * head_dim / 2 bytes: with M = head_dim / 32, 256 M bytes of codes, two dims to a byte (the even one in the low
+ *     half), and 16 M bytes E + 127, [block][token].  Offsets of the codes, a word being 4 bytes:
+ *     K: dims 8 u .. 8 u + 7 of token t are word s of lane 16 j + t, V: dims 2 u, 2 u + 1 of token t are byte t % 4 of word i of
+ *     lane 16 (t / 4) + c; word w of lane l lies at 4 (l M + w).  M a power of two: j = u / M, s = u % M (K), c = u / M,
+ *     i = u % M (V); else j = u % 4, s = u / 4, c = u % 16, i = u / 16.
+ *     k_scale and v_scale must be NULL.
+ *
  * fp8 (OCP e4m3fn): value = code * scale, one fp32 scale per (page, kv head), separately
  * for K and V, in the caller-owned DEVICE arrays k_scale / v_scale [num_pages][num_kv_heads].
  * Scales must be finite and >= 0 (0: a page of zeros).
@@ -87,7 +102,7 @@ typedef enum { SPEX_F32 = 0, SPEX_BF16 = 1, SPEX_FP8_E4M3 = 2 } spex_dtype_t;
  *   - code * v_scale is formed in half precision in two steps (the power of two of the scale,
  *     then its mantissa rounded to 11 bits): relative error at most 2^-10, and for a magnitude
  *     below 2^-14 an absolute error below 2^-23;
- * the other kernels of an fp8 pool reproduce code * v_scale exactly.  Row-major pools (fp32, other
+ * the other kernels of an fp8 pool reproduce code * v_scale exactly.  Attention over an MXFP4 pool takes its values as they are.  Row-major pools (fp32, other
  * page sizes and head dims) hold and return V as given.  Inside the range every kernel meets the
  * same error bound.
  */
@@ -96,7 +111,7 @@ typedef struct {
   int32_t num_kv_heads;
   int32_t head_dim;     /* 1..256 */
   int32_t page_size;    /* power of two, 1..64 */
-  int32_t q_dtype;      /* spex_dtype_t: (F32,F32) | (BF16,BF16) | (BF16,FP8_E4M3) as (q, kv) */
+  int32_t q_dtype;      /* spex_dtype_t: (F32,F32) | (BF16,BF16) | (BF16,FP8_E4M3) | (BF16,MXFP4) as (q, kv) */
   int32_t kv_dtype;
   int64_t num_pages;
   void *k_pool;         /* DEVICE; may be NULL for a host-only handle (no append data, no attention) */
@@ -107,7 +122,8 @@ typedef struct {
                                 pages are first handed out; NULL = ascending.  Copied by create. */
   int32_t prefix_chunk_pages; /* split granularity of shared-prefix segments; 0 = automatic */
   int32_t suffix_chunk_pages; /* split granularity of private suffixes;       0 = automatic */
-  int32_t kernel_mode;  /* 0 = automatic; 1 = generic (non-MFMA) kernels; 2 = shared-prefix + suffix +
+  int32_t kernel_mode;  /* 0 = automatic; 1 = generic (non-MFMA) kernels (MXFP4 pools have none: decode_attention fails with
+                           SPEX_ERR_UNSUPPORTED); 2 = shared-prefix + suffix +
                            merge kernels; 3 = tree-walk kernel (decode_attention fails with
                            SPEX_ERR_UNSUPPORTED where it does not apply) */
   int32_t page_stride_tiles; /* distance between consecutive pages of a pool, in (page, head) tiles;
@@ -156,13 +172,15 @@ spex_status_t spex_tree_fork(spex_tree_t *tree, spex_node_t parent, int32_t n_ch
  * the source buffers must stay valid until that work has run.
  * k == NULL and v == NULL: only the page table is updated (host-only handles, or callers that
  * never read these tokens back).
+ * MXFP4 pools: SPEX_ERR_UNSUPPORTED with data; spex_tree_append_step_quantize writes them.
  */
 spex_status_t spex_tree_append_step(spex_tree_t *tree, spex_node_t node, int32_t n_tokens,
                                     const void *k, const void *v, const float *k_scales,
                                     const float *v_scales, void *hip_stream);
 /*
- * The same append with the cache quantised on the fly (fp8 pools only, else SPEX_ERR_UNSUPPORTED):
- * k, v are DEVICE [n_tokens][num_kv_heads][head_dim] in bf16 with finite values.  For every page
+ * The same append with the cache quantised on the fly (fp8 and MXFP4 pools, else SPEX_ERR_UNSUPPORTED):
+ * k, v are DEVICE [n_tokens][num_kv_heads][head_dim] in bf16 with finite values.  MXFP4: as stated there, every token by itself; the
+ * page ids of a long append lie in pinned memory of the handle, as those of spex_tree_append_tokens.  fp8: for every page
  * the append starts, the scatter kernel first takes amax = the largest magnitude among the tokens
  * this append puts into that page, per kv head and separately for K and V, and sets the page's
  * scale = max(amax / 448, 2^-40); tokens that continue a partially filled page use the scale the
@@ -193,9 +211,9 @@ spex_status_t spex_tree_append_tokens(spex_tree_t *tree, const spex_node_t *node
                                       const void *k, const void *v, const float *k_scales,
                                       const float *v_scales, void *hip_stream);
 /*
- * The same step with the cache quantised on the fly (fp8 pools only, else SPEX_ERR_UNSUPPORTED):
+ * The same step with the cache quantised on the fly (fp8 and MXFP4 pools, else SPEX_ERR_UNSUPPORTED):
  * k, v are DEVICE [n_nodes][num_kv_heads][head_dim] in bf16, as the model produces them, and the
- * kernel that scatters them also encodes them: code = e4m3fn(x * (1 / scale)), product and
+ * kernel that scatters them also encodes them.  MXFP4: finite values, k_scales and v_scales NULL.  fp8: code = e4m3fn(x * (1 / scale)), product and
  * reciprocal in fp32, round to nearest even, saturating at +-448, NaN kept.  scale is row i of
  * k_scales / v_scales if node i's token starts a page (the row becomes that page's scale) and the
  * scale the page already has otherwise -- a page is never requantised, later tokens saturate.
@@ -247,6 +265,7 @@ typedef struct {
  * saturating; k and v must be finite there.  A page the call starts takes its row of k_scales / v_scales (pages in the order of the nodes, within a node in token
  * order) if they are given, and else scale = max(amax / 448, 2^-40) over the tokens the call puts into it, as
  * spex_tree_append_step_quantize; other pages keep the scale they have.
+ * MXFP4 pools are quantised the same way, a scale to every 32 dims of a token; k and v must be finite and no scales are given.
  * All or nothing, page order, structure version and patches of the cached launch lists as spex_tree_append_tokens; like it,
  * the call is not for recording in a HIP graph.  Rows, rotary_dim or buffers that are not made of 16-byte pieces take a slower
  * kernel.  More than 2^22 pages written by one call are SPEX_ERR_UNSUPPORTED, as is a position beyond INT32_MAX; SPEX_ERR_CAPACITY:
@@ -404,10 +423,27 @@ typedef struct {
 spex_status_t spex_tree_plan_dump(spex_tree_t *tree, const spex_node_t *leaves,
                                   const int32_t *q_lens, int32_t n_leaves, spex_plan_view_t *out);
 
+/*
+ * Reads an MXFP4 cache back (other pools: SPEX_ERR_UNSUPPORTED, see spex_tree_gather_kv): the values that the codes stand for, of tokens
+ * of many nodes, in one launch.  For a program that hands the tokens of a search to something else -- a reward model's own cache,
+ * another process -- or computes on them itself.
+ *   nodes : HOST [n_nodes], live nodes, leaves or not, in any order and any number of times
+ *   firsts, counts : HOST [n_nodes] or NULL: node i's own tokens firsts[i] .. firsts[i] + counts[i] - 1 (firsts NULL: from its
+ *     first on, counts NULL: to its last).  Tokens beyond a node's are SPEX_ERR_INVALID_ARG
+ *   k_out, v_out : DEVICE bf16 [sum of the counts][num_kv_heads][head_dim], dense, the nodes one behind the other.  Every value is exact.
+ *     Both NULL: only n_tokens is asked for (no device needed)
+ *   n_tokens : HOST or NULL: receives the sum of the counts
+ * More than 2^22 pages read by one call are SPEX_ERR_UNSUPPORTED; SPEX_ERR_CAPACITY: no host memory for the lists.  Like an append the call
+ * reads its lists from the handle's pinned memory and is not for recording in a HIP graph.
+ */
+spex_status_t spex_tree_read_back(spex_tree_t *tree, const spex_node_t *nodes, const int32_t *firsts, const int32_t *counts,
+                                  int32_t n_nodes, void *k_out, void *v_out, int64_t *n_tokens, void *hip_stream);
+
 /* Copy a node's own tokens [first, first + n) out of the pool in logical order:
  * k_out, v_out DEVICE [n][num_kv_heads][head_dim] in kv_dtype; fp8 codes are copied as stored and
  * k_scale_out / v_scale_out (DEVICE [n][num_kv_heads] fp32, may be NULL) receive each token's
- * page scale.  Enqueued on hip_stream. */
+ * page scale.  MXFP4 pools: spex_tree_read_back of the one node, bf16 values; no scales (SPEX_ERR_INVALID_ARG).
+ * Enqueued on hip_stream. */
 spex_status_t spex_tree_gather_kv(spex_tree_t *tree, spex_node_t node, int32_t first, int32_t n,
                                   void *k_out, void *v_out, float *k_scale_out, float *v_scale_out,
                                   void *hip_stream);

@@ -18,9 +18,9 @@ import torch
 from .build import LIB_PATH
 
 NO_NODE = -1
-F32, BF16, FP8_E4M3 = 0, 1, 2
-_DTYPES = {"f32": F32, "bf16": BF16, "fp8_e4m3": FP8_E4M3}
-_TORCH_KV = {F32: torch.float32, BF16: torch.bfloat16, FP8_E4M3: torch.uint8}
+F32, BF16, FP8_E4M3, MXFP4 = 0, 1, 2, 3
+_DTYPES = {"f32": F32, "bf16": BF16, "fp8_e4m3": FP8_E4M3, "mxfp4": MXFP4}
+_TORCH_KV = {F32: torch.float32, BF16: torch.bfloat16, FP8_E4M3: torch.uint8, MXFP4: torch.bfloat16}  # of tokens read back
 
 STATUS_NAMES = ["OK", "INVALID_ARG", "BAD_NODE", "NOT_LEAF", "OOM_PAGES", "EMPTY_PATH",
                 "UNSUPPORTED", "DEVICE", "CAPACITY"]
@@ -89,7 +89,7 @@ EXPORTS = [
     "spex_tree_free_pages", "spex_tree_stats", "spex_tree_plan_dump", "spex_tree_gather_kv",
     "spex_tree_set_tuning", "spex_tree_set_profiling", "spex_tree_read_profile",
     "spex_tree_last_launch_info", "spex_tree_split_form", "spex_tree_walk_dump", "spex_tree_append_tokens", "spex_tree_append_tokens_quantize", "spex_tree_append_step_quantize",
-    "spex_tree_set_rotation", "spex_tree_append_rotated",
+    "spex_tree_set_rotation", "spex_tree_append_rotated", "spex_tree_read_back",
 ]
 # spex_sched.h: host-side scheduling primitives
 SCHED_EXPORTS = [
@@ -135,6 +135,7 @@ def _load():
     lib.spex_tree_append_tokens_quantize.argtypes = [vp, ip, i32, vp, vp, vp, vp, vp]
     lib.spex_tree_set_rotation.argtypes = [vp, i32, vp, i32]
     lib.spex_tree_append_rotated.argtypes = [vp, ip, ip, i32, ip, C.POINTER(Rotated), vp]
+    lib.spex_tree_read_back.argtypes = [vp, ip, ip, ip, i32, vp, vp, C.POINTER(i64), vp]
     lib.spex_tree_prune.argtypes = [vp, i32]
     lib.spex_tree_decode_attention.argtypes = [vp, ip, ip, i32, vp, vp, vp, f32, vp]
     lib.spex_tree_decode_attention_masked.argtypes = [vp, ip, ip, ip, i32, vp, vp, vp, f32, vp]
@@ -249,8 +250,10 @@ class SpexTree:
             fill = 0 if pool_fill is None else pool_fill
             if interleave_kv:
                 # one buffer, [page][K tiles of all heads | V tiles of all heads]
-                esz = {F32: 4, BF16: 2, FP8_E4M3: 1}[self.kv_dtype]
-                half = num_kv_heads * page_size * head_dim * esz
+                one = Config.from_buffer_copy(cfg)
+                one.num_pages, one.page_stride_tiles = 1, 0
+                _check(lib.spex_pool_bytes(C.byref(one), C.byref(nbytes)))
+                half = nbytes.value
                 self.k_pool = torch.full((max(2 * half * self.num_pages, 16),), fill, dtype=torch.uint8,
                                          device=self.device)
                 self.v_pool = self.k_pool[half:]
@@ -302,7 +305,7 @@ class SpexTree:
         if k is None:
             _check(lib.spex_tree_append_step(self._h, node, int(n_tokens), None, None, None, None, None))
             return
-        if quantize:                     # bf16 in, e4m3 codes and page scales made by the library
+        if quantize:                     # bf16 in, codes and scales made by the library
             assert k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and k_scales is None
             assert k.is_contiguous() and v.is_contiguous() and self._here(k)
             shape = k.shape
@@ -331,7 +334,7 @@ class SpexTree:
                       k_scales: Optional[torch.Tensor] = None, v_scales: Optional[torch.Tensor] = None,
                       quantize: bool = False):
         """One token per node, one launch.  k, v: [len(nodes), Hkv, D] on the tree's device, in the
-        pool's dtype, or -- quantize=True, fp8 pools -- in bf16, encoded by the library."""
+        pool's dtype, or -- quantize=True, fp8 and mxfp4 pools -- in bf16, encoded by the library."""
         na = _i32(nodes)
         if k is not None:
             assert k.is_contiguous() and v.is_contiguous() and k.shape == (len(na), self.Hkv, self.D)
@@ -357,7 +360,7 @@ class SpexTree:
                        v_scales: Optional[torch.Tensor] = None, want_k: bool = False):
         """Rotate and append counts[i] tokens (None: one) to each of nodes, one launch.  q [tokens, Hq, D] or None, k and v
         [tokens, Hkv, D] in bfloat16 (float32 for fp32 pools), dense or with a stride between tokens.  Returns the rotated
-        queries and -- want_k, or k_out given -- keys; q_out=q and k_out=k rotate in place.  fp8 pools: k and v must be finite."""
+        queries and -- want_k, or k_out given -- keys; q_out=q and k_out=k rotate in place.  fp8 and mxfp4 pools: k and v must be finite."""
         na = _i32(nodes)
         ca = None if counts is None else _i32(counts)
         pa = None if positions is None else _i32(positions)
@@ -388,6 +391,29 @@ class SpexTree:
             d.k_scales, d.v_scales, d.n_scales = k_scales.data_ptr(), v_scales.data_ptr(), k_scales.shape[0]
         _check(lib.spex_tree_append_rotated(self._h, _addr(na), _addr(ca), len(na), _addr(pa), C.byref(d), _stream()))
         return q_out, k_out
+
+    def read_back(self, nodes: Sequence[int], firsts: Optional[Sequence[int]] = None, counts: Optional[Sequence[int]] = None,
+                  k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None):
+        """The values that an mxfp4 cache holds for tokens firsts[i] .. firsts[i] + counts[i] - 1 of nodes[i] (None: from the first on, to the
+        last), one launch.  Returns k and v, bfloat16 [tokens, Hkv, D], the nodes one behind the other."""
+        na = _i32(nodes)
+        fa = None if firsts is None else _i32(firsts)
+        ca = None if counts is None else _i32(counts)
+        assert (fa is None or len(fa) == len(na)) and (ca is None or len(ca) == len(na))
+        total = C.c_int64()
+        _check(lib.spex_tree_read_back(self._h, _addr(na), _addr(fa), _addr(ca), len(na), None, None, C.byref(total), None))
+        device = _device()
+        assert self.k_pool is None or self.k_pool.get_device() == device, "the tree's pools must lie on the current device"
+        shape = (total.value, self.Hkv, self.D)
+        if k_out is None:
+            k_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        if v_out is None:
+            v_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        for x in (k_out, v_out):
+            assert x.shape == shape and x.dtype is torch.bfloat16 and x.is_contiguous()
+            assert self.k_pool is None or x.get_device() == device, "all tensors must lie on the current device"
+        _check(lib.spex_tree_read_back(self._h, _addr(na), _addr(fa), _addr(ca), len(na), _dev(k_out), _dev(v_out), None, _stream()))
+        return k_out, v_out
 
     def prune(self, node: int) -> None:
         _check(lib.spex_tree_prune(self._h, node))
@@ -644,6 +670,10 @@ prompt_attention = spex_prompt_attention
 def spex_tree_append_rotated(tree: SpexTree, nodes, counts, q, k, v, q_out=None, k_out=None, positions=None, k_scales=None,
                              v_scales=None, want_k=False):
     return tree.append_rotated(nodes, counts, q, k, v, q_out, k_out, positions, k_scales, v_scales, want_k)
+
+
+def spex_tree_read_back(tree: SpexTree, nodes, firsts=None, counts=None, k_out=None, v_out=None):
+    return tree.read_back(nodes, firsts, counts, k_out, v_out)
 
 
 # ---- spex_sched.h: argument marshalling only ------------------------------------------------

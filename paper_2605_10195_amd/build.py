@@ -9,8 +9,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libspex_tree.so")
-SOURCES = ["api.cpp", "page_table.cpp", "planner.cpp", "sched.cpp", "rotated_append.cpp", "prompt.cpp"]
-KERNELS = ["kernels.hip", "rotated_append.hip", "prompt.hip"]
+SOURCES = ["api.cpp", "page_table.cpp", "planner.cpp", "sched.cpp", "rotated_append.cpp", "mxfp4.cpp", "prompt.cpp"]
+KERNELS = ["kernels.hip", "rotated_append.hip", "prompt.hip", "mxfp4_cache.hip", "mxfp4_attention.hip"]
 
 
 def hipcc() -> str:

@@ -20,6 +20,8 @@ thread_local std::string g_last_error;
 }  // namespace
 
 namespace spex {
+const Mxfp4Calls *mxfp4_calls = nullptr;
+
 bool hip_failed(hipError_t e, const char *what) {
   if (e == hipSuccess) return false;
   g_last_error = std::string(what) + ": " + hipGetErrorString(e);
@@ -35,6 +37,9 @@ using spex::hip_failed;
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 bool is_pow2(int32_t x) { return x > 0 && (x & (x - 1)) == 0; }
+
+// Whether a pool of this shape can be held in MXFP4.
+bool mxfp4_shape(const spex_config_t *c) { return c->page_size == 16 && c->head_dim % 32 == 0; }
 
 spex_status_t check_config(const spex_config_t *c) {
   if (!c) return SPEX_ERR_INVALID_ARG;
@@ -52,8 +57,12 @@ spex_status_t check_config(const spex_config_t *c) {
   if (c->walk_waves != 0 && c->walk_waves != 2 && c->walk_waves != 4 && c->walk_waves != 8) return SPEX_ERR_INVALID_ARG;
   const bool ok = (c->q_dtype == SPEX_F32 && c->kv_dtype == SPEX_F32) ||
                   (c->q_dtype == SPEX_BF16 && c->kv_dtype == SPEX_BF16) ||
-                  (c->q_dtype == SPEX_BF16 && c->kv_dtype == SPEX_FP8_E4M3);
+                  (c->q_dtype == SPEX_BF16 && c->kv_dtype == SPEX_FP8_E4M3) ||
+                  (c->q_dtype == SPEX_BF16 && c->kv_dtype == SPEX_MXFP4 && spex::mxfp4_calls && mxfp4_shape(c));
   if (!ok) return SPEX_ERR_UNSUPPORTED;
+  if (c->kv_dtype == SPEX_MXFP4 && (c->k_scale || c->v_scale)) return SPEX_ERR_INVALID_ARG;
+  if (c->kv_dtype == SPEX_MXFP4 && ((reinterpret_cast<uintptr_t>(c->k_pool) | reinterpret_cast<uintptr_t>(c->v_pool)) & 15) != 0)
+    return SPEX_ERR_UNSUPPORTED;
   if ((c->k_pool == nullptr) != (c->v_pool == nullptr)) return SPEX_ERR_INVALID_ARG;
   if (c->kv_dtype == SPEX_FP8_E4M3 && c->k_pool && (!c->k_scale || !c->v_scale))
     return SPEX_ERR_INVALID_ARG;
@@ -61,6 +70,11 @@ spex_status_t check_config(const spex_config_t *c) {
 }
 
 size_t elem_size(int32_t dt) { return dt == SPEX_F32 ? 4 : (dt == SPEX_BF16 ? 2 : 1); }
+// Bytes of one kv head of a page; of one token's share in it.
+size_t token_bytes(const spex_config_t &c) {
+  return c.kv_dtype == SPEX_MXFP4 ? static_cast<size_t>(c.head_dim) / 32 * 17 : static_cast<size_t>(c.head_dim) * elem_size(c.kv_dtype);
+}
+size_t tile_bytes(const spex_config_t &c) { return static_cast<size_t>(c.page_size) * token_bytes(c); }
 
 spex::Shape make_shape(const spex_config_t &c) {
   spex::Shape s{};
@@ -71,8 +85,8 @@ spex::Shape make_shape(const spex_config_t &c) {
   s.P = c.page_size;
   s.q_dtype = c.q_dtype;
   s.kv_dtype = c.kv_dtype;
-  const bool tiled = c.kv_dtype != SPEX_F32 && c.page_size == 16 && (c.head_dim == 64 || c.head_dim == 128);
-  s.layout = tiled ? spex::kMfmaTiled : spex::kRowMajor;
+  const bool tiled = c.kv_dtype != SPEX_F32 && c.kv_dtype != SPEX_MXFP4 && c.page_size == 16 && (c.head_dim == 64 || c.head_dim == 128);
+  s.layout = c.kv_dtype == SPEX_MXFP4 ? spex::kMxTiled : tiled ? spex::kMfmaTiled : spex::kRowMajor;
   s.page_tiles = c.page_stride_tiles ? c.page_stride_tiles : c.num_kv_heads;
   return s;
 }
@@ -476,14 +490,14 @@ const char *spex_last_device_error(void) { return g_last_error.c_str(); }
 spex_status_t spex_pool_bytes(const spex_config_t *cfg, size_t *bytes_per_pool) {
   if (!cfg || !bytes_per_pool) return SPEX_ERR_INVALID_ARG;
   if (cfg->num_pages < 0 || cfg->num_kv_heads <= 0 || cfg->page_size <= 0 || cfg->head_dim <= 0 ||
-      cfg->kv_dtype < 0 || cfg->kv_dtype > 2)
+      cfg->kv_dtype < 0 || cfg->kv_dtype > 3)
     return SPEX_ERR_INVALID_ARG;
+  if (cfg->kv_dtype == SPEX_MXFP4 && !mxfp4_shape(cfg)) return SPEX_ERR_UNSUPPORTED;
   const size_t tiles = cfg->page_stride_tiles ? cfg->page_stride_tiles : cfg->num_kv_heads;
-  const size_t tile_bytes = static_cast<size_t>(cfg->page_size) * cfg->head_dim * elem_size(cfg->kv_dtype);
   // A strided pool ends with the last page's own tiles, not with a full stride.
   *bytes_per_pool = cfg->num_pages == 0 ? 0
                                         : (static_cast<size_t>(cfg->num_pages - 1) * tiles +
-                                           cfg->num_kv_heads) * tile_bytes;
+                                           cfg->num_kv_heads) * tile_bytes(*cfg);
   return SPEX_OK;
 }
 
@@ -506,7 +520,7 @@ spex_status_t spex_tree_create(const spex_config_t *cfg, spex_tree_t **out) {
   spex::AttnArgs pools{};
   pools.k_pool = cfg->k_pool;
   pools.v_pool = cfg->v_pool;
-  const bool tiled = spex::has_mfma_kernel(t->shape);
+  const bool tiled = spex::has_mfma_kernel(t->shape) || cfg->kv_dtype == SPEX_MXFP4;
   t->planner.pool = {tiled, !tiled && !spex::has_rowmajor_kernel(t->shape, pools), cfg->head_dim,
                      static_cast<int32_t>(elem_size(cfg->kv_dtype))};
   t->pt = new (std::nothrow) spex::PageTable(cfg->num_pages, cfg->page_size, cfg->free_order);
@@ -571,11 +585,13 @@ static spex_status_t append_step_impl(spex_tree_t *t, spex_node_t node, int32_t 
                                       const void *v, const float *k_scales, const float *v_scales,
                                       void *hip_stream, bool quantise) {
   if (!t || n_tokens < 0 || ((k == nullptr) != (v == nullptr))) return SPEX_ERR_INVALID_ARG;
-  if (quantise && t->cfg.kv_dtype != SPEX_FP8_E4M3) return SPEX_ERR_UNSUPPORTED;
+  const bool mxfp4 = t->cfg.kv_dtype == SPEX_MXFP4;
+  if (quantise ? t->cfg.kv_dtype != SPEX_FP8_E4M3 && !mxfp4 : mxfp4 && k) return SPEX_ERR_UNSUPPORTED;
   if (!t->pt->valid(node)) return SPEX_ERR_BAD_NODE;
   if (t->pt->node(node).n_live_children > 0) return SPEX_ERR_NOT_LEAF;
   if (k && !t->cfg.k_pool) return SPEX_ERR_INVALID_ARG;
   if (n_tokens == 0) return SPEX_OK;
+  if (mxfp4 && k) return spex::mxfp4_calls->append(t, &node, &n_tokens, 1, k, v, hip_stream);
   const int32_t P = t->cfg.page_size;
   const int32_t old_tokens = t->pt->node(node).n_tokens;
   if (static_cast<int64_t>(old_tokens) + n_tokens > INT32_MAX / 2) return SPEX_ERR_UNSUPPORTED;
@@ -636,9 +652,12 @@ static spex_status_t append_tokens_impl(spex_tree_t *t, const spex_node_t *nodes
                                         const float *v_scales, void *hip_stream, bool quantise) {
   if (!t || n_nodes < 0 || (n_nodes > 0 && !nodes) || ((k == nullptr) != (v == nullptr)))
     return SPEX_ERR_INVALID_ARG;
-  if (quantise && t->cfg.kv_dtype != SPEX_FP8_E4M3) return SPEX_ERR_UNSUPPORTED;
+  const bool mxfp4 = t->cfg.kv_dtype == SPEX_MXFP4;
+  if (quantise ? t->cfg.kv_dtype != SPEX_FP8_E4M3 && !mxfp4 : mxfp4 && k) return SPEX_ERR_UNSUPPORTED;
+  if (mxfp4 && (k_scales || v_scales)) return SPEX_ERR_INVALID_ARG;
   if (k && !t->cfg.k_pool) return SPEX_ERR_INVALID_ARG;
   if (n_nodes == 0) return SPEX_OK;
+  if (mxfp4 && k) return spex::mxfp4_calls->append(t, nodes, nullptr, n_nodes, k, v, hip_stream);
   // Check everything before touching the table: the call is all or nothing.
   const int32_t P = t->cfg.page_size;
   int64_t need = 0;
@@ -763,15 +782,17 @@ static spex_status_t decode_attention_impl(spex_tree_t *t, const spex_node_t *le
   if (st != SPEX_OK) return st;
   spex::Plan &pl = t->plan;
   const bool tree_masks = draft_masks != nullptr;
+  const bool mxfp4 = t->cfg.kv_dtype == SPEX_MXFP4, walkable = spex::has_mfma_kernel(t->shape);
+  if (mxfp4 && t->kernel_mode == 1) return SPEX_ERR_UNSUPPORTED;
   bool use_walk = false;
   if (t->kernel_mode == 3) {
-    if (!spex::has_mfma_kernel(t->shape)) return SPEX_ERR_UNSUPPORTED;
+    if (!walkable) return SPEX_ERR_UNSUPPORTED;
     t->planner.ensure_walk(*t->pt, &pl);
     // Draft-tree masks are understood by every kernel but the tree-walk kernel that splits the path
     // (walk_waves 2).
     if (!pl.walk_ok || (tree_masks && pl.walk_waves == 2)) return SPEX_ERR_UNSUPPORTED;
     use_walk = true;
-  } else if (t->kernel_mode == 0 && spex::has_mfma_kernel(t->shape)) {
+  } else if (t->kernel_mode == 0 && walkable) {
     use_walk = t->planner.prefers_walk(*t->pt, &pl);
   }
   ++pl.calls;
@@ -876,7 +897,7 @@ static spex_status_t decode_attention_impl(spex_tree_t *t, const spex_node_t *le
   a.scale_log2 = sm_scale * 1.4426950408889634f;
   a.qt_mask = dp.qt_mask;
   const bool generic =
-      t->kernel_mode == 1 || !(spex::has_mfma_kernel(t->shape) || spex::has_rowmajor_kernel(t->shape, a));
+      !mxfp4 && (t->kernel_mode == 1 || !(spex::has_mfma_kernel(t->shape) || spex::has_rowmajor_kernel(t->shape, a)));
   // Every query token has at least one piece; if none has more, the rows need no merge.
   a.finish = !generic && pl.part_base.size() == pl.qt_limit.size();
 
@@ -893,9 +914,11 @@ static spex_status_t decode_attention_impl(spex_tree_t *t, const spex_node_t *le
   a.part_indptr = dp.part_indptr;
   a.part_base = dp.part_base;
   a.part_hstride = dp.part_hstride;
-  const bool phases = !generic && pl.split_phases && !pl.split_together;
+  const bool phases = !generic && !mxfp4 && pl.split_phases && !pl.split_together;
   HIP_TRY(bracket(0, true));
-  if (generic) {
+  if (mxfp4) {
+    HIP_TRY(spex::mxfp4_calls->split(t->shape, a, il, stream));
+  } else if (generic) {
     for (int k = 0; k < 4; ++k) {
       a.items = il.items[k];
       a.n_items = il.n_items[k];
@@ -989,8 +1012,7 @@ spex_status_t spex_tree_path_kv_bytes(const spex_tree_t *t, spex_node_t node, do
     tokens += t->pt->node(u).n_tokens;
     pages += static_cast<int64_t>(t->pt->node(u).pages.size());
   }
-  double b = static_cast<double>(tokens) * 2.0 * t->cfg.num_kv_heads * t->cfg.head_dim *
-             static_cast<double>(elem_size(t->cfg.kv_dtype));
+  double b = static_cast<double>(tokens) * 2.0 * t->cfg.num_kv_heads * static_cast<double>(token_bytes(t->cfg));
   if (t->cfg.kv_dtype == SPEX_FP8_E4M3) b += static_cast<double>(pages) * 8.0 * t->cfg.num_kv_heads;
   *bytes = b;
   return SPEX_OK;
@@ -1059,6 +1081,10 @@ spex_status_t spex_tree_gather_kv(spex_tree_t *t, spex_node_t node, int32_t firs
   if (!t->cfg.k_pool) return SPEX_ERR_INVALID_ARG;
   const spex::Node &nd = t->pt->node(node);
   if (static_cast<int64_t>(first) + n > nd.n_tokens) return SPEX_ERR_INVALID_ARG;
+  if (t->cfg.kv_dtype == SPEX_MXFP4) {
+    if (k_scale_out || v_scale_out) return SPEX_ERR_INVALID_ARG;
+    return spex::mxfp4_calls->read_back(t, &node, &first, &n, 1, k_out, v_out, nullptr, hip_stream);
+  }
   if (n == 0) return SPEX_OK;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const int32_t P = t->cfg.page_size;

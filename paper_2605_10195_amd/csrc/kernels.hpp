@@ -9,13 +9,13 @@
 
 namespace spex {
 
-enum Dtype : int32_t { kF32 = 0, kBF16 = 1, kFP8 = 2 };
+enum Dtype : int32_t { kF32 = 0, kBF16 = 1, kFP8 = 2, kMXFP4 = 3 };
 
 // Whether a HIP call failed; the error's text is then what spex_last_device_error tells this thread.  In api.cpp.
 bool hip_failed(hipError_t e, const char *what);
 
 // Element arrangement inside a (page, kv head) tile; see the pool layout in spex_tree.h.
-enum Layout : int32_t { kRowMajor = 0, kMfmaTiled = 1 };
+enum Layout : int32_t { kRowMajor = 0, kMfmaTiled = 1, kMxTiled = 2 };
 
 struct Shape {
   int32_t Hq, Hkv, G, D, P;
@@ -143,6 +143,17 @@ struct RotateArgs {
   int32_t patches, n_patches;              // where the patches begin in the lists, and how many there are
 };
 
+// Tokens of many nodes as values (MXFP4 pools).  A record per page that is read: {page id, first slot | slot behind the last << 8, index of
+// the first token in the output}; the lists as those of a rotated append.
+constexpr int kReadInts = 3;
+struct ReadBackArgs {
+  const void *k_pool, *v_pool;
+  void *k_out, *v_out;   // bf16 [tokens][Hkv][D]
+  const int32_t *lists;  // pinned host memory, or null: RotateLists
+  int32_t n_recs;
+  int32_t parts;         // set by launch_mxfp4_read
+};
+
 struct GatherArgs {
   const void *k_pool, *v_pool;
   const float *k_scale, *v_scale;
@@ -174,6 +185,11 @@ hipError_t launch_scatter_quantise(const Shape &sh, const ScatterArgs &a, hipStr
 hipError_t launch_gather(const Shape &sh, const GatherArgs &a, hipStream_t stream);
 hipError_t launch_append_tokens(const Shape &sh, const AppendTokensArgs &a, hipStream_t stream);
 hipError_t launch_append_rotated(const Shape &sh, const RotateArgs &a, const RotateLists &in, hipStream_t stream);
+// MXFP4 pools: the appends (rotary_dim 0: unrotated), and read back.
+hipError_t launch_mxfp4_append(const Shape &sh, const RotateArgs &a, const RotateLists &in, hipStream_t stream);
+hipError_t launch_mxfp4_read(const Shape &sh, const ReadBackArgs &a, const RotateLists &in, hipStream_t stream);
+// Attention over MXFP4 pools, in mxfp4_attention.hip.
+hipError_t launch_mxfp4_split(const Shape &sh, const AttnArgs &a, const ItemLists &lists, hipStream_t stream);
 // blob[pairs[2i]] = pairs[2i+1] for i < n (all DEVICE): patches the device copy of a plan.
 hipError_t launch_patch(int32_t *blob, const int32_t *pairs, int32_t n, hipStream_t stream);
 // Tree-walk kernel; ntw in {1, 2, 4} = 16-row tiles per wavefront and waves in {2, 4, 8} = wavefronts

@@ -24,10 +24,9 @@ spex_status_t upload_rotation(spex_tree *t, hipStream_t stream) {
   return SPEX_OK;
 }
 
+// rotary_dim: the handle's, or 0: nothing is rotated, and positions are not asked for.
 spex_status_t append_rotated_impl(spex_tree_t *t, const spex_node_t *nodes, const int32_t *counts, int32_t n_nodes, const int32_t *positions,
-                                  const spex_rotated_t *data, void *hip_stream) {
-  if (!t || !data || n_nodes < 0 || (n_nodes > 0 && !nodes)) return SPEX_ERR_INVALID_ARG;
-  if (!t->cfg.k_pool || t->rotary_dim == 0) return SPEX_ERR_INVALID_ARG;
+                                  const spex_rotated_t *data, int32_t rotary_dim, void *hip_stream) {
   const bool fp8 = t->cfg.kv_dtype == SPEX_FP8_E4M3;
   if ((data->q == nullptr) != (data->q_out == nullptr) || (data->k_scales == nullptr) != (data->v_scales == nullptr) ||
       (data->k_scales && !fp8))
@@ -80,7 +79,7 @@ spex_status_t append_rotated_impl(spex_tree_t *t, const spex_node_t *nodes, cons
   if (need > t->pt->free_pages()) return SPEX_ERR_OOM_PAGES;
   // Tokens before each node's own: nodes of a list are mostly siblings, so the last parent's sum is kept.
   std::vector<int32_t> before(positions ? 0 : static_cast<size_t>(n_nodes));
-  if (!positions) {
+  if (!positions && rotary_dim > 0) {
     int32_t parent = spex::kNoNode;
     int64_t sum = 0;
     for (int32_t i = 0; i < n_nodes; ++i) {
@@ -99,8 +98,10 @@ spex_status_t append_rotated_impl(spex_tree_t *t, const spex_node_t *nodes, cons
     for (int32_t i = 0; i < n_nodes; ++i) t->pt->reserve(nodes[i], counts ? counts[i] : 1);
 
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const spex_status_t us = upload_rotation(t, stream);
-  if (us != SPEX_OK) return us;
+  if (rotary_dim > 0) {
+    const spex_status_t us = upload_rotation(t, stream);
+    if (us != SPEX_OK) return us;
+  }
   // The lists go into the kernel arguments if they fit, with some room for length patches of the cached plan, and else into
   // the ring, with room for 32 patches a node as in append_tokens_impl.  A call through the ring takes 5 us more on the host (an event
   // behind the kernel; 140 and 141 nodes of one token: 5.1 / 10.2) and 1.3 on the GPU (records read over the bus; 32/8/128: 6.7 / 8.0).
@@ -162,7 +163,7 @@ spex_status_t append_rotated_impl(spex_tree_t *t, const spex_node_t *nodes, cons
   a.lists = ring ? h : nullptr;
   a.has_positions = positions != nullptr;
   a.n_recs = static_cast<int32_t>(visits);
-  a.rotary_dim = t->rotary_dim;
+  a.rotary_dim = rotary_dim;
   a.interleaved = t->interleaved;
   a.most_tokens = most;
   a.plan = static_cast<int32_t *>(t->d_plan);
@@ -173,6 +174,22 @@ spex_status_t append_rotated_impl(spex_tree_t *t, const spex_node_t *nodes, cons
 }
 
 }  // namespace
+
+namespace spex {
+
+spex_status_t append_quantised(spex_tree *t, const spex_node_t *nodes, const int32_t *counts, int32_t n_nodes, const void *k, const void *v,
+                               void *hip_stream) {
+  spex_rotated_t data{};
+  data.k = k;
+  data.v = v;
+  try {
+    return append_rotated_impl(t, nodes, counts, n_nodes, nullptr, &data, 0, hip_stream);
+  } catch (const std::bad_alloc &) {
+    return SPEX_ERR_CAPACITY;
+  }
+}
+
+}  // namespace spex
 
 extern "C" {
 
@@ -195,8 +212,10 @@ spex_status_t spex_tree_set_rotation(spex_tree_t *t, int32_t rotary_dim, const d
 
 spex_status_t spex_tree_append_rotated(spex_tree_t *t, const spex_node_t *nodes, const int32_t *counts, int32_t n_nodes,
                                        const int32_t *positions, const spex_rotated_t *data, void *hip_stream) {
+  if (!t || !data || n_nodes < 0 || (n_nodes > 0 && !nodes)) return SPEX_ERR_INVALID_ARG;
+  if (!t->cfg.k_pool || t->rotary_dim == 0) return SPEX_ERR_INVALID_ARG;
   try {
-    return append_rotated_impl(t, nodes, counts, n_nodes, positions, data, hip_stream);
+    return append_rotated_impl(t, nodes, counts, n_nodes, positions, data, t->rotary_dim, hip_stream);
   } catch (const std::bad_alloc &) {
     return SPEX_ERR_CAPACITY;
   }

@@ -100,5 +100,18 @@ spex_status_t ring_commit(spex_tree *t, size_t bytes, hipStream_t stream);
 // Behind an append to the page table, in api.cpp: the cached plan's patches as {index, value} pairs for the append's launch, at most
 // `room` of them (0 where there are none, or more).
 size_t follow_append(spex_tree *t, int32_t *pairs, size_t room);
+// The quantising appends of MXFP4 pools, in rotated_append.cpp: dense bf16 k and v.  t, nodes and n_nodes >= 0 have been checked.
+spex_status_t append_quantised(spex_tree *t, const spex_node_t *nodes, const int32_t *counts, int32_t n_nodes, const void *k, const void *v,
+                               void *hip_stream);
+
+// What the calls of api.cpp go through on MXFP4 pools.  mxfp4.cpp sets it; a program linked without that file has no such pools.
+struct Mxfp4Calls {
+  spex_status_t (*append)(spex_tree *t, const spex_node_t *nodes, const int32_t *counts, int32_t n_nodes, const void *k, const void *v,
+                          void *hip_stream);
+  spex_status_t (*read_back)(spex_tree *t, const spex_node_t *nodes, const int32_t *firsts, const int32_t *counts, int32_t n_nodes,
+                             void *k_out, void *v_out, int64_t *n_tokens, void *hip_stream);
+  hipError_t (*split)(const Shape &sh, const AttnArgs &a, const ItemLists &lists, hipStream_t stream);
+};
+extern const Mxfp4Calls *mxfp4_calls;
 
 }  // namespace spex
