@@ -782,7 +782,7 @@ static spex_status_t decode_attention_impl(spex_tree_t *t, const spex_node_t *le
   if (st != SPEX_OK) return st;
   spex::Plan &pl = t->plan;
   const bool tree_masks = draft_masks != nullptr;
-  const bool mxfp4 = t->cfg.kv_dtype == SPEX_MXFP4, walkable = spex::has_mfma_kernel(t->shape);
+  const bool mxfp4 = t->cfg.kv_dtype == SPEX_MXFP4, walkable = mxfp4 || spex::has_mfma_kernel(t->shape);
   if (mxfp4 && t->kernel_mode == 1) return SPEX_ERR_UNSUPPORTED;
   bool use_walk = false;
   if (t->kernel_mode == 3) {
@@ -856,8 +856,9 @@ static spex_status_t decode_attention_impl(spex_tree_t *t, const spex_node_t *le
     wa.qt_mask = dp.qt_mask;
     wa.cut = pl.walk_cut;
     HIP_TRY(bracket(3, true));
-    HIP_TRY(spex::launch_tree_walk(t->shape, wa, pl.walk_row_tiles, pl.walk_waves, pl.walk_halves,
-                                   pl.walk_by_tile, stream));
+    HIP_TRY(mxfp4 ? spex::mxfp4_calls->walk(t->shape, wa, pl.walk_row_tiles, pl.walk_waves, stream)
+                  : spex::launch_tree_walk(t->shape, wa, pl.walk_row_tiles, pl.walk_waves, pl.walk_halves,
+                                           pl.walk_by_tile, stream));
     HIP_TRY(bracket(3, false));
     t->info[0] = pl.unique_tokens;
     t->info[1] = pl.prefix_tokens;

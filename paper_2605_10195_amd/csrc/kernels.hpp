@@ -190,6 +190,8 @@ hipError_t launch_mxfp4_append(const Shape &sh, const RotateArgs &a, const Rotat
 hipError_t launch_mxfp4_read(const Shape &sh, const ReadBackArgs &a, const RotateLists &in, hipStream_t stream);
 // Attention over MXFP4 pools, in mxfp4_attention.hip.
 hipError_t launch_mxfp4_split(const Shape &sh, const AttnArgs &a, const ItemLists &lists, hipStream_t stream);
+// ntw and waves: of the lists, as for launch_tree_walk.
+hipError_t launch_mxfp4_walk(const Shape &sh, const WalkArgs &a, int ntw, int waves, hipStream_t stream);
 // blob[pairs[2i]] = pairs[2i+1] for i < n (all DEVICE): patches the device copy of a plan.
 hipError_t launch_patch(int32_t *blob, const int32_t *pairs, int32_t n, hipStream_t stream);
 // Tree-walk kernel; ntw in {1, 2, 4} = 16-row tiles per wavefront and waves in {2, 4, 8} = wavefronts

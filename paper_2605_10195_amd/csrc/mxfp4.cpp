@@ -70,7 +70,7 @@ spex_status_t read_back(spex_tree_t *t, const spex_node_t *nodes, const int32_t 
   }
 }
 
-const spex::Mxfp4Calls kCalls = {spex::append_quantised, read_back, spex::launch_mxfp4_split};
+const spex::Mxfp4Calls kCalls = {spex::append_quantised, read_back, spex::launch_mxfp4_split, spex::launch_mxfp4_walk};
 const bool kKnown = (spex::mxfp4_calls = &kCalls, true);
 
 }  // namespace

@@ -3,6 +3,9 @@
 //   spex_mxfp4_split_kernel
 //       The split path's items, a workgroup for up to 16 NT rows of one: its four wavefronts take every fourth block of 32 tokens
 //       and join their softmax states through LDS.  Partial states go to the merge kernel, as for the other pools.
+//   spex_mxfp4_walk_kernel
+//       The tree walk: the same over the whole path of up to 16 NT rows, from the root to the requested nodes.  Nothing but finished
+//       rows is written.
 //
 // Mathematics: S^T = K Q^T, p = 2^(c S^T - m), l += sum p, O^T += V^T P^T, out = O / l, with keys and values code * 2^E.
 // Keys become bf16 operands, which hold code * 2^E exactly (two significant bits), values fp16, which do as well since the values' E is
@@ -368,68 +371,128 @@ __device__ __forceinline__ void join_rows(MxRows<M, NT> &st, int ks, float c, fl
   }
 }
 
-// Walks the blocks that next() gives: one is worked on while the next is on its way, in registers of its own.
-template <int M, int NT, bool TREE, class Next>
-__device__ __forceinline__ void walk_blocks(MxRows<M, NT> &st, const char *kpool, const char *vpool, int page_tiles, int g, int row0, float c,
-                                            Next next) {
+constexpr int kWaves = 4;  // of a workgroup: they hold the same rows
+
+// The blocks of wavefront w of a workgroup: records w, w + 4, .. of a list, 64 of them at a time in registers, a lane each.
+// read(i): record i, for a lane; lanes whose record does not concern the wavefront's rows drop out.
+struct MxLanes {
+  int pid_a, vp_a, pid_b, vp_b, rows, flags;
+};
+template <class Read>
+struct MxSource {
+  Read read;
+  int n, at;
+  uint64_t left;
+  MxLanes r;
+  __device__ __forceinline__ MxBlock next() {
+    while (left == 0 && at < n) {
+      const int i = at + kWaves * (threadIdx.x & 63);
+      bool concerns = i < n;
+      if (concerns) concerns = read(i, r);
+      left = __ballot(concerns);
+      at += 64 * kWaves;
+    }
+    MxBlock b;
+    b.live = left != 0;
+    const int l = b.live ? __builtin_ctzll(left) : 0;
+    left &= left - 1;
+    b.pid_a = __builtin_amdgcn_readlane(r.pid_a, l);
+    b.vp_a = __builtin_amdgcn_readlane(r.vp_a, l);
+    b.pid_b = __builtin_amdgcn_readlane(r.pid_b, l);
+    b.vp_b = __builtin_amdgcn_readlane(r.vp_b, l);
+    const int rows = __builtin_amdgcn_readlane(r.rows, l);
+    b.lo = rows & 0xffff;
+    b.hi = static_cast<int>(static_cast<uint32_t>(rows) >> 16);
+    b.masked = __builtin_amdgcn_readlane(r.flags, l) & 1;
+    return b;
+  }
+};
+
+// One block is worked on while the next is on its way, in registers of its own.
+template <int M, int NT, bool TREE, class Read>
+__device__ __forceinline__ void walk_blocks(MxRows<M, NT> &st, const void *k, const void *v, int page_tiles, int g, int row0, float c, int n, int w,
+                                            Read read) {
+  const char *kpool = static_cast<const char *>(k), *vpool = static_cast<const char *>(v);
   const float slack = kSlackLog2 / c;
+  MxSource<Read> src{read, n, w, 0, {}};
   MxRaw<M> x0, x1;
-  MxBlock b0 = next();
+  MxBlock b0 = src.next();
   load_block<M>(x0, b0, kpool, vpool, page_tiles, g);
-  MxBlock b1 = next();
+  MxBlock b1 = src.next();
   load_block<M>(x1, b1, kpool, vpool, page_tiles, g);
   while (b0.live) {
     block_step<M, NT, TREE>(st, x0, b0, row0, c, slack);
-    b0 = next();
+    b0 = src.next();
     load_block<M>(x0, b0, kpool, vpool, page_tiles, g);
     if (!b1.live) break;
     block_step<M, NT, TREE>(st, x1, b1, row0, c, slack);
-    b1 = next();
+    b1 = src.next();
     load_block<M>(x1, b1, kpool, vpool, page_tiles, g);
   }
 }
 
+// Wavefronts a SIMD: with one the compiler keeps accumulators in the other half of the register file and moves them for every block.
+constexpr int mx_occupancy(int blocks, int row_tiles) { return blocks * row_tiles <= 4 ? 3 : 2; }
+
 template <int M, int NT, bool TREE>
-__global__ __launch_bounds__(256) void spex_mxfp4_split_kernel(AttnArgs p, Shape sh, SplitLists ls) {
-  constexpr int kWaves = 4;
+__global__ __launch_bounds__(64 * kWaves, mx_occupancy(M, NT)) void spex_mxfp4_split_kernel(AttnArgs p, Shape sh, SplitLists ls) {
   __shared__ __attribute__((aligned(16))) float lds[MxJoin<M, NT>::floats(kWaves)];
   const ListPos at = list_of(ls, static_cast<int>(blockIdx.x));
   const int tile = at.local / at.n_items;
   Item cur = load_item(at.items, at.local - tile * at.n_items);
   cur.row0 += tile * 16 * NT;
-  const int rows = cur.qt_count * sh.G;
-  // whole workgroup: padding item, no such tile, or one of the next span
-  if (cur.pg_count == 0 || cur.row0 >= rows || tile * 16 * NT >= at.span) return;
+  const int G = sh.G, rows = cur.qt_count * G;
+  if (cur.pg_count == 0 || cur.row0 >= rows) return;  // whole workgroup: padding item, or no such tile
   const int w = uniform(threadIdx.x >> 6), g = cur.g;
   const float c = p.scale_log2;
   MxRows<M, NT> st;
   load_rows<M, NT, TREE>(st, p.q, p.qt_rec, p.qt_mask, cur.qt_begin, cur.row0, rows, g, sh, c);
-  const int nblk = (cur.pg_count + 1) >> 1;
-  int i = w;
-  auto next = [&]() {
-    MxBlock b;
-    b.live = i < nblk;
-    const int a = cur.pg_begin + 2 * (b.live ? i : nblk - 1);
-    const bool has_b = a + 1 < cur.pg_begin + cur.pg_count;
-    const int at_b = has_b ? a + 1 : a;
-    b.pid_a = sload(p.pg_rec, 2 * static_cast<int64_t>(a));
-    b.vp_a = sload(p.pg_rec, 2 * static_cast<int64_t>(a) + 1);
-    b.pid_b = sload(p.pg_rec, 2 * static_cast<int64_t>(at_b));
-    b.vp_b = has_b ? sload(p.pg_rec, 2 * static_cast<int64_t>(at_b) + 1) : 0;
-    b.lo = 0;
-    b.hi = INT_MAX;
-    b.masked = (cur.flags & 1) != 0 || !has_b;
-    b.live = b.live && (b.vp_a >> 7) < st.seen_end;  // blocks follow each other along the path: behind one that no row sees there is none
-    i += kWaves;
-    return b;
-  };
-  walk_blocks<M, NT, TREE>(st, static_cast<const char *>(p.k_pool), static_cast<const char *>(p.v_pool), sh.page_tiles, g, 0, c, next);
-  const int G = sh.G;
+  walk_blocks<M, NT, TREE>(st, p.k_pool, p.v_pool, sh.page_tiles, g, 0, c, (cur.pg_count + 1) >> 1, w, [&](int i, MxLanes &r) {
+    const int2 *pages = reinterpret_cast<const int2 *>(p.pg_rec) + cur.pg_begin + 2 * i;
+    const bool has_b = 2 * i + 1 < cur.pg_count;
+    const int2 a = pages[0], b = pages[has_b ? 1 : 0];
+    r = {a.x, a.y, b.x, has_b ? b.y : 0, static_cast<int>(0xffff0000u), cur.flags | (has_b ? 0 : 1)};
+    return (a.y >> 7) < st.seen_end;
+  });
   join_rows<M, NT, kWaves>(st, w, c, lds, p.finish ? p.out : p.part_o, p.finish ? nullptr : p.part_ml, p.lse, [&](int nt, int row) {
     const int r = cur.row0 + 16 * nt + row;
     if (r >= rows) return static_cast<int64_t>(-1);
     return p.finish ? static_cast<int64_t>(st.qtok[nt]) * sh.Hq + g * G + r % G
                     : static_cast<int64_t>(cur.pbase) + static_cast<int64_t>(g) * rows + r;
+  });
+}
+
+// One workgroup for each set of 16 NT rows of the row blocks' NW wavefronts of 16 ntw.  The sets of a row block read its shared blocks
+// one beside the other: they are eight workgroups apart, which is one XCD.
+template <int M, int NT, bool TREE>
+__global__ __launch_bounds__(64 * kWaves, mx_occupancy(M, NT)) void spex_mxfp4_walk_kernel(WalkArgs p, Shape sh, int nw, int ntw) {
+  __shared__ __attribute__((aligned(16))) float lds[MxJoin<M, NT>::floats(kWaves)];
+  const int groups = ntw / NT, sets = nw * groups;
+  const int batch = static_cast<int>(blockIdx.x) / (8 * sets), within = static_cast<int>(blockIdx.x) - batch * 8 * sets;
+  const int set = within >> 3, item = batch * 8 + (within & 7);
+  if (item >= p.n_items) return;
+  const int rw = set / groups, row_base = (set - rw * groups) * 16 * NT;
+  const int64_t ir = static_cast<int64_t>(item) * (nw <= 4 ? 16 : 32);
+  const int rows = sload(p.items, ir + 3 + 2 * nw + rw) * sh.G;
+  if (row_base >= rows) return;  // padding, a wavefront without rows, or no such tile
+  const int g = sload(p.items, ir), blk_begin = sload(p.items, ir + 1), n_shared = sload(p.items, ir + 2);
+  // per wavefront: private blocks | room << 16
+  const int n_priv = sload(p.items, ir + 3 + rw) & 0xffff;
+  int priv_begin = blk_begin + n_shared;
+  for (int v = 0; v < rw; ++v) priv_begin += static_cast<int>(static_cast<uint32_t>(sload(p.items, ir + 3 + v)) >> 16);
+  const int row0 = rw * 16 * ntw + row_base, qt_begin = sload(p.items, ir + 3 + nw + rw), G = sh.G, w = uniform(threadIdx.x >> 6);
+  const float c = p.scale_log2;
+  MxRows<M, NT> st;
+  load_rows<M, NT, TREE>(st, p.q, p.qt_rec, p.qt_mask, qt_begin, row_base, rows, g, sh, c);
+  walk_blocks<M, NT, TREE>(st, p.k_pool, p.v_pool, sh.page_tiles, g, row0, c, n_shared + n_priv, w, [&](int i, MxLanes &r) {
+    const u32x4 *rec = reinterpret_cast<const u32x4 *>(p.blocks) + 2 * static_cast<int64_t>(i < n_shared ? blk_begin + i : priv_begin + i - n_shared);
+    const u32x4 a = rec[0], b = rec[1];
+    r = {static_cast<int>(a[0]), static_cast<int>(a[1]), static_cast<int>(a[2]), static_cast<int>(a[3]), static_cast<int>(b[0]), static_cast<int>(b[1])};
+    return static_cast<int>(b[0] & 0xffffu) < row0 + 16 * NT && static_cast<int>(b[0] >> 16) > row0 && (r.vp_a >> 7) < st.seen_end;
+  });
+  join_rows<M, NT, kWaves>(st, w, c, lds, p.out, nullptr, p.lse, [&](int nt, int row) {
+    const int r = row_base + 16 * nt + row;
+    return r < rows ? static_cast<int64_t>(st.qtok[nt]) * sh.Hq + g * G + r % G : static_cast<int64_t>(-1);
   });
 }
 
@@ -449,17 +512,32 @@ hipError_t with_blocks(int head_dim, F f) {
   return hipErrorInvalidValue;
 }
 
+// Row tiles of a workgroup: two where there are rows for them; wide heads have registers for one.
+constexpr int mx_row_tiles(int blocks) { return blocks <= 4 ? 2 : 1; }
+
 template <int M, int NT>
 hipError_t launch_split(const Shape &sh, const AttnArgs &a, const ItemLists &l, hipStream_t stream) {
   int64_t n_wg = 0;
   const SplitLists ls = make_lists(l, 16 * NT, &n_wg);
   if (n_wg < 0) return hipErrorInvalidValue;
   if (n_wg == 0) return hipSuccess;
-  const dim3 grid(static_cast<unsigned>(n_wg)), block(256);
+  const dim3 grid(static_cast<unsigned>(n_wg)), block(64 * kWaves);
   if (a.qt_mask)
     hipLaunchKernelGGL((spex_mxfp4_split_kernel<M, NT, true>), grid, block, 0, stream, a, sh, ls);
   else
     hipLaunchKernelGGL((spex_mxfp4_split_kernel<M, NT, false>), grid, block, 0, stream, a, sh, ls);
+  return hipGetLastError();
+}
+
+template <int M, int NT>
+hipError_t launch_walk(const Shape &sh, const WalkArgs &a, int ntw, int waves, hipStream_t stream) {
+  const int64_t n_wg = (static_cast<int64_t>(a.n_items) + 7) / 8 * 8 * waves * (ntw / NT);
+  if (n_wg > INT32_MAX) return hipErrorInvalidValue;
+  const dim3 grid(static_cast<unsigned>(n_wg)), block(64 * kWaves);
+  if (a.qt_mask)
+    hipLaunchKernelGGL((spex_mxfp4_walk_kernel<M, NT, true>), grid, block, 0, stream, a, sh, waves, ntw);
+  else
+    hipLaunchKernelGGL((spex_mxfp4_walk_kernel<M, NT, false>), grid, block, 0, stream, a, sh, waves, ntw);
   return hipGetLastError();
 }
 
@@ -468,7 +546,17 @@ hipError_t launch_split(const Shape &sh, const AttnArgs &a, const ItemLists &l, 
 hipError_t launch_mxfp4_split(const Shape &sh, const AttnArgs &a, const ItemLists &l, hipStream_t stream) {
   return with_blocks(sh.D, [&](auto m) {
     constexpr int M = decltype(m)::value;
-    return std::max({l.span[0], l.span[1], l.span[2], l.span[3]}) <= 16 ? launch_split<M, 1>(sh, a, l, stream) : launch_split<M, 2>(sh, a, l, stream);
+    return std::max({l.span[0], l.span[1], l.span[2], l.span[3]}) <= 16 ? launch_split<M, 1>(sh, a, l, stream)
+                                                                       : launch_split<M, mx_row_tiles(M)>(sh, a, l, stream);
+  });
+}
+
+hipError_t launch_mxfp4_walk(const Shape &sh, const WalkArgs &a, int ntw, int waves, hipStream_t stream) {
+  if (a.n_items <= 0) return hipSuccess;
+  if ((ntw != 1 && ntw != 2 && ntw != 4) || (waves != 2 && waves != 4 && waves != 8)) return hipErrorInvalidValue;
+  return with_blocks(sh.D, [&](auto m) {
+    constexpr int M = decltype(m)::value;
+    return ntw == 1 ? launch_walk<M, 1>(sh, a, ntw, waves, stream) : launch_walk<M, mx_row_tiles(M)>(sh, a, ntw, waves, stream);
   });
 }
 

@@ -111,6 +111,7 @@ struct Mxfp4Calls {
   spex_status_t (*read_back)(spex_tree *t, const spex_node_t *nodes, const int32_t *firsts, const int32_t *counts, int32_t n_nodes,
                              void *k_out, void *v_out, int64_t *n_tokens, void *hip_stream);
   hipError_t (*split)(const Shape &sh, const AttnArgs &a, const ItemLists &lists, hipStream_t stream);
+  hipError_t (*walk)(const Shape &sh, const WalkArgs &a, int ntw, int waves, hipStream_t stream);
 };
 extern const Mxfp4Calls *mxfp4_calls;
 

@@ -93,13 +93,13 @@ def bushy(rng, roots, depth, fan, longest):
     return nodes, leaves
 
 
-MODES = [0, 2]
+MODES = [0, 2, 3]
 
 
 @pytest.mark.parametrize("mode", MODES)
 @pytest.mark.parametrize("heads", HEADS)
 def test_trees(heads, mode):
-    """Every head size and grouping: shared nodes, empty nodes, pages that end anywhere."""
+    """Every head size and grouping, in both kernel sets: shared nodes, empty nodes, pages that end anywhere."""
     rng = np.random.default_rng(heads[0] + heads[2])
     nodes, leaves = bushy(rng, 2, 3, 3, 70)
     f = Forest(heads, nodes, seed=heads[2], kernel_mode=mode)
@@ -141,6 +141,20 @@ def test_draft_trees(heads, mode):
     chain = np.concatenate([(1 << np.arange(1, n + 1)) - 1 for n in lens]).astype(np.uint32)
     f.check([1, 2, 3, 4], lens, chain)
     f.check([1, 2, 3, 4], lens, np.concatenate([1 << np.arange(n) for n in lens]).astype(np.uint32))
+    f.tree.close()
+
+
+@pytest.mark.parametrize("waves", [2, 4, 8])
+@pytest.mark.parametrize("tiles", [1, 2, 4])
+@pytest.mark.parametrize("heads", [(8, 2, 128), (16, 1, 64), (6, 3, 96)])
+def test_walk_shapes(heads, tiles, waves):
+    """Every shape of the tree walk that can be asked for."""
+    if waves == 2 and tiles == 4:
+        pytest.skip("no such lists")
+    rng = np.random.default_rng(7)
+    nodes, leaves = bushy(rng, 3, 2, 5, 90)
+    f = Forest(heads, nodes, seed=9, kernel_mode=3, walk_row_tiles=tiles, walk_waves=waves)
+    f.check(leaves)
     f.tree.close()
 
 
