@@ -78,10 +78,12 @@ typedef enum { SPEX_F32 = 0, SPEX_BF16 = 1, SPEX_FP8_E4M3 = 2, SPEX_MXFP4 = 3 /*
  *     a number is the nearest to x * 2^-E, ties to the one whose last bit is 0, at most 6 in magnitude.  So a key or value
  *     is off by at most 2 * 2^E, a value of V beyond 49152 is held as 49152, one of 2^-25 or less may be held as 0.
  *     A tile is 17 * head_dim / 2 bytes: with M = head_dim / 32, 256 M bytes of codes, two dims to a byte (the even one in the low
- *     half), and 16 M bytes E + 127, [block][token].  Offsets of the codes, a word being 4 bytes:
- *     K: dims 8 u .. 8 u + 7 of token t are word s of lane 16 j + t, V: dims 2 u, 2 u + 1 of token t are byte t % 4 of word i of
- *     lane 16 (t / 4) + c; word w of lane l lies at 4 (l M + w).  M a power of two: j = u / M, s = u % M (K), c = u / M,
- *     i = u % M (V); else j = u % 4, s = u / 4, c = u % 16, i = u / 16.
+ *     half), and 16 M bytes E + 127.  Byte offsets:
+ *     K codes, dims 8 u .. 8 u + 7 of token t, a word:      4 ((16 j + t) M + s)
+ *     V codes, dims 2 u, 2 u + 1 of token t, a byte:        4 (((16 ((t / 4) % 2) + c) 2 + t / 8) M + i) + t % 4
+ *     K scale of block b, token t:                          256 M + 16 b + t
+ *     V scale of block b, token t:                          256 M + 16 b + 8 ((t / 4) % 2) + 4 (t / 8) + t % 4
+ *     with M a power of two: j = u / M, s = u % M (K), c = u / M, i = u % M (V); else j = u % 4, s = u / 4, c = u % 16, i = u / 16.
  *     k_scale and v_scale must be NULL.
  *
  * fp8 (OCP e4m3fn): value = code * scale, one fp32 scale per (page, kv head), separately
@@ -102,8 +104,9 @@ typedef enum { SPEX_F32 = 0, SPEX_BF16 = 1, SPEX_FP8_E4M3 = 2, SPEX_MXFP4 = 3 /*
  *   - code * v_scale is formed in half precision in two steps (the power of two of the scale,
  *     then its mantissa rounded to 11 bits): relative error at most 2^-10, and for a magnitude
  *     below 2^-14 an absolute error below 2^-23;
- * the other kernels of an fp8 pool reproduce code * v_scale exactly.  Attention over an MXFP4 pool takes its values as they are.  Row-major pools (fp32, other
- * page sizes and head dims) hold and return V as given.  Inside the range every kernel meets the
+ * the other kernels of an fp8 pool reproduce code * v_scale exactly.  Attention over an MXFP4 pool
+ * takes its values as they are.  Row-major pools (fp32, other page sizes and head dims) hold and
+ * return V as given.  Inside the range every kernel meets the
  * same error bound.
  */
 typedef struct {

@@ -152,7 +152,7 @@ spex_status_t make_plan(spex_tree *t, const int32_t *leaves, const int32_t *q_le
   return st;
 }
 
-constexpr int kPlanArrays = 14;
+constexpr int kPlanArrays = 16;
 // The lists of a plan in the order in which they lie in its device copy.  Only those of the kernel set
 // that runs: a request that the automatic choice moved has the tree-walk lists of the comparison
 // too, and both together may not fit where one set does.
@@ -164,16 +164,16 @@ struct PlanArrays {
     const std::vector<int32_t> *all[kPlanArrays] = {
         &pl.prefix_items, &pl.suffix_items, &pl.pg_rec, &pl.qt_rec,
         &pl.part_indptr, &pl.part_base,    &pl.part_hstride, &pl.merge_qt, &pl.coop_items[0], &pl.coop_items[1],
-        &pl.walk_items, &pl.walk_blocks, &pl.walk_qt, &pl.qt_mask};
+        &pl.walk_items, &pl.walk_blocks, &pl.walk_qt, &pl.qt_mask, &pl.walk_pieces, &pl.walk_merges};
     if (pl.merge_stride > 0) {  // the pieces' records in place of the arrays they are made of
       all[4] = &pl.merge_rec;
       all[5] = all[6] = &none;
     }
     for (int i = 0; i < kPlanArrays; ++i) {
-      const bool both = i == kPlanArrays - 1, of_walk = i >= 10;
+      const bool both = i == 13, of_walk = i >= 10;
       a[i] = both || of_walk == walk ? all[i] : &none;
       off[i] = total;
-      total += align_up(a[i]->size() * sizeof(int32_t) + 16, 256);
+      if (i < 14 || !a[i]->empty()) total += align_up(a[i]->size() * sizeof(int32_t) + 16, 256);
     }
   }
   void copy_to(char *dst) const {
@@ -196,6 +196,8 @@ struct PlanArrays {
     dp.walk_blocks = ptr(11);
     dp.walk_qt = ptr(12);
     dp.qt_mask = a[13]->empty() ? nullptr : ptr(13);
+    dp.walk_pieces = ptr(14);
+    dp.walk_merges = ptr(15);
     return dp;
   }
 };
@@ -522,7 +524,7 @@ spex_status_t spex_tree_create(const spex_config_t *cfg, spex_tree_t **out) {
   pools.v_pool = cfg->v_pool;
   const bool tiled = spex::has_mfma_kernel(t->shape) || cfg->kv_dtype == SPEX_MXFP4;
   t->planner.pool = {tiled, !tiled && !spex::has_rowmajor_kernel(t->shape, pools), cfg->head_dim,
-                     static_cast<int32_t>(elem_size(cfg->kv_dtype))};
+                     static_cast<int32_t>(elem_size(cfg->kv_dtype)), cfg->kv_dtype == SPEX_MXFP4};
   t->pt = new (std::nothrow) spex::PageTable(cfg->num_pages, cfg->page_size, cfg->free_order);
   if (!t->pt) {
     delete t;
@@ -800,6 +802,7 @@ static spex_status_t decode_attention_impl(spex_tree_t *t, const spex_node_t *le
     const spex_status_t ss = plan_status(t, t->planner.ensure_split(*t->pt, &pl));
     if (ss != SPEX_OK) return ss;
   }
+  const int64_t partial_rows = use_walk ? pl.walk_partial_rows : pl.n_partial_rows;
   unsigned char *sbase = nullptr;
   DevicePlan static_dp;
   if (use_static) {
@@ -807,8 +810,7 @@ static spex_status_t decode_attention_impl(spex_tree_t *t, const spex_node_t *le
     // every call: another handle's call may have overwritten it), partial results follow them
     // there, and no events are made.  The handle's own device copy, if any, and the patches that
     // wait for it are left as they are.
-    if (!use_walk && align_up(static_cast<size_t>(pl.n_partial_rows) * t->cfg.head_dim * 4, 256) +
-                             static_cast<size_t>(pl.n_partial_rows) * 8 > kStaticPartBytes)
+    if (align_up(static_cast<size_t>(partial_rows) * t->cfg.head_dim * 4, 256) + static_cast<size_t>(partial_rows) * 8 > kStaticPartBytes)
       return SPEX_ERR_CAPACITY;
     const spex_status_t gs = static_scratch(&sbase);
     if (gs != SPEX_OK) return gs;
@@ -839,6 +841,18 @@ static spex_status_t decode_attention_impl(spex_tree_t *t, const spex_node_t *le
     return hipEventRecord(slot->ev[2 * which + (begin ? 0 : 1)], stream);
   };
 
+  float *part_o = nullptr, *part_ml = nullptr;
+  if (use_static) {
+    part_o = reinterpret_cast<float *>(sbase + kStaticPlanBytes);
+    part_ml = reinterpret_cast<float *>(
+        sbase + kStaticPlanBytes + align_up(static_cast<size_t>(partial_rows) * t->cfg.head_dim * 4, 256));
+  } else if (partial_rows > 0) {
+    const spex_status_t ps = ensure_partials(t, partial_rows);
+    if (ps != SPEX_OK) return ps;
+    part_o = t->d_part_o;
+    part_ml = t->d_part_ml;
+  }
+
   if (use_walk) {
     spex::WalkArgs wa{};
     wa.k_pool = t->cfg.k_pool;
@@ -855,6 +869,12 @@ static spex_status_t decode_attention_impl(spex_tree_t *t, const spex_node_t *le
     wa.scale_log2 = sm_scale * 1.4426950408889634f;
     wa.qt_mask = dp.qt_mask;
     wa.cut = pl.walk_cut;
+    wa.pieces = dp.walk_pieces;
+    wa.merges = dp.walk_merges;
+    wa.n_pieces = static_cast<int32_t>(pl.walk_pieces.size() / spex::Plan::kPieceInts);
+    wa.n_merges = static_cast<int32_t>(pl.walk_merges.size() / spex::Plan::kMergeInts);
+    wa.part_o = part_o;
+    wa.part_ml = part_ml;
     HIP_TRY(bracket(3, true));
     HIP_TRY(mxfp4 ? spex::mxfp4_calls->walk(t->shape, wa, pl.walk_row_tiles, pl.walk_waves, stream)
                   : spex::launch_tree_walk(t->shape, wa, pl.walk_row_tiles, pl.walk_waves, pl.walk_halves,
@@ -865,22 +885,10 @@ static spex_status_t decode_attention_impl(spex_tree_t *t, const spex_node_t *le
     t->info[2] = pl.suffix_tokens;
     t->info[3] = pl.walk_real_items;
     t->info[4] = pl.walk_block_visits;
-    t->info[5] = 0;
+    t->info[5] = partial_rows;
     t->info[6] = plan_state;
     t->info[7] = pl.walk_row_tiles + 256 * pl.walk_waves;
     return SPEX_OK;
-  }
-
-  float *part_o = nullptr, *part_ml = nullptr;
-  if (use_static) {
-    part_o = reinterpret_cast<float *>(sbase + kStaticPlanBytes);
-    part_ml = reinterpret_cast<float *>(
-        sbase + kStaticPlanBytes + align_up(static_cast<size_t>(pl.n_partial_rows) * t->cfg.head_dim * 4, 256));
-  } else {
-    const spex_status_t ps = ensure_partials(t, pl.n_partial_rows);
-    if (ps != SPEX_OK) return ps;
-    part_o = t->d_part_o;
-    part_ml = t->d_part_ml;
   }
 
   spex::AttnArgs a{};

@@ -67,6 +67,10 @@ struct WalkArgs {
   float scale_log2;
   const int32_t *qt_mask; // as in AttnArgs; null for the causal chain
   bool cut;               // some request has more rows than a row block holds
+  // MXFP4 pools: what the workgroups and their merge do (Planner::build_pieces), and where partial states go
+  const int32_t *pieces, *merges;
+  int32_t n_pieces, n_merges;
+  float *part_o, *part_ml;
 };
 
 struct MergeArgs {

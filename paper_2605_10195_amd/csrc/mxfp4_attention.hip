@@ -4,17 +4,24 @@
 //       The split path's items, a workgroup for up to 16 NT rows of one: its four wavefronts take every fourth block of 32 tokens
 //       and join their softmax states through LDS.  Partial states go to the merge kernel, as for the other pools.
 //   spex_mxfp4_walk_kernel
-//       The tree walk: the same over the whole path of up to 16 NT rows, from the root to the requested nodes.  Nothing but finished
-//       rows is written.
+//       The tree walk: the same over the whole path of up to 16 NT rows, from the root to the requested nodes, by a wavefront or by
+//       four.  Nothing but finished rows is written, except where long paths go in pieces.
+//   spex_mxfp4_merge_kernel
+//       Merges the pieces' states of every row.
 //
-// Mathematics: S^T = K Q^T, p = 2^(c S^T - m), l += sum p, O^T += V^T P^T, out = O / l, with keys and values code * 2^E.
+// Mathematics: S^T = K Q^T, p = 2^(c S^T - m), l += sum p, O += P V, out = O / l, with keys and values code * 2^E.
 // Keys become bf16 operands, which hold code * 2^E exactly (two significant bits), values fp16, which do as well since the values' E is
 // bounded; v_cvt_scalef32_pk_* makes two of them from a byte and the scale.  Queries are the caller's bf16.  Weights go into the product
 // as two fp16 pieces, 22 bits, so that nothing is rounded to fewer bits than fp32 sums lose.
 //
+// Bound: the instructions a SIMD can issue.  A block of 32 tokens and a tile of 16 rows of a head of 128 are 26 products of 16 cycles and
+// about 145 vector instructions of 4 (64 conversions, 70 for the weights), and the two kinds of a SIMD's wavefronts hardly run side by
+// side; a second row tile shares the conversions.  The second piece of the weights is a third of the products.  Few rows on long paths
+// are bound by how fast wavefronts get their blocks.
+//
 // No LDS in the loop: a tile is held in the order in which its lanes consume it (mxfp4_device.hpp), so a block's codes go from memory
-// into the registers they are converted in, and sharing converted tiles between wavefronts would cost as many LDS reads
-// as the conversions take vector instructions.
+// into the registers they are converted in.  A ring of blocks in LDS, filled by copies of its own three or four ahead, was slower
+// (64 roots of 2500 tokens with 32 branches of 256: 190 us against 171).
 #include <algorithm>
 #include <type_traits>
 
@@ -25,92 +32,109 @@
 namespace spex {
 namespace {
 
-typedef uint32_t u32x3 __attribute__((ext_vector_type(3)));
+typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x16 __attribute__((ext_vector_type(16)));
 typedef u32x4 u32x4_q __attribute__((aligned(2)));   // queries: any alignment of their type
 typedef f32x4 f32x4_out __attribute__((aligned(4)));
+typedef f32x2 f32x2_out __attribute__((aligned(4)));
 
 // Start of a row's softmax reference: finite, so that (-inf) - m stays -inf, and below any score.
 constexpr float kMInit = -1.0e30f;
 // How far a score may exceed the reference before that moves, and the exponent of a weight at the reference: weights stay below 2^15,
 // fp16's largest, and the smallest fp16 step is 2^-31 of a row's largest weight at most.
 constexpr float kSlackLog2 = 8.f, kWeightLog2 = 7.f;
+// Places of a sparse product's weights: 0 and 2, or 1 and 3, of every four.
+constexpr int kEvenDims = static_cast<int>(0x88888888u), kOddDims = static_cast<int>(0xddddddddu);
 // Scaled references from here on are not subtracted in scaled form: their rounding would shift weights by many units.
 constexpr float kFarLog2 = 4194304.f;
 
 // A block of 32 tokens: pages a and b, wave-uniform.
 struct MxBlock {
-  int pid_a, vp_a, pid_b, vp_b;  // vp: position << 7 | valid tokens; vp_b 0: no page b
-  int lo, hi;                    // rows of the row block whose path holds it
-  bool masked, live;             // live: there is such a block
+  int64_t at[2];   // where the pages' tiles begin in a pool
+  int vp_a, vp_b;  // position << 7 | kMasked | valid tokens; vp_b 0: no page b
+  int rows;        // first row | (last row + 1) << 16 of the row block whose path holds it
+  bool live;       // there is such a block
+};
+constexpr int kMasked = 64, kValid = 63;  // of page a: some row of the wavefront does not see all of the block
+
+// The keys and the values of a block as they lie in memory.
+template <int M>
+struct MxKeys {
+  static constexpr int kScales = kMxRun<M> ? (M == 8 ? 2 : 1) : M;
+  uint32_t w[2][M];
+  uint32_t scale[2][kScales];  // a byte each
+};
+template <int M>
+struct MxValues {
+  static constexpr int kScales = kMxRun<M> ? 1 : M;
+  uint32_t w[2 * M];           // of the lane's first four tokens, of its second
+  uint32_t scale[2][kScales];  // four tokens' bytes each
 };
 
-// The words of a block as they lie in memory.
-template <int M>
-struct MxRaw {
-  static constexpr int kKeyScales = kMxRun<M> ? (M == 8 ? 2 : 1) : M, kValueScales = kMxRun<M> ? 1 : M;
-  uint32_t k[2][M], v[2][M];
-  uint32_t ks[2][kKeyScales];    // a byte each
-  uint32_t vs[2][kValueScales];  // four tokens' bytes each
-};
-
-typedef __amdgpu_buffer_rsrc_t rsrc_t;
-
-template <int M>
-__device__ __forceinline__ void load_words(rsrc_t r, int at, uint32_t (&w)[M]) {
+template <int N>
+__device__ __forceinline__ void load_words(const char *p, uint32_t (&w)[N]) {
+  typedef uint32_t word4 __attribute__((ext_vector_type(4), aligned(4)));
+  typedef uint32_t word3 __attribute__((ext_vector_type(3), aligned(4)));
+  typedef uint32_t word2 __attribute__((ext_vector_type(2), aligned(4)));
 #pragma unroll
-  for (int i = 0; i < M; i += 4) {
-    if (M - i >= 4) {
-      const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at + 4 * i, 0, 0));
+  for (int i = 0; i < N; i += 4) {
+    if (N - i >= 4) {
+      const word4 x = *reinterpret_cast<const word4 *>(p + 4 * i);
 #pragma unroll
       for (int j = 0; j < 4; ++j) w[i + j] = x[j];
-    } else if (M - i == 3) {
-      const u32x3 x = __builtin_bit_cast(u32x3, __builtin_amdgcn_raw_buffer_load_b96(r, at + 4 * i, 0, 0));
+    } else if (N - i == 3) {
+      const word3 x = *reinterpret_cast<const word3 *>(p + 4 * i);
 #pragma unroll
       for (int j = 0; j < 3; ++j) w[i + j] = x[j];
-    } else if (M - i == 2) {
-      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, at + 4 * i, 0, 0));
+    } else if (N - i == 2) {
+      const word2 x = *reinterpret_cast<const word2 *>(p + 4 * i);
       w[i] = x[0];
       w[i + 1] = x[1];
     } else {
-      w[i] = __builtin_amdgcn_raw_buffer_load_b32(r, at + 4 * i, 0, 0);
+      w[i] = *reinterpret_cast<const uint32_t *>(p + 4 * i);
     }
   }
 }
 
-// Requests a block.  A block or page that is not there has no bytes: its loads give zeros and move nothing.
+// Lane (g, t): token t of both pages.  A block that is not there, and page b of a block without one, are read at another place of the pool.
 template <int M>
-__device__ __forceinline__ void load_block(MxRaw<M> &x, const MxBlock &b, const char *kpool, const char *vpool, int page_tiles, int g) {
+__device__ __forceinline__ void load_keys(MxKeys<M> &x, const MxBlock &b, const void *pool) {
   const int lane = threadIdx.x & 63, c = lane & 15, jj = lane >> 4;
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
-    const int64_t at = (static_cast<int64_t>(p ? b.pid_b : b.pid_a) * page_tiles + g) * mx_tile_bytes(M);
-    const int bytes = b.live && (p ? b.vp_b : b.vp_a) != 0 ? mx_tile_bytes(M) : 0;
-    const rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(kpool + at), 0, bytes, 0x00020000);
-    const rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(vpool + at), 0, bytes, 0x00020000);
-    load_words<M>(kr, lane * 4 * M, x.k[p]);
+    const char *tile = static_cast<const char *>(pool) + b.at[p];
+    load_words<M>(tile + static_cast<uint32_t>(lane * 4 * M), x.w[p]);
 #pragma unroll
-    for (int i = 0; i < MxRaw<M>::kKeyScales; ++i) {
+    for (int i = 0; i < MxKeys<M>::kScales; ++i) {
       const int block = kMxRun<M> ? (M >= 4 ? jj * (M / 4) + i : jj * M / 4) : i;
-      x.ks[p][i] = __builtin_amdgcn_raw_buffer_load_b8(kr, mx_scale_at<M>(block, c), 0, 0);
+      x.scale[p][i] = *reinterpret_cast<const uint8_t *>(tile + static_cast<uint32_t>(mx_key_scale_at<M>(block, c)));
     }
-    load_words<M>(vr, lane * 4 * M, x.v[p]);
+  }
+}
+// Lane (g, c): page g % 2, tokens 4 (g / 2) .. + 3 and 8 further on, the order in which the sparse product takes them (block_values).
+template <int M>
+__device__ __forceinline__ void load_values(MxValues<M> &x, const MxBlock &b, const void *pool) {
+  const int lane = threadIdx.x & 63, c = lane & 15, page = (lane >> 4) & 1, tg = lane >> 5;
+  const char *tile = static_cast<const char *>(pool) + (b.at[0] + ((b.at[1] - b.at[0]) & -static_cast<int64_t>(page)));
+  load_words<2 * M>(tile + (16 * tg + c) * 8 * M, x.w);
 #pragma unroll
-    for (int i = 0; i < MxRaw<M>::kValueScales; ++i) {
-      const int block = kMxRun<M> ? c * M / 16 : i;
-      x.vs[p][i] = __builtin_amdgcn_raw_buffer_load_b32(vr, mx_scale_at<M>(block, 4 * jj), 0, 0);
-    }
+  for (int i = 0; i < MxValues<M>::kScales; ++i) {
+    const u32x2 e = *reinterpret_cast<const u32x2 *>(tile + mx_value_scale_at<M>(kMxRun<M> ? c * M / 16 : i, tg));
+    x.scale[0][i] = e[0];
+    x.scale[1][i] = e[1];
   }
 }
 
 // A wavefront's rows, 16 to a tile: lane (c = lane % 16, jj = lane / 16) has row c of every tile; its scores are of tokens 4 jj .. + 3
-// of page a, then of page b, its accumulators of the dims mx_value_dim(4 jj + i, j) and the one behind, i < 4.
+// of page a, then of page b; its accumulators 2 j and 2 j + 1 are of rows 4 jj .. + 3 and the dims mx_value_dim(c, j) and the one behind.
 template <int M, int NT>
 struct MxRows {
   bf16x8 q[NT][M];
   int limit[NT], qtok[NT], qidx[NT];
   uint32_t dmask[NT];
   f32x4 o[NT][2 * M];
-  float m[NT], mc[NT], l[NT];  // reference as a score, and scaled less kWeightLog2; l is the lane's share
+  f32x4 l[NT];                 // the weights' sums of rows 4 jj .. + 3, as a product with ones gives them
+  float m[NT], mc[NT];         // reference as a score, and scaled less kWeightLog2
   int seen_end;                // path positions from here on no row sees (wave-uniform)
   bool far;                    // wave-uniform: some reference is beyond kFarLog2
 };
@@ -128,7 +152,7 @@ __device__ __forceinline__ void load_rows(MxRows<M, NT> &st, const void *q, cons
     st.dmask[nt] = 0;
     st.m[nt] = kMInit;
     st.mc[nt] = kMInit * c - kWeightLog2;
-    st.l[nt] = 0.f;
+    st.l[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 2 * M; ++i) st.o[nt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (r < rows) {
@@ -158,7 +182,7 @@ __device__ __forceinline__ void load_rows(MxRows<M, NT> &st, const void *q, cons
 // Which of the lane's four tokens of a page the row sees, as bits.
 template <bool TREE>
 __device__ __forceinline__ uint32_t seen_bits(int limit, int qidx, uint32_t dmask, int vp, int first) {
-  const int valid = (vp & 127) - first, pos = (vp >> 7) + first;
+  const int valid = (vp & kValid) - first, pos = (vp >> 7) + first;
   if (TREE) {  // positions below base, and base + k for the set bits k of the mask
     const int shift = pos - (limit - 1 - qidx) + 32;
     const uint64_t bits = (static_cast<uint64_t>(dmask) << 32) | 0xffffffffull;
@@ -186,102 +210,140 @@ __device__ __forceinline__ bf16x8 key_operand(uint32_t w, float scale) {
   return __builtin_bit_cast(bf16x8, r);
 }
 
-// A block against the wavefront's rows.  row0: the first of them in the row block.
-template <int M, int NT, bool TREE>
-__device__ __forceinline__ void block_step(MxRows<M, NT> &st, const MxRaw<M> &x, const MxBlock &b, int row0, float c, float slack) {
-  const int lane = threadIdx.x & 63, jj = lane >> 4;
+// Scores of a block's 32 tokens, eight a lane and row: the four of page a, the four of page b.
+template <int NT>
+struct MxScores {
   f32x4 s[NT][2];
+};
+// (T0, T1: the first row tile concerned, and the one behind the last.)
+template <int T0, int T1, int M, int NT>
+__device__ __forceinline__ void block_scores(MxScores<NT> &y, const MxRows<M, NT> &st, const MxKeys<M> &x) {
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
-    float scale[MxRaw<M>::kKeyScales];
+    float scale[MxKeys<M>::kScales];
 #pragma unroll
-    for (int i = 0; i < MxRaw<M>::kKeyScales; ++i) scale[i] = mx_scale(x.ks[p][i]);
+    for (int i = 0; i < MxKeys<M>::kScales; ++i) scale[i] = mx_scale(x.scale[p][i]);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) s[nt][p] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int nt = T0; nt < T1; ++nt) y.s[nt][p] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < M; ++i) {
-      const bf16x8 kf = key_operand<M>(x.k[p][i], scale[kMxRun<M> ? (M == 8 ? i / 4 : 0) : i]);
+      const bf16x8 kf = key_operand<M>(x.w[p][i], scale[kMxRun<M> ? (M == 8 ? i / 4 : 0) : i]);
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) s[nt][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, st.q[nt][i], s[nt][p], 0, 0, 0);
+      for (int nt = T0; nt < T1; ++nt) y.s[nt][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, st.q[nt][i], y.s[nt][p], 0, 0, 0);
     }
   }
-  f16x8 ph[NT], pl[NT];
+}
+// Those that a row does not see become -inf.  row0: the wavefront's first row in the row block.
+template <int T0, int T1, bool TREE, int M, int NT>
+__device__ __forceinline__ void mask_block(MxScores<NT> &y, const MxRows<M, NT> &st, const MxBlock &b, int row0) {
+  if (!(b.vp_a & kMasked)) return;
+  const int lane = threadIdx.x & 63, jj = lane >> 4, lo = b.rows & 0xffff, hi = static_cast<int>(static_cast<uint32_t>(b.rows) >> 16);
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    float y[8];
+  for (int nt = T0; nt < T1; ++nt) {
+    const int row = row0 + 16 * nt + (lane & 15);
+    uint32_t seen = seen_bits<TREE>(st.limit[nt], st.qidx[nt], st.dmask[nt], b.vp_a, 4 * jj) |
+                    seen_bits<TREE>(st.limit[nt], st.qidx[nt], st.dmask[nt], b.vp_b, 4 * jj) << 4;
+    if (row < lo || row >= hi) seen = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      y[i] = s[nt][0][i];
-      y[4 + i] = s[nt][1][i];
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t keep = static_cast<uint32_t>(static_cast<int32_t>(seen << (31 - i)) >> 31);
+      const float score = y.s[nt][i >> 2][i & 3];  // a select here compiles to three instructions a score
+      y.s[nt][i >> 2][i & 3] = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, score) & keep) | (0xff800000u & ~keep));
     }
-    const int first_row = row0 + 16 * nt;
-    if (b.masked || b.lo > first_row || b.hi < first_row + 16) {
-      const int row = first_row + (lane & 15);
-      uint32_t seen = seen_bits<TREE>(st.limit[nt], st.qidx[nt], st.dmask[nt], b.vp_a, 4 * jj) |
-                      seen_bits<TREE>(st.limit[nt], st.qidx[nt], st.dmask[nt], b.vp_b, 4 * jj) << 4;
-      if (row < b.lo || row >= b.hi) seen = 0;
+  }
+}
+
+// Moves the references that a block's scores are far above; scores of far rows become differences to theirs.
+template <int T0, int T1, int M, int NT>
+__device__ __forceinline__ void move_references(MxRows<M, NT> &st, MxScores<NT> &y, float c, float slack) {
+  float top[NT];
+  bool above = false;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = (seen >> i) & 1 ? y[i] : kNegInf;
-    }
-    const float top = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
-    if (__any(top > st.m[nt] + slack)) {
-      const float m_new = row_group_max(fmaxf(top, st.m[nt]));
+  for (int nt = T0; nt < T1; ++nt) {
+    const f32x4 a = y.s[nt][0], b = y.s[nt][1];
+    top[nt] = fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3])));
+    above = above || top[nt] > st.m[nt] + slack;
+  }
+  if (__any(above)) {
+#pragma unroll
+    for (int nt = T0; nt < T1; ++nt) {
+      const float m_new = row_group_max(fmaxf(top[nt], st.m[nt]));
       const float alpha = fast_exp2((st.m[nt] - m_new) * c);
       st.m[nt] = m_new;
       st.mc[nt] = __builtin_fmaf(m_new, c, -kWeightLog2);
       st.far = st.far || __any(fabsf(st.mc[nt]) >= kFarLog2 && m_new != kMInit);
-      st.l[nt] *= alpha;
+      f32x4 of_rows;  // the lane's accumulators are of four rows
 #pragma unroll
-      for (int i = 0; i < 2 * M; ++i) st.o[nt][i] *= alpha;
+      for (int i = 0; i < 4; ++i) of_rows[i] = __shfl(alpha, 4 * (static_cast<int>(threadIdx.x & 63) >> 4) + i);
+      st.l[nt] *= of_rows;
+#pragma unroll
+      for (int i = 0; i < 2 * M; ++i) st.o[nt][i] *= of_rows;
     }
-    if (st.far) {
+  }
+  if (st.far) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = fast_exp2(__builtin_fmaf(y[i] - st.m[nt], c, kWeightLog2));
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = fast_exp2(__builtin_fmaf(y[i], c, -st.mc[nt]));
+    for (int nt = T0; nt < T1; ++nt) {
+      y.s[nt][0] -= st.m[nt];
+      y.s[nt][1] -= st.m[nt];
+      st.mc[nt] = -kWeightLog2;
     }
-    st.l[nt] += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
+  }
+}
+
+// Weights of a block's scores and their product with its values.
+template <int T0, int T1, bool OVERLAP, int M, int NT>
+__device__ __forceinline__ void block_values(MxRows<M, NT> &st, const MxScores<NT> &y, const MxValues<M> &x, float c) {
+  f16x8 ph[NT], pl[NT];
+#pragma unroll
+  for (int nt = T0; nt < T1; ++nt) {
+    float w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = fast_exp2(__builtin_fmaf(y.s[nt][i >> 2][i & 3], c, -st.mc[nt]));
     u32x4 h, rest;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      h[i] = __builtin_bit_cast(uint32_t, f16x2{static_cast<_Float16>(y[2 * i]), static_cast<_Float16>(y[2 * i + 1])});
-      rest[i] = rest_of(h[i], y[2 * i], y[2 * i + 1]);
+      h[i] = __builtin_bit_cast(uint32_t, f16x2{static_cast<_Float16>(w[2 * i]), static_cast<_Float16>(w[2 * i + 1])});
+      rest[i] = rest_of(h[i], w[2 * i], w[2 * i + 1]);
     }
     ph[nt] = __builtin_bit_cast(f16x8, h);
     pl[nt] = __builtin_bit_cast(f16x8, rest);
+    const _Float16 one = static_cast<_Float16>(1.f);
+    const f16x8 ones = {one, one, one, one, one, one, one, one};
+    st.l[nt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph[nt], ones, st.l[nt], 0, 0, 0);
+    st.l[nt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl[nt], ones, st.l[nt], 0, 0, 0);
   }
+  if (!OVERLAP) __builtin_amdgcn_sched_barrier(0);  // the values' conversions ahead of the weights would take the registers of a wavefront
   float vs[2][4];
 #pragma unroll
   for (int j = 0; j < M; ++j) {
     if (j == 0 || !kMxRun<M>) {
 #pragma unroll
-      for (int p = 0; p < 2; ++p)
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) vs[p][t] = mx_scale((x.vs[p][kMxRun<M> ? 0 : j] >> (8 * t)) & 255u);
+        for (int t = 0; t < 4; ++t) vs[h][t] = mx_scale(x.scale[h][kMxRun<M> ? 0 : j], t);
     }
-    // a word: dims d, d + 1 of four tokens, a byte each -> the rows of d and of d + 1, tokens side by side
-    u32x4 r0, r1;
+    // A byte of a word is the dims d, d + 1 of one token, which one conversion puts side by side, where a product over tokens wants
+    // two tokens of one dim.  So the product is one over (token, dim) pairs of which every second weight is zero: the sparse one,
+    // which takes two of four at a dense product's rate; kEvenDims and kOddDims choose d and d + 1.  It wants a lane's values in the
+    // order in which load_values has taken them.
+    u32x8 r;
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      uint32_t w[4];
-      w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x.v[p][j], vs[p][0], 0));
-      w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x.v[p][j], vs[p][1], 1));
-      w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x.v[p][j], vs[p][2], 2));
-      w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x.v[p][j], vs[p][3], 3));
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        r0[2 * p + t] = __builtin_amdgcn_perm(w[2 * t + 1], w[2 * t], 0x05040100u);
-        r1[2 * p + t] = __builtin_amdgcn_perm(w[2 * t + 1], w[2 * t], 0x07060302u);
-      }
+    for (int h = 0; h < 2; ++h) {
+      r[4 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x.w[h * M + j], vs[h][0], 0));
+      r[4 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x.w[h * M + j], vs[h][1], 1));
+      r[4 * h + 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x.w[h * M + j], vs[h][2], 2));
+      r[4 * h + 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x.w[h * M + j], vs[h][3], 3));
     }
-    const f16x8 a0 = __builtin_bit_cast(f16x8, r0), a1 = __builtin_bit_cast(f16x8, r1);
+    const f16x16 vf = __builtin_bit_cast(f16x16, r);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      st.o[nt][2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, ph[nt], st.o[nt][2 * j], 0, 0, 0);
-      st.o[nt][2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, pl[nt], st.o[nt][2 * j], 0, 0, 0);
-      st.o[nt][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, ph[nt], st.o[nt][2 * j + 1], 0, 0, 0);
-      st.o[nt][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, pl[nt], st.o[nt][2 * j + 1], 0, 0, 0);
+    for (int nt = T0; nt < T1; ++nt) {
+      st.o[nt][2 * j] = __builtin_amdgcn_smfmac_f32_16x16x64_f16(ph[nt], vf, st.o[nt][2 * j], kEvenDims, 0, 0);
+      st.o[nt][2 * j + 1] = __builtin_amdgcn_smfmac_f32_16x16x64_f16(ph[nt], vf, st.o[nt][2 * j + 1], kOddDims, 0, 0);
+    }
+#pragma unroll
+    for (int nt = T0; nt < T1; ++nt) {
+      st.o[nt][2 * j] = __builtin_amdgcn_smfmac_f32_16x16x64_f16(pl[nt], vf, st.o[nt][2 * j], kEvenDims, 0, 0);
+      st.o[nt][2 * j + 1] = __builtin_amdgcn_smfmac_f32_16x16x64_f16(pl[nt], vf, st.o[nt][2 * j + 1], kOddDims, 0, 0);
     }
   }
 }
@@ -291,22 +353,25 @@ struct RowPlace {
   int64_t at;  // row of the destination, or -1: none
   float inv;
 };
-// LDS of a set of wavefronts that hold the same rows: a stage of 16 rows each, softmax states, places.
+// LDS of a set of wavefronts that hold the same rows: softmax states, factors and places, and of several wavefronts a stage of 16 rows each.
 template <int M, int NT>
 struct MxJoin {
   static constexpr int kRow = 32 * M + 4;  // the pad spreads rows over the banks
   static constexpr int kStage = 16 * kRow;
-  static constexpr int floats(int waves) { return waves * (kStage + 2 * 16 * NT) + 4 * 16; }
+  static constexpr int floats(int waves) { return waves * ((waves > 1 ? kStage : 0) + 2 * 16 * NT + 16) + 4 * 16; }
 };
 
-// Joins the states of the KS wavefronts (number ks of them calls) that hold the same rows, and writes the rows.  Called by all of a
-// workgroup's wavefronts together, with an area of their own for each set.  place(nt, row of the tile): the destination row or -1.
+// Joins the states of the KS wavefronts (number ks of them calls) that hold the same rows, and writes the rows.  Several: called by all
+// of a workgroup together.  place(nt, row of the tile): the destination row or -1.
 template <int M, int NT, int KS, class Place>
 __device__ __forceinline__ void join_rows(MxRows<M, NT> &st, int ks, float c, float *area, float *dst, float *ml, float *lse, Place place) {
-  constexpr int kRow = MxJoin<M, NT>::kRow, kStage = MxJoin<M, NT>::kStage, D = 32 * M;
+  constexpr int kRow = MxJoin<M, NT>::kRow, kStage = KS > 1 ? MxJoin<M, NT>::kStage : 0, D = 32 * M;
+  constexpr int kRun = kMxRun<M> ? 2 * M : 2;  // dims of a lane that follow each other
   const int lane = threadIdx.x & 63, row = lane & 15, jj = lane >> 4;
-  float *states = area + KS * kStage;  // [wavefront][row]{m, l}
-  RowPlace *places = reinterpret_cast<RowPlace *>(states + KS * 2 * 16 * NT);
+  RowPlace *places = reinterpret_cast<RowPlace *>(area);
+  float *states = area + 4 * 16;  // [wavefront][m of all rows, l of all rows]
+  float *factors = states + KS * 2 * 16 * NT + 16 * ks;
+  float *stage = states + KS * (2 * 16 * NT + 16);
   auto meet = [&]() {
     if (KS > 1) {
       __syncthreads();
@@ -317,125 +382,202 @@ __device__ __forceinline__ void join_rows(MxRows<M, NT> &st, int ks, float c, fl
   };
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    st.l[nt] += __shfl_xor(st.l[nt], 16);
-    st.l[nt] += __shfl_xor(st.l[nt], 32);
-    if (KS > 1 && jj == 0) *reinterpret_cast<f32x2 *>(states + (ks * 16 * NT + 16 * nt + row) * 2) = f32x2{st.m[nt], st.l[nt]};
+    float *mine = states + ks * 2 * 16 * NT + 16 * nt;
+    if (jj == 0) mine[row] = st.m[nt];
+    if (row == 0) *reinterpret_cast<f32x4 *>(mine + 16 * NT + 4 * jj) = st.l[nt];
   }
-  if (KS > 1) __syncthreads();
+  meet();
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    float m = st.m[nt], l = st.l[nt], factor = 1.f;
+    const float *of = states + 16 * nt + row;
+    float m = st.m[nt], l = of[16 * NT], factor = 1.f;
     if (KS > 1) {
-      f32x2 all[KS];
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        all[k] = *reinterpret_cast<const f32x2 *>(states + (k * 16 * NT + 16 * nt + row) * 2);
-        m = fmaxf(m, all[k][0]);
-      }
+      for (int k = 0; k < KS; ++k) m = fmaxf(m, of[k * 2 * 16 * NT]);
       l = 0.f;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) l += all[k][1] * fast_exp2((all[k][0] - m) * c);
+      for (int k = 0; k < KS; ++k) l += of[(2 * k + 1) * 16 * NT] * fast_exp2((of[k * 2 * 16 * NT] - m) * c);
       factor = fast_exp2((st.m[nt] - m) * c);
     }
-    float *stage = area + ks * kStage;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 2 * M; j += (kMxRun<M> && M > 1 ? 4 : 2)) {
-        float *to = stage + row * kRow + mx_value_dim<M>(4 * jj + i, j / 2);
-        if constexpr (kMxRun<M> && M > 1)
-          *reinterpret_cast<f32x4 *>(to) = f32x4{st.o[nt][j][i], st.o[nt][j + 1][i], st.o[nt][j + 2][i], st.o[nt][j + 3][i]} * factor;
-        else
-          *reinterpret_cast<f32x2 *>(to) = f32x2{st.o[nt][j][i], st.o[nt][j + 1][i]} * factor;
+    if (jj == 0) {
+      const float inv = ml ? 1.f : 1.f / l;
+      if (ks == 0) {
+        const int64_t at = place(nt, row);
+        places[row] = {at, inv};
+        if (at >= 0) {
+          if (ml)
+            *reinterpret_cast<f32x2 *>(ml + 2 * at) = f32x2{__builtin_fmaf(m, c, -kWeightLog2), l};
+          else if (lse)
+            lse[at] = (__builtin_fmaf(m, c, -kWeightLog2) + __builtin_log2f(l)) * 0.6931471805599453f;
+        }
       }
-    if (ks == 0 && jj == 0) {
-      const int64_t at = place(nt, row);
-      places[row] = {at, ml ? 1.f : 1.f / l};
-      if (at >= 0) {
-        if (ml)
-          *reinterpret_cast<f32x2 *>(ml + 2 * at) = f32x2{__builtin_fmaf(m, c, -kWeightLog2), l};
-        else if (lse)
-          lse[at] = (__builtin_fmaf(m, c, -kWeightLog2) + __builtin_log2f(l)) * 0.6931471805599453f;
+      factors[row] = factor;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const f32x4 f = *reinterpret_cast<const f32x4 *>(factors + 4 * jj);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const RowPlace to = places[4 * jj + i];
+      const float by = KS > 1 ? f[i] : to.inv;
+      if (KS == 1 && to.at < 0) continue;
+      float *out = KS > 1 ? stage + ks * kStage + (4 * jj + i) * kRow : dst + to.at * D;
+#pragma unroll
+      for (int j = 0; j < M; j += kRun / 2) {
+        float *p = out + mx_value_dim<M>(row, j);
+        if constexpr (kRun >= 4) {
+#pragma unroll
+          for (int k = 0; k < kRun; k += 4) {
+            const f32x4 *o = st.o[nt] + 2 * j + k;
+            *reinterpret_cast<f32x4_out *>(p + k) = f32x4{o[0][i], o[1][i], o[2][i], o[3][i]} * by;
+          }
+        } else {
+          *reinterpret_cast<f32x2_out *>(p) = f32x2{st.o[nt][2 * j][i], st.o[nt][2 * j + 1][i]} * by;
+        }
       }
     }
     meet();
-    for (int i = ks * 64 + lane; i < 16 * (D / 4); i += 64 * KS) {
-      const int r = i / (D / 4), d = i % (D / 4) * 4;
-      const RowPlace to = places[r];
-      f32x4 v = *reinterpret_cast<const f32x4 *>(area + r * kRow + d);
+    if (KS > 1) {
+      for (int i = ks * 64 + lane; i < 16 * (D / 4); i += 64 * KS) {
+        const int r = i / (D / 4), d = i % (D / 4) * 4;
+        const RowPlace to = places[r];
+        f32x4 v = *reinterpret_cast<const f32x4 *>(stage + r * kRow + d);
 #pragma unroll
-      for (int k = 1; k < KS; ++k) v += *reinterpret_cast<const f32x4 *>(area + k * kStage + r * kRow + d);
-      if (to.at >= 0) *reinterpret_cast<f32x4_out *>(dst + to.at * D + d) = v * to.inv;
+        for (int k = 1; k < KS; ++k) v += *reinterpret_cast<const f32x4 *>(stage + k * kStage + r * kRow + d);
+        if (to.at >= 0) *reinterpret_cast<f32x4_out *>(dst + to.at * D + d) = v * to.inv;
+      }
+      if (nt + 1 < NT) meet();
     }
-    if (nt + 1 < NT) meet();
   }
 }
 
-constexpr int kWaves = 4;  // of a workgroup: they hold the same rows
+constexpr int kWaves = 4;  // of a workgroup
+// Private blocks of a set from which on those of one row tile have rounds of their own: 64 branches of four rows each, eight blocks long, took
+// 171 us without and 160 with; two or three blocks a branch 140 and 152.
+constexpr int kAlone = 16;
 
-// The blocks of wavefront w of a workgroup: records w, w + 4, .. of a list, 64 of them at a time in registers, a lane each.
-// read(i): record i, for a lane; lanes whose record does not concern the wavefront's rows drop out.
+// The blocks of one of the wavefronts that hold the same rows: every stride-th record of a list, 64 of them at a time in registers, a lane
+// each.  read(i, r): record i, for a lane; false where it does not concern the wavefront's rows.
 struct MxLanes {
-  int pid_a, vp_a, pid_b, vp_b, rows, flags;
+  int64_t at[2];
+  int vp_a, vp_b, rows;
 };
-template <class Read>
+template <int M>
+__device__ __forceinline__ int64_t tile_at(int page, int page_tiles, int g) {
+  return (static_cast<int64_t>(page) * page_tiles + g) * mx_tile_bytes(M);
+}
+// Records from number `alone` on whose rows lie in one tile are left out of those for all tiles, and are the only ones of a single tile.
+template <int T0, int T1, int NT, class Read>
 struct MxSource {
   Read read;
-  int n, at;
+  int n, at, stride, alone, row0;
+  bool &left_out;
   uint64_t left;
   MxLanes r;
   __device__ __forceinline__ MxBlock next() {
     while (left == 0 && at < n) {
-      const int i = at + kWaves * (threadIdx.x & 63);
+      const int i = at + stride * static_cast<int>(threadIdx.x & 63);
       bool concerns = i < n;
       if (concerns) concerns = read(i, r);
+      const int lo = r.rows & 0xffff, hi = static_cast<int>(static_cast<uint32_t>(r.rows) >> 16);
+      if (NT > 1 && T1 - T0 == NT) {
+        const bool one = i >= alone && (lo >= row0 + 16 || hi <= row0 + 16);
+        left_out = left_out || __any(concerns && one);
+        concerns = concerns && !one;
+      } else if (NT > 1) {
+        concerns = concerns && (T0 == 0 ? hi <= row0 + 16 : lo >= row0 + 16);
+      }
+      if (lo > row0 + 16 * T0 || hi < row0 + 16 * T1) r.vp_a |= kMasked;
       left = __ballot(concerns);
-      at += 64 * kWaves;
+      at += 64 * stride;
     }
     MxBlock b;
     b.live = left != 0;
     const int l = b.live ? __builtin_ctzll(left) : 0;
+    const int none = b.live ? 0 : kMasked;  // a block that is not there is one of no rows
     left &= left - 1;
-    b.pid_a = __builtin_amdgcn_readlane(r.pid_a, l);
-    b.vp_a = __builtin_amdgcn_readlane(r.vp_a, l);
-    b.pid_b = __builtin_amdgcn_readlane(r.pid_b, l);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const uint32_t low = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.at[p]), l));
+      b.at[p] = static_cast<int64_t>(__builtin_amdgcn_readlane(static_cast<int>(r.at[p] >> 32), l)) << 32 | low;
+    }
+    b.vp_a = __builtin_amdgcn_readlane(r.vp_a, l) | none;
     b.vp_b = __builtin_amdgcn_readlane(r.vp_b, l);
-    const int rows = __builtin_amdgcn_readlane(r.rows, l);
-    b.lo = rows & 0xffff;
-    b.hi = static_cast<int>(static_cast<uint32_t>(rows) >> 16);
-    b.masked = __builtin_amdgcn_readlane(r.flags, l) & 1;
+    b.rows = b.live ? __builtin_amdgcn_readlane(r.rows, l) : 0;
     return b;
   }
 };
 
-// One block is worked on while the next is on its way, in registers of its own.
-template <int M, int NT, bool TREE, class Read>
-__device__ __forceinline__ void walk_blocks(MxRows<M, NT> &st, const void *k, const void *v, int page_tiles, int g, int row0, float c, int n, int w,
-                                            Read read) {
-  const char *kpool = static_cast<const char *>(k), *vpool = static_cast<const char *>(v);
+// Blocks first, first + stride, .. of n, for the row tiles T0 .. T1.  OVERLAP: a block's scores are computed beside the weights and values
+// of the block before, so that matrix and vector instructions of one wavefront run at the same time; keys are requested two blocks ahead,
+// values one.  Otherwise a block at a time, the next one's keys and values requested where this one's have been used.
+template <int T0, int T1, bool TREE, bool OVERLAP, int M, int NT, class Read>
+__device__ __forceinline__ void walk_tiles(MxRows<M, NT> &st, const void *k, const void *v, int row0, float c, int n, int first, int stride,
+                                           int alone, bool &left_out, Read read) {
   const float slack = kSlackLog2 / c;
-  MxSource<Read> src{read, n, w, 0, {}};
-  MxRaw<M> x0, x1;
+  MxSource<T0, T1, NT, Read> src{read, n, first, stride, alone, row0, left_out, 0, {}};
+  MxKeys<M> k0;
+  MxValues<M> v0;
+  MxScores<NT> y0;
   MxBlock b0 = src.next();
-  load_block<M>(x0, b0, kpool, vpool, page_tiles, g);
-  MxBlock b1 = src.next();
-  load_block<M>(x1, b1, kpool, vpool, page_tiles, g);
-  while (b0.live) {
-    block_step<M, NT, TREE>(st, x0, b0, row0, c, slack);
-    b0 = src.next();
-    load_block<M>(x0, b0, kpool, vpool, page_tiles, g);
-    if (!b1.live) break;
-    block_step<M, NT, TREE>(st, x1, b1, row0, c, slack);
-    b1 = src.next();
-    load_block<M>(x1, b1, kpool, vpool, page_tiles, g);
+  if (!b0.live) return;
+  load_keys<M>(k0, b0, k);
+  load_values<M>(v0, b0, v);
+  if constexpr (OVERLAP) {
+    MxKeys<M> k1;
+    MxValues<M> v1;
+    MxScores<NT> y1;
+    MxBlock b1 = src.next();
+    load_keys<M>(k1, b1, k);
+    block_scores<T0, T1>(y0, st, k0);
+    mask_block<T0, T1, TREE>(y0, st, b0, row0);
+    // y, x: of block b; the block behind it has its keys in nk and its place in nb, the one behind that is requested into b and k
+    auto step = [&](MxScores<NT> &y, MxValues<M> &x, MxKeys<M> &key, MxBlock &b, MxScores<NT> &ny, MxValues<M> &nx, MxKeys<M> &nk, MxBlock &nb) {
+      b = src.next();
+      load_keys<M>(key, b, k);
+      load_values<M>(nx, nb, v);
+      move_references<T0, T1>(st, y, c, slack);
+      block_scores<T0, T1>(ny, st, nk);
+      block_values<T0, T1, OVERLAP>(st, y, x, c);
+      mask_block<T0, T1, TREE>(ny, st, nb, row0);
+    };
+    do {  // two at a time: a block that is not there is one of no rows
+      step(y0, v0, k0, b0, y1, v1, k1, b1);
+      step(y1, v1, k1, b1, y0, v0, k0, b0);
+    } while (b0.live);
+  } else {
+    do {
+      const MxBlock b = b0;
+      b0 = src.next();
+      block_scores<T0, T1>(y0, st, k0);
+      load_keys<M>(k0, b0, k);
+      mask_block<T0, T1, TREE>(y0, st, b, row0);
+      move_references<T0, T1>(st, y0, c, slack);
+      block_values<T0, T1, OVERLAP>(st, y0, v0, c);
+      load_values<M>(v0, b0, v);
+    } while (b0.live);
+  }
+}
+// Of two tiles, blocks that concern one of them only have rounds of their own from record `alone` on: half the products and weights.
+template <bool TREE, bool OVERLAP, int M, int NT, class Read>
+__device__ __forceinline__ void walk_blocks(MxRows<M, NT> &st, const void *k, const void *v, int row0, float c, int n, int first, int stride,
+                                            int alone, Read read) {
+  bool left_out = false;
+  walk_tiles<0, NT, TREE, OVERLAP>(st, k, v, row0, c, n, first, stride, alone, left_out, read);
+  if constexpr (NT == 2) {
+    if (!left_out) return;
+    const int from = first >= alone ? first : first + (alone - first + stride - 1) / stride * stride;
+    walk_tiles<0, 1, TREE, OVERLAP>(st, k, v, row0, c, n, from, stride, alone, left_out, read);
+    walk_tiles<1, 2, TREE, OVERLAP>(st, k, v, row0, c, n, from, stride, alone, left_out, read);
   }
 }
 
-// Wavefronts a SIMD: with one the compiler keeps accumulators in the other half of the register file and moves them for every block.
-constexpr int mx_occupancy(int blocks, int row_tiles) { return blocks * row_tiles <= 4 ? 3 : 2; }
+// Overlapped where the registers for two blocks are there (heads of 128 and one tile would have two wavefronts a SIMD instead of three:
+// 177 us against 165).
+constexpr bool mx_overlap(int blocks, int row_tiles) { return row_tiles == 2 || blocks <= 2; }
 
 template <int M, int NT, bool TREE>
-__global__ __launch_bounds__(64 * kWaves, mx_occupancy(M, NT)) void spex_mxfp4_split_kernel(AttnArgs p, Shape sh, SplitLists ls) {
+__global__ __launch_bounds__(64 * kWaves, mx_occupancy(32 * M, NT)) void spex_mxfp4_split_kernel(AttnArgs p, Shape sh, SplitLists ls) {
   __shared__ __attribute__((aligned(16))) float lds[MxJoin<M, NT>::floats(kWaves)];
   const ListPos at = list_of(ls, static_cast<int>(blockIdx.x));
   const int tile = at.local / at.n_items;
@@ -447,11 +589,13 @@ __global__ __launch_bounds__(64 * kWaves, mx_occupancy(M, NT)) void spex_mxfp4_s
   const float c = p.scale_log2;
   MxRows<M, NT> st;
   load_rows<M, NT, TREE>(st, p.q, p.qt_rec, p.qt_mask, cur.qt_begin, cur.row0, rows, g, sh, c);
-  walk_blocks<M, NT, TREE>(st, p.k_pool, p.v_pool, sh.page_tiles, g, 0, c, (cur.pg_count + 1) >> 1, w, [&](int i, MxLanes &r) {
+  const int n_blocks = (cur.pg_count + 1) >> 1;
+  walk_blocks<TREE, mx_overlap(M, NT)>(st, p.k_pool, p.v_pool, 0, c, n_blocks, w, kWaves, INT_MAX, [&](int i, MxLanes &r) {
     const int2 *pages = reinterpret_cast<const int2 *>(p.pg_rec) + cur.pg_begin + 2 * i;
     const bool has_b = 2 * i + 1 < cur.pg_count;
     const int2 a = pages[0], b = pages[has_b ? 1 : 0];
-    r = {a.x, a.y, b.x, has_b ? b.y : 0, static_cast<int>(0xffff0000u), cur.flags | (has_b ? 0 : 1)};
+    r = {{tile_at<M>(a.x, sh.page_tiles, g), tile_at<M>(b.x, sh.page_tiles, g)}, a.y | ((cur.flags & 1) || !has_b ? kMasked : 0), has_b ? b.y : 0,
+         static_cast<int>(0xffff0000u)};
     return (a.y >> 7) < st.seen_end;
   });
   join_rows<M, NT, kWaves>(st, w, c, lds, p.finish ? p.out : p.part_o, p.finish ? nullptr : p.part_ml, p.lse, [&](int nt, int row) {
@@ -462,38 +606,130 @@ __global__ __launch_bounds__(64 * kWaves, mx_occupancy(M, NT)) void spex_mxfp4_s
   });
 }
 
-// One workgroup for each set of 16 NT rows of the row blocks' NW wavefronts of 16 ntw.  The sets of a row block read its shared blocks
-// one beside the other: they are eight workgroups apart, which is one XCD.
-template <int M, int NT, bool TREE>
-__global__ __launch_bounds__(64 * kWaves, mx_occupancy(M, NT)) void spex_mxfp4_walk_kernel(WalkArgs p, Shape sh, int nw, int ntw) {
-  __shared__ __attribute__((aligned(16))) float lds[MxJoin<M, NT>::floats(kWaves)];
-  const int groups = ntw / NT, sets = nw * groups;
-  const int batch = static_cast<int>(blockIdx.x) / (8 * sets), within = static_cast<int>(blockIdx.x) - batch * 8 * sets;
-  const int set = within >> 3, item = batch * 8 + (within & 7);
-  if (item >= p.n_items) return;
-  const int rw = set / groups, row_base = (set - rw * groups) * 16 * NT;
+// A set of up to 16 NT rows of a work item of the tree-walk lists: those of tile set `part >> 8` of its wavefront of rows `part & 0xff`.
+struct MxSet {
+  int g, rows, row_base;      // rows of the wavefront, the set's first one among them
+  int row0;                   // the same in the row block
+  int qt_begin;
+  int blk_begin, n_shared, priv_begin, n_priv;
+};
+template <int NT>
+__device__ __forceinline__ MxSet load_set(const int32_t *items, int item, int part, int nw, int ntw, int G) {
   const int64_t ir = static_cast<int64_t>(item) * (nw <= 4 ? 16 : 32);
-  const int rows = sload(p.items, ir + 3 + 2 * nw + rw) * sh.G;
-  if (row_base >= rows) return;  // padding, a wavefront without rows, or no such tile
-  const int g = sload(p.items, ir), blk_begin = sload(p.items, ir + 1), n_shared = sload(p.items, ir + 2);
-  // per wavefront: private blocks | room << 16
-  const int n_priv = sload(p.items, ir + 3 + rw) & 0xffff;
-  int priv_begin = blk_begin + n_shared;
-  for (int v = 0; v < rw; ++v) priv_begin += static_cast<int>(static_cast<uint32_t>(sload(p.items, ir + 3 + v)) >> 16);
-  const int row0 = rw * 16 * ntw + row_base, qt_begin = sload(p.items, ir + 3 + nw + rw), G = sh.G, w = uniform(threadIdx.x >> 6);
+  const int w = part & 0xff;
+  // The whole record in one load, a lane an int.
+  const int x = items[ir + min(static_cast<int>(threadIdx.x & 63), nw <= 4 ? 15 : 31)];
+  auto field = [&](int i) { return __builtin_amdgcn_readlane(x, i); };
+  MxSet t;
+  t.g = field(0);
+  t.blk_begin = field(1);
+  t.n_shared = field(2);
+  t.n_priv = field(3 + w) & 0xffff;  // blocks | room << 16
+  t.priv_begin = t.blk_begin + t.n_shared;
+  for (int v = 0; v < w; ++v) t.priv_begin += static_cast<int>(static_cast<uint32_t>(field(3 + v)) >> 16);
+  t.qt_begin = field(3 + nw + w);
+  t.rows = field(3 + 2 * nw + w) * G;
+  t.row_base = (part >> 8) * 16 * NT;
+  t.row0 = w * 16 * ntw + t.row_base;
+  return t;
+}
+
+// A workgroup of four pieces, a wavefront each, or of one whose blocks the four wavefronts take in turn (Planner::build_pieces).
+template <int M, int NT, bool TREE>
+__global__ __launch_bounds__(64 * kWaves, mx_occupancy(32 * M, NT)) void spex_mxfp4_walk_kernel(WalkArgs p, Shape sh, int nw, int ntw) {
+  constexpr int kOne = MxJoin<M, NT>::floats(1), kAll = MxJoin<M, NT>::floats(kWaves);
+  __shared__ __attribute__((aligned(16))) float lds[kWaves * kOne > kAll ? kWaves * kOne : kAll];
+  const int w = uniform(threadIdx.x >> 6);
+  const int64_t pr = (static_cast<int64_t>(blockIdx.x) * kWaves + w) * 8;
+  const int item = sload(p.pieces, pr), begin = sload(p.pieces, pr + 2), end = sload(p.pieces, pr + 3), slot = sload(p.pieces, pr + 4);
+  const bool together = sload(p.pieces, pr + 5) != 0;  // all of the workgroup or none
+  if (item < 0) return;  // padding
+  const MxSet t = load_set<NT>(p.items, item, sload(p.pieces, pr + 1), nw, ntw, sh.G);
+  const int G = sh.G;
   const float c = p.scale_log2;
   MxRows<M, NT> st;
-  load_rows<M, NT, TREE>(st, p.q, p.qt_rec, p.qt_mask, qt_begin, row_base, rows, g, sh, c);
-  walk_blocks<M, NT, TREE>(st, p.k_pool, p.v_pool, sh.page_tiles, g, row0, c, n_shared + n_priv, w, [&](int i, MxLanes &r) {
-    const u32x4 *rec = reinterpret_cast<const u32x4 *>(p.blocks) + 2 * static_cast<int64_t>(i < n_shared ? blk_begin + i : priv_begin + i - n_shared);
-    const u32x4 a = rec[0], b = rec[1];
-    r = {static_cast<int>(a[0]), static_cast<int>(a[1]), static_cast<int>(a[2]), static_cast<int>(a[3]), static_cast<int>(b[0]), static_cast<int>(b[1])};
-    return static_cast<int>(b[0] & 0xffffu) < row0 + 16 * NT && static_cast<int>(b[0] >> 16) > row0 && (r.vp_a >> 7) < st.seen_end;
-  });
-  join_rows<M, NT, kWaves>(st, w, c, lds, p.out, nullptr, p.lse, [&](int nt, int row) {
-    const int r = row_base + 16 * nt + row;
-    return r < rows ? static_cast<int64_t>(st.qtok[nt]) * sh.Hq + g * G + r % G : static_cast<int64_t>(-1);
-  });
+  load_rows<M, NT, TREE>(st, p.q, p.qt_rec, p.qt_mask, t.qt_begin, t.row_base, t.rows, t.g, sh, c);
+  const int stride = together ? kWaves : 1;
+  walk_blocks<TREE, mx_overlap(M, NT)>(
+      st, p.k_pool, p.v_pool, t.row0, c, min(end, t.n_shared + t.n_priv), begin + (together ? w : 0), stride,
+      t.n_priv >= kAlone * stride ? t.n_shared : INT_MAX,
+      [&](int i, MxLanes &r) {
+        const u32x4 *rec =
+            reinterpret_cast<const u32x4 *>(p.blocks) + 2 * static_cast<int64_t>(i < t.n_shared ? t.blk_begin + i : t.priv_begin + i - t.n_shared);
+        const u32x4 a = rec[0], b = rec[1];
+        const int lo = static_cast<int>(b[0] & 0xffffu), hi = static_cast<int>(b[0] >> 16);
+        r = {{tile_at<M>(static_cast<int>(a[0]), sh.page_tiles, t.g), tile_at<M>(static_cast<int>(a[3] != 0 ? a[2] : a[0]), sh.page_tiles, t.g)},
+             static_cast<int>(a[1]) | ((b[1] & 1) != 0 ? kMasked : 0), static_cast<int>(a[3]), static_cast<int>(b[0])};
+        return lo < t.row0 + 16 * NT && hi > t.row0 && (r.vp_a >> 7) < st.seen_end;
+      });
+  const bool whole = slot < 0;
+  float *dst = whole ? p.out : p.part_o, *ml = whole ? nullptr : p.part_ml;
+  auto place = [&](int nt, int row) {
+    const int r = t.row_base + 16 * nt + row;
+    if (r >= t.rows) return static_cast<int64_t>(-1);
+    return whole ? static_cast<int64_t>(st.qtok[nt]) * sh.Hq + t.g * G + r % G : static_cast<int64_t>(slot) + 16 * nt + row;
+  };
+  if (together)
+    join_rows<M, NT, kWaves>(st, w, c, lds, dst, ml, p.lse, place);
+  else
+    join_rows<M, NT, 1>(st, 0, c, lds + w * kOne, dst, ml, p.lse, place);
+}
+
+// Rows whose path was walked in pieces: a workgroup a row; threads of four dims each, in as many groups as fit, which take the pieces
+// in turn and are summed through LDS.  Up to 64 pieces: a lane holds the weight of one.
+template <int M, int NT>
+__global__ __launch_bounds__(256) void spex_mxfp4_merge_kernel(WalkArgs p, Shape sh, int nw, int ntw) {
+  constexpr int D = 32 * M, kLanes = D / 4, kGroups = 256 / kLanes, kBatch = (64 + kGroups - 1) / kGroups < 4 ? (64 + kGroups - 1) / kGroups : 4;
+  __shared__ __attribute__((aligned(16))) float lds[kGroups * D];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int merge = static_cast<int>(blockIdx.x) / (16 * NT), row = static_cast<int>(blockIdx.x) - merge * 16 * NT;
+  const int item = sload(p.merges, 4 * static_cast<int64_t>(merge)), part = sload(p.merges, 4 * static_cast<int64_t>(merge) + 1);
+  const int64_t slot = sload(p.merges, 4 * static_cast<int64_t>(merge) + 2);
+  const int n = sload(p.merges, 4 * static_cast<int64_t>(merge) + 3);
+  const MxSet t = load_set<NT>(p.items, item, part, nw, ntw, sh.G);
+  const int r = t.row_base + row;
+  if (r >= t.rows) return;  // the whole workgroup
+  f32x2 ml = {kNegInf, 0.f};
+  if (lane < n) ml = *reinterpret_cast<const f32x2 *>(p.part_ml + 2 * (slot + static_cast<int64_t>(lane) * 16 * NT + row));
+  const int group = tid / kLanes, d = (tid - group * kLanes) * 4;
+  const float *src = p.part_o + (slot + row) * D + d;
+  constexpr int64_t kStep = static_cast<int64_t>(16 * NT) * D;
+  f32x4 x[kBatch];
+#pragma unroll
+  for (int k = 0; k < kBatch; ++k) {
+    const int at = group + k * kGroups;
+    x[k] = *reinterpret_cast<const f32x4 *>(src + (group < kGroups && at < n ? at : 0) * kStep);
+  }
+  float m = ml[0];
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  const float weight = fast_exp2(ml[0] - m);
+  float l = weight * ml[1];
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) l += __shfl_xor(l, o);
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int i = group; i - group < n; i += kBatch * kGroups) {  // every lane goes round as often: the weights are exchanged
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int at = i + k * kGroups;
+      const float f = __shfl(weight, min(at, 63));
+      o += x[k] * (at < n ? f : 0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int at = i + (kBatch + k) * kGroups;
+      if (at < n && group < kGroups) x[k] = *reinterpret_cast<const f32x4 *>(src + at * kStep);
+    }
+  }
+  if (group < kGroups) *reinterpret_cast<f32x4 *>(lds + group * D + d) = o;
+  __syncthreads();
+  if (tid >= kLanes) return;
+#pragma unroll
+  for (int k = 1; k < kGroups; ++k) o += *reinterpret_cast<const f32x4 *>(lds + k * D + d);
+  const int qtok = sload(p.qt_rec, 2 * (static_cast<int64_t>(t.qt_begin) + r / sh.G));
+  const int64_t at = static_cast<int64_t>(qtok) * sh.Hq + t.g * sh.G + r % sh.G;
+  *reinterpret_cast<f32x4_out *>(p.out + at * D + d) = o * (1.f / l);
+  if (tid == 0 && p.lse) p.lse[at] = (m + __builtin_log2f(l)) * 0.6931471805599453f;
 }
 
 // f(integral constant M)
@@ -512,9 +748,6 @@ hipError_t with_blocks(int head_dim, F f) {
   return hipErrorInvalidValue;
 }
 
-// Row tiles of a workgroup: two where there are rows for them; wide heads have registers for one.
-constexpr int mx_row_tiles(int blocks) { return blocks <= 4 ? 2 : 1; }
-
 template <int M, int NT>
 hipError_t launch_split(const Shape &sh, const AttnArgs &a, const ItemLists &l, hipStream_t stream) {
   int64_t n_wg = 0;
@@ -531,13 +764,14 @@ hipError_t launch_split(const Shape &sh, const AttnArgs &a, const ItemLists &l, 
 
 template <int M, int NT>
 hipError_t launch_walk(const Shape &sh, const WalkArgs &a, int ntw, int waves, hipStream_t stream) {
-  const int64_t n_wg = (static_cast<int64_t>(a.n_items) + 7) / 8 * 8 * waves * (ntw / NT);
-  if (n_wg > INT32_MAX) return hipErrorInvalidValue;
-  const dim3 grid(static_cast<unsigned>(n_wg)), block(64 * kWaves);
+  const dim3 grid(static_cast<unsigned>(a.n_pieces / kWaves)), block(64 * kWaves);
   if (a.qt_mask)
     hipLaunchKernelGGL((spex_mxfp4_walk_kernel<M, NT, true>), grid, block, 0, stream, a, sh, waves, ntw);
   else
     hipLaunchKernelGGL((spex_mxfp4_walk_kernel<M, NT, false>), grid, block, 0, stream, a, sh, waves, ntw);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.n_merges == 0) return e;
+  hipLaunchKernelGGL((spex_mxfp4_merge_kernel<M, NT>), dim3(static_cast<unsigned>(a.n_merges) * 16 * NT), dim3(256), 0, stream, a, sh, waves, ntw);
   return hipGetLastError();
 }
 
@@ -547,16 +781,16 @@ hipError_t launch_mxfp4_split(const Shape &sh, const AttnArgs &a, const ItemList
   return with_blocks(sh.D, [&](auto m) {
     constexpr int M = decltype(m)::value;
     return std::max({l.span[0], l.span[1], l.span[2], l.span[3]}) <= 16 ? launch_split<M, 1>(sh, a, l, stream)
-                                                                       : launch_split<M, mx_row_tiles(M)>(sh, a, l, stream);
+                                                                       : launch_split<M, mx_row_tiles(32 * M, 2)>(sh, a, l, stream);
   });
 }
 
 hipError_t launch_mxfp4_walk(const Shape &sh, const WalkArgs &a, int ntw, int waves, hipStream_t stream) {
-  if (a.n_items <= 0) return hipSuccess;
+  if (a.n_pieces <= 0) return hipSuccess;
   if ((ntw != 1 && ntw != 2 && ntw != 4) || (waves != 2 && waves != 4 && waves != 8)) return hipErrorInvalidValue;
   return with_blocks(sh.D, [&](auto m) {
     constexpr int M = decltype(m)::value;
-    return ntw == 1 ? launch_walk<M, 1>(sh, a, ntw, waves, stream) : launch_walk<M, mx_row_tiles(M)>(sh, a, ntw, waves, stream);
+    return ntw == 1 ? launch_walk<M, 1>(sh, a, ntw, waves, stream) : launch_walk<M, mx_row_tiles(32 * M, 2)>(sh, a, ntw, waves, stream);
   });
 }
 

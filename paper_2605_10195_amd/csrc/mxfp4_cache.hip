@@ -170,7 +170,7 @@ __global__ __launch_bounds__(256) void spex_mxfp4_append_kernel(RotateArgs a, Sh
         }
       }
       if ((chunk & 3) == 0) {
-        char *dst = tile + mx_scale_at<M>(chunk >> 2, 4 * tg);
+        char *dst = tile + mx_value_scale_at<M>(chunk >> 2, tg);
         if (whole) {
           *reinterpret_cast<uint32_t *>(dst) = scales;
         } else {
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(256) void spex_mxfp4_append_kernel(RotateArgs a, Sh
       if (!live) continue;
       char *tile = static_cast<char *>(a.k_pool) + (tile0 + gi) * mx_tile_bytes(M);
       *reinterpret_cast<uint32_t *>(tile + mx_key_at<M>(chunk, pv.lo + t)) = encode_chunk(e, mx_scale(b));
-      if ((chunk & 3) == 0) tile[mx_scale_at<M>(chunk >> 2, pv.lo + t)] = static_cast<char>(token ? b : kEmptyScale);
+      if ((chunk & 3) == 0) tile[mx_key_scale_at<M>(chunk >> 2, pv.lo + t)] = static_cast<char>(token ? b : kEmptyScale);
     } else {
       const int i = (j - v_jobs - k_jobs) * RW + sub, t = i / nq, head = g0 * sh.G + i - t * nq;
       if (sub >= RW || i >= n_q) continue;
@@ -246,20 +246,20 @@ __global__ __launch_bounds__(256) void spex_mxfp4_read_kernel(ReadBackArgs a, Sh
       uint32_t w[4], c[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const uint32_t *>(tile + mx_value_at<M>(4 * chunk + k, tg));
-      const uint32_t scales = *reinterpret_cast<const uint32_t *>(tile + mx_scale_at<M>(chunk >> 2, 4 * tg));
+      const uint32_t scales = *reinterpret_cast<const uint32_t *>(tile + mx_value_scale_at<M>(chunk >> 2, tg));
       transpose_bytes(w, c);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int s = 4 * tg + k;
         if (s < lo || s >= hi) continue;
-        put_values<WIDE>(a.v_out, row_of(s - lo, gi), c[k], mx_scale((scales >> (8 * k)) & 255));
+        put_values<WIDE>(a.v_out, row_of(s - lo, gi), c[k], mx_scale(scales, k));
       }
     } else {
       const int i = (j - v_jobs) * RW + sub, t = i / ng, gi = i - t * ng;
       if (i >= n_k) continue;
       const char *tile = static_cast<const char *>(a.k_pool) + (tile0 + gi) * mx_tile_bytes(M);
       const uint32_t w = *reinterpret_cast<const uint32_t *>(tile + mx_key_at<M>(chunk, lo + t));
-      put_values<WIDE>(a.k_out, row_of(t, gi), w, mx_scale(static_cast<uint8_t>(tile[mx_scale_at<M>(chunk >> 2, lo + t)])));
+      put_values<WIDE>(a.k_out, row_of(t, gi), w, mx_scale(static_cast<uint8_t>(tile[mx_key_scale_at<M>(chunk >> 2, lo + t)])));
     }
   }
 }

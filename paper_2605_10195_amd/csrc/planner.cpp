@@ -139,6 +139,11 @@ Chunks choose_chunks(const std::vector<Run> &groups, const std::vector<Run> &suf
   return c;
 }
 
+// Pieces of the walk over MXFP4 pools, in blocks of 32 tokens: lists up to kWholeBlocks stay whole, pieces have kPieceBlocks at least, a
+// set kMostPieces at most.  A cut costs a second launch: paths of 60 to 90 blocks on 30 to 250 workgroups took 14 to 17 us whole and 15 to
+// 24 in pieces of 16.
+constexpr int64_t kWholeBlocks = 96, kPieceBlocks = 32, kMostPieces = 64;
+
 struct Segment {
   std::vector<int32_t> ids, valid, pos;
   std::vector<int32_t> last_of;  // node whose last page the entry is, else -1
@@ -753,6 +758,12 @@ bool Planner::prefers_walk(const PageTable &pt, Plan *plan) {
   Plan &pl = *plan;
   if (pl.route >= 0) return pl.route == 1;
   bool walk = false;
+  if (pool.mxfp4) {  // long paths go in pieces: the walk serves every shape that has lists
+    ensure_walk(pt, &pl);
+    walk = pl.walk_ok && (pl.req_masks.empty() || pl.walk_waves != 2);
+    pl.route = walk ? 1 : 0;
+    return walk;
+  }
   if (pl.has_walk || !obviously_split(pl)) {  // few requests with long paths: no need to build the lists
     ensure_walk(pt, &pl);
     // masks: see the kernel that splits the path
@@ -860,7 +871,14 @@ void Planner::ensure_walk(const PageTable &pt, Plan *plan) {
   int32_t ntw = walk_row_tiles;
   if (ntw == 0) {
     if (G > 64) return;
-    if (max_rows <= 16) {
+    if (pool.mxfp4) {
+      // Two tiles convert a block once for twice the rows, but leave half the wavefronts, and two of them on a SIMD instead of three.  Heads
+      // of 128, one tile / two, us: 6100 wavefronts of two tiles 170 / 155, 3300 221 / 207, 2050 182 / 171, 1600 68.4 / 68.9, 1200 16.2 / 19.7.
+      int64_t sets = 0;
+      for (int64_t r : root_rows) sets += (r + 31) / 32;
+      ntw = mx_row_tiles(pool.head_dim, 2) == 2 && sets * num_kv_heads >= 4 * 256 * mx_occupancy(pool.head_dim, 2) ? 2 : 1;
+      while (G > 16 * ntw) ntw *= 2;
+    } else if (max_rows <= 16) {
       ntw = 1;
       if (*std::max_element(root_rows.begin(), root_rows.end()) > 64) {
         // Two tiles per wavefront halve the number of row blocks that walk a wide root's shared
@@ -1223,6 +1241,103 @@ void Planner::ensure_walk(const PageTable &pt, Plan *plan) {
   pl.walk_ok = true;
   pl.walk_halves = walk_in_halves(pl);
   pl.walk_by_tile = walk_by_tile(pl);
+  if (pool.mxfp4) build_pieces(&pl);
+}
+
+// MXFP4 pools: the workgroups of the walk.  A set of rows is 16 * mx_row_tiles() of a wavefront of the lists; it has the row block's
+// shared blocks and then the wavefront's private ones.  Four sets are a workgroup, a wavefront each, or the four wavefronts of one take a
+// set's blocks in turn (`together`), which is four times the workgroups and a quarter of their steps: whichever takes fewer steps in
+// all, with about two for a wavefront to start and one more for four to join.  Lists much longer than the others', or few of
+// them, are cut into pieces of about equal length, together too, whose states a second launch merges.
+// The last piece of a set ends where its list does, so that blocks started by appends fall to it.  Launch order: workgroups that read the
+// same blocks go to one XCD, whose L2 they share, the one with the least work so far; the XCDs' lists are dealt in turn, short ones padded.
+void Planner::build_pieces(Plan *plan) const {
+  Plan &pl = *plan;
+  const int32_t NW = pl.walk_waves, ints = pl.item_ints(), G = pl.num_q_heads / pl.num_kv_heads;
+  const int32_t tiles = mx_row_tiles(pool.head_dim, pl.walk_row_tiles), groups = pl.walk_row_tiles / tiles;
+  const int32_t n_items = static_cast<int32_t>(pl.walk_items.size()) / ints;
+  auto rows_of = [&](const int32_t *rec, int32_t w) { return rec[3 + 2 * NW + w] * G; };
+  auto blocks_of = [&](const int32_t *rec, int32_t w) { return rec[2] + (rec[3 + w] & 0xffff); };
+  int64_t total = 0, sets = 0;
+  for (int32_t i = 0; i < n_items; ++i) {
+    const int32_t *rec = &pl.walk_items[static_cast<size_t>(i) * ints];
+    for (int32_t w = 0; w < NW; ++w) {
+      const int64_t n = (rows_of(rec, w) + 16 * tiles - 1) / (16 * tiles);
+      sets += n;
+      total += blocks_of(rec, w) * n;
+    }
+  }
+  if (sets == 0) return;
+  const int64_t resident = 256 * mx_occupancy(pool.head_dim, tiles), mean = (total + sets - 1) / sets;  // workgroups; blocks
+  const int64_t steps_alone = (sets + 4 * resident - 1) / (4 * resident) * (mean + 2);
+  const int64_t steps_together = (sets + resident - 1) / resident * ((mean + 3) / 4 + 3);
+  const bool all_together = steps_together <= steps_alone;
+  int64_t length = std::max<int64_t>(kPieceBlocks, (total + resident - 1) / resident);
+  const int64_t most_alone = 3 * std::max<int64_t>(kWholeBlocks, (total + 4 * resident - 1) / (4 * resident)) / 2;
+  auto pieces_of = [&](int64_t blocks) -> int64_t {
+    if (blocks <= kWholeBlocks || 2 * blocks <= 3 * length) return 1;
+    return std::min((blocks + length - 1) / length, kMostPieces);
+  };
+  auto each_set = [&](int32_t i, auto f) {  // f(wavefront, tile set, blocks)
+    const int32_t *rec = &pl.walk_items[static_cast<size_t>(i) * ints];
+    for (int32_t w = 0; w < NW; ++w)
+      for (int32_t s = 0; s < groups && s * 16 * tiles < rows_of(rec, w); ++s) f(w, s, static_cast<int64_t>(blocks_of(rec, w)));
+  };
+  if (all_together && sets <= resident)  // a few pieces more than run at a time would take a round of their own
+    for (int64_t n = resident + 1; n > resident;) {
+      n = 0;
+      for (int32_t i = 0; i < n_items; ++i) each_set(i, [&](int32_t, int32_t, int64_t blocks) { n += pieces_of(blocks); });
+      if (n > resident) length += std::max<int64_t>(1, length * (n - resident) / resident);
+    }
+  int64_t rows = 0, load[8] = {0};
+  std::vector<int32_t> of_xcd[8], alone;
+  std::vector<std::vector<int32_t>> units;  // workgroups of one XCD: an item's sets, or its sets' pieces of the same blocks
+  const std::vector<int32_t> none = {-1, 0, 0, 0, -1, 0, 0, 0};
+  constexpr size_t kGroup = static_cast<size_t>(4) * Plan::kPieceInts;
+  auto fill = [&](std::vector<int32_t> *out) {
+    while (out->size() % kGroup != 0) out->insert(out->end(), none.begin(), none.end());
+  };
+  auto place = [&](const std::vector<int32_t> &unit, int64_t steps) {
+    if (unit.empty()) return;
+    const int x = static_cast<int>(std::min_element(load, load + 8) - load);
+    of_xcd[x].insert(of_xcd[x].end(), unit.begin(), unit.end());
+    load[x] += steps * static_cast<int64_t>(unit.size() / kGroup);
+  };
+  for (int32_t i = 0; i < n_items; ++i) {
+    alone.clear();
+    units.clear();
+    int64_t longest_alone = 0, longest = 0;
+    each_set(i, [&](int32_t w, int32_t s, int64_t n) {
+      const bool together = all_together || n > most_alone;
+      const int64_t count = together ? pieces_of(n) : 1;
+      if (count > 1) pl.walk_merges.insert(pl.walk_merges.end(), {i, w | s << 8, static_cast<int32_t>(rows), static_cast<int32_t>(count)});
+      if (together && count > static_cast<int64_t>(units.size())) units.resize(static_cast<size_t>(count));
+      for (int64_t p = 0; p < count; ++p) {
+        const int32_t end = p + 1 == count ? std::numeric_limits<int32_t>::max() : static_cast<int32_t>(n * (p + 1) / count);
+        std::vector<int32_t> *to = together ? &units[static_cast<size_t>(p)] : &alone;
+        const int32_t begin = static_cast<int32_t>(n * p / count), slot = count > 1 ? static_cast<int32_t>(rows) : -1;
+        for (int k = together ? 4 : 1; k > 0; --k) to->insert(to->end(), {i, w | s << 8, begin, end, slot, together, 0, 0});
+        if (count > 1) rows += 16 * tiles;
+      }
+      if (together)
+        longest = std::max(longest, (n / count + 3) / 4);
+      else
+        longest_alone = std::max(longest_alone, n);
+    });
+    fill(&alone);
+    place(alone, longest_alone + 2);
+    for (const std::vector<int32_t> &unit : units) place(unit, longest + 3);
+  }
+  size_t most = 0;
+  for (const std::vector<int32_t> &of : of_xcd) most = std::max(most, of.size());
+  for (size_t at = 0; at < most; at += kGroup)
+    for (const std::vector<int32_t> &of : of_xcd) {
+      if (at < of.size())
+        pl.walk_pieces.insert(pl.walk_pieces.end(), of.begin() + at, of.begin() + at + kGroup);
+      else
+        for (int32_t k = 0; k < 4; ++k) pl.walk_pieces.insert(pl.walk_pieces.end(), none.begin(), none.end());
+    }
+  pl.walk_partial_rows = rows;
 }
 
 // Appends to requested nodes since the plan was made (no fork, no prune): the lists stay as they

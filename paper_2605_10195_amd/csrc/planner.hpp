@@ -115,6 +115,13 @@ struct Plan {
   //   row block index in the last int}; a padding item has row block index -1 and no blocks
   int item_ints() const { return walk_waves <= 4 ? 16 : 32; }
   std::vector<int32_t> walk_items;
+  // MXFP4 pools, see Planner::build_pieces.  A wavefront's piece is kPieceInts ints, four to a workgroup:
+  //   {work item (-1: none, padding), wavefront of rows | row tile set << 8, first block, block behind the last, first row of its
+  //    partial state (-1: none, it finishes its rows), shared with the workgroup's others, 0, 0}
+  // merges: {work item, wavefront | set << 8, first row of the partial states, pieces} of every set of rows with several.
+  static constexpr int kPieceInts = 8, kMergeInts = 4;
+  std::vector<int32_t> walk_pieces, walk_merges;
+  int64_t walk_partial_rows = 0;
   int32_t walk_real_items = 0;       // workgroups with work
   int32_t walk_max_item_blocks = 0;  // longest workgroup: shared blocks + most private blocks of a wavefront
   int64_t walk_tiles_touched = 0, walk_tiles_held = 0;  // row tiles a block's rows lie in / its wavefronts hold, over all blocks
@@ -135,6 +142,7 @@ struct PoolShape {
   bool tiled = false;    // MFMA-tiled: the tree-walk kernel and the split path's launches in phases exist
   bool generic = false;  // neither tiled nor fit for the row-major kernel
   int32_t head_dim = 128, kv_bytes = 2;
+  bool mxfp4 = false;    // (tiled as well) the kernels of mxfp4_attention.hip
 };
 
 enum class PlanError { kOk, kBadNode, kEmptyPath, kInvalid, kTooLarge };
@@ -170,6 +178,7 @@ class Planner {
   static float estimate_walk(const Plan &plan);
   bool walk_in_halves(const Plan &plan) const;
   bool walk_by_tile(const Plan &plan) const;
+  void build_pieces(Plan *plan) const;
   std::vector<int32_t> multi_, last_pg_;
   std::vector<int32_t> stamp_, slot_;  // per-node scratch of build_walk, valid where stamp_ == current stamp
   // scratch of the request ordering in ensure_walk: pre-order rank and child ranges per node,

@@ -25,6 +25,7 @@ struct DevicePlan {
   const int32_t *part_indptr = nullptr, *part_base = nullptr, *part_hstride = nullptr, *merge_qt = nullptr;
   const int32_t *coop_items[2] = {nullptr, nullptr};
   const int32_t *walk_items = nullptr, *walk_blocks = nullptr, *walk_qt = nullptr, *qt_mask = nullptr;
+  const int32_t *walk_pieces = nullptr, *walk_merges = nullptr;
 };
 
 }  // namespace spex
@@ -38,7 +39,7 @@ struct spex_tree {
   bool plan_on_device = false, device_has_split = false, device_has_walk = false;
   bool plan_patched_by_append = false;  // the cached plan was brought up to date by an append call
   spex::DevicePlan dplan;
-  size_t blob_off[14] = {}, blob_ints[14] = {};  // byte offset and length of each list in the blob
+  size_t blob_off[16] = {}, blob_ints[16] = {};  // byte offset and length of each list in the blob
   std::vector<int32_t> pending_patches;          // {array, index, value} not yet on the device
   void *d_patch = nullptr;
   size_t d_patch_cap = 0;

@@ -1,0 +1,115 @@
+"""The workgroups of the tree walk over MXFP4 pools: their lists on the host, and attention through every kind of them."""
+
+import os
+import shutil
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_10195_amd as spex
+from mxfp4_common import quantised
+from test_host_sanitizers import CSRC, HERE, build_with_sanitizers
+from test_mxfp4_attention import Forest
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+def test_lists_of_pieces_under_sanitizers(tmp_path):
+    exe = str(tmp_path / "mxfp4_pieces")
+    build_with_sanitizers(exe, [os.path.join(HERE, "mxfp4_pieces.cpp"), os.path.join(CSRC, "planner.cpp"), os.path.join(CSRC, "page_table.cpp")])
+    run = subprocess.run([exe, "120"], capture_output=True, text=True, timeout=600)
+    assert run.returncode == 0, (run.stdout[-2000:], run.stderr[-4000:])
+    assert run.stdout == "ok\n", run.stdout
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [(4, 2, 32), (8, 1, 64), (6, 2, 96), (8, 2, 128), (2, 1, 160), (3, 1, 192), (4, 1, 224), (4, 1, 256), (40, 1, 128)])
+@pytest.mark.parametrize("tiles", [0, 2])
+def test_long_paths_in_pieces(heads, tiles):
+    """Few requests on long paths: their states are merged by a second launch."""
+    f = Forest(heads, [(-1, 5003), (0, 70), (0, 1), (-1, 4100), (-1, 9)], seed=heads[2] + tiles, kernel_mode=3, walk_row_tiles=tiles)
+    if tiles and heads[0] // heads[1] > 16 * tiles:  # a token's rows stay together
+        with pytest.raises(spex.SpexError, match="UNSUPPORTED"):
+            f.check([1, 2, 3, 4])
+        f.tree.close()
+        return
+    f.check([1, 2, 3, 4])
+    assert f.tree.last_launch_info()["partial_rows"] > 0
+    f.check([2])
+    f.check([1, 3, 1], [5, 3, 1])
+    f.tree.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [(16, 16, 32), (16, 8, 64), (8, 8, 128)])
+def test_many_short_paths(heads):
+    """Enough sets of rows for a wavefront each, with a path among them that takes four, and one that goes in pieces."""
+    nodes = [(-1, 1 + 7 * i % 50) for i in range(400)] + [(-1, 5500), (-1, 14000)]
+    f = Forest(heads, nodes, seed=heads[2])
+    f.check(list(range(402)))
+    assert f.tree.last_launch_info()["partial_rows"] > 0
+    f.tree.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [(8, 2, 128), (10, 2, 64), (28, 4, 96), (5, 1, 32)])
+@pytest.mark.parametrize("tokens", [70, 300])
+def test_branches_within_a_row_tile(heads, tokens):
+    """Two row tiles, and private blocks that concern one of them, the other, or both: from 16 a wavefront on they are taken apart."""
+    nodes = [(-1, 45)] + [(0, tokens + i) for i in range(16)]
+    f = Forest(heads, nodes, seed=heads[0], kernel_mode=3, walk_row_tiles=2)
+    leaves = list(range(1, 17))
+    f.check(leaves)
+    f.check(leaves[:5], [1, 3, 1, 2, 1])
+    masks = np.concatenate([1 << np.arange(n) for n in [2] * 16]).astype(np.uint32)
+    f.check(leaves, [2] * 16, masks)
+    f.tree.close()
+
+
+@pytest.mark.gpu
+def test_pieces_that_grow():
+    """Appends to branches of a path in pieces: the last piece takes what they start, eagerly and in a graph that is captured again."""
+    f = Forest((8, 2, 128), [(-1, 6000)] + [(0, 14 + i) for i in range(4)], seed=3, spare=40)
+    leaves = [1, 2, 3, 4]
+    ids = [f.ids[u] for u in leaves]
+    states = set()
+    for step in range(36):
+        x = torch.as_tensor(f.rng.standard_normal((2, 4, 2, 128))).to(torch.bfloat16)
+        f.tree.append_tokens(ids, x[0].cuda(), x[1].cuda(), quantize=True)
+        for i, u in enumerate(leaves):
+            f.k[u] = np.concatenate([f.k[u], quantised(x[0, i].double().numpy(), "k")[None]])
+            f.v[u] = np.concatenate([f.v[u], quantised(x[1, i].double().numpy(), "v")[None]])
+        f.check(leaves)
+        states.add(f.tree.last_launch_info()["plan_rebuilt"])
+        assert f.tree.last_launch_info()["partial_rows"] > 0
+    assert 2 in states  # some plans were patched
+    q = torch.as_tensor(f.rng.standard_normal((4, 8, 128))).to(torch.bfloat16).cuda()
+    out, lse = f.tree.decode_attention(ids, None, q, 128 ** -0.5)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        f.tree.decode_attention(ids, None, q, 128 ** -0.5, out, lse)
+    for i in range(4):
+        out.fill_(float("nan"))
+        q.mul_(1.5)
+        graph.replay()
+        torch.cuda.synchronize()
+        eager, eager_lse = f.tree.decode_attention(ids, None, q, 128 ** -0.5)
+        assert torch.equal(out, eager) and torch.equal(lse, eager_lse)
+    f.check(leaves, static=True)
+    f.tree.close()
+
+
+@pytest.mark.gpu
+def test_pieces_of_far_scores():
+    """Scores far from zero, whose references differ from piece to piece, and rows that one piece of many decides."""
+    def value(rng, shape):
+        x = rng.standard_normal(shape) * 3
+        x[shape[0] // 3] *= 20
+        return x
+
+    f = Forest((8, 2, 128), [(-1, 7000), (0, 33)], seed=5, value=value, kernel_mode=3)
+    f.check([0, 1], spread=8.0, loose=1e-4)
+    assert f.tree.last_launch_info()["partial_rows"] > 0
+    f.tree.close()
