@@ -216,11 +216,12 @@ struct MxScores {
   f32x4 s[NT][2];
 };
 // (T0, T1: the first row tile concerned, and the one behind the last.)
-template <int T0, int T1, int M, int NT>
+template <int T0, int T1, bool OVERLAP, int M, int NT>
 __device__ __forceinline__ void block_scores(MxScores<NT> &y, const MxRows<M, NT> &st, const MxKeys<M> &x) {
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
     float scale[MxKeys<M>::kScales];
+    if (!OVERLAP && p == 1) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < MxKeys<M>::kScales; ++i) scale[i] = mx_scale(x.scale[p][i]);
 #pragma unroll
@@ -253,8 +254,37 @@ __device__ __forceinline__ void mask_block(MxScores<NT> &y, const MxRows<M, NT> 
   }
 }
 
+// x *= by and x -= by.  IN_PLACE: in assembly, because the compiler gives results in a branch registers of their own and copies them back, 36 of
+// them for a head of 128.  (Not where blocks overlap: there it would copy for the assembly what it does not copy without.)
+template <bool IN_PLACE>
+__device__ __forceinline__ void scale_by(f32x4 &x, const f32x4 by) {
+  if constexpr (IN_PLACE) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float e = x[i];
+      asm("v_mul_f32 %0, %1, %0" : "+v"(e) : "v"(by[i]));
+      x[i] = e;
+    }
+  } else {
+    x *= by;
+  }
+}
+template <bool IN_PLACE>
+__device__ __forceinline__ void lower_by(f32x4 &x, float by) {
+  if constexpr (IN_PLACE) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float e = x[i];
+      asm("v_sub_f32 %0, %0, %1" : "+v"(e) : "v"(by));
+      x[i] = e;
+    }
+  } else {
+    x -= by;
+  }
+}
+
 // Moves the references that a block's scores are far above; scores of far rows become differences to theirs.
-template <int T0, int T1, int M, int NT>
+template <int T0, int T1, bool OVERLAP, int M, int NT>
 __device__ __forceinline__ void move_references(MxRows<M, NT> &st, MxScores<NT> &y, float c, float slack) {
   float top[NT];
   bool above = false;
@@ -275,17 +305,17 @@ __device__ __forceinline__ void move_references(MxRows<M, NT> &st, MxScores<NT> 
       f32x4 of_rows;  // the lane's accumulators are of four rows
 #pragma unroll
       for (int i = 0; i < 4; ++i) of_rows[i] = __shfl(alpha, 4 * (static_cast<int>(threadIdx.x & 63) >> 4) + i);
-      st.l[nt] *= of_rows;
+      scale_by<!OVERLAP>(st.l[nt], of_rows);
 #pragma unroll
-      for (int i = 0; i < 2 * M; ++i) st.o[nt][i] *= of_rows;
+      for (int i = 0; i < 2 * M; ++i) scale_by<!OVERLAP>(st.o[nt][i], of_rows);
     }
   }
   if (st.far) {
 #pragma unroll
     for (int nt = T0; nt < T1; ++nt) {
-      y.s[nt][0] -= st.m[nt];
-      y.s[nt][1] -= st.m[nt];
-      st.mc[nt] = -kWeightLog2;
+      lower_by<!OVERLAP>(y.s[nt][0], st.m[nt]);
+      lower_by<!OVERLAP>(y.s[nt][1], st.m[nt]);
+      if (OVERLAP) st.mc[nt] = -kWeightLog2;
     }
   }
 }
@@ -297,8 +327,9 @@ __device__ __forceinline__ void block_values(MxRows<M, NT> &st, const MxScores<N
 #pragma unroll
   for (int nt = T0; nt < T1; ++nt) {
     float w[8];
+    const float mc = !OVERLAP && st.far ? -kWeightLog2 : st.mc[nt];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = fast_exp2(__builtin_fmaf(y.s[nt][i >> 2][i & 3], c, -st.mc[nt]));
+    for (int i = 0; i < 8; ++i) w[i] = fast_exp2(__builtin_fmaf(y.s[nt][i >> 2][i & 3], c, -mc));
     u32x4 h, rest;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -326,6 +357,7 @@ __device__ __forceinline__ void block_values(MxRows<M, NT> &st, const MxScores<N
     // two tokens of one dim.  So the product is one over (token, dim) pairs of which every second weight is zero: the sparse one,
     // which takes two of four at a dense product's rate; kEvenDims and kOddDims choose d and d + 1.  It wants a lane's values in the
     // order in which load_values has taken them.
+    if (!OVERLAP && j > 0 && j % 2 == 0) __builtin_amdgcn_sched_barrier(0);
     u32x8 r;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -452,25 +484,25 @@ __device__ __forceinline__ void join_rows(MxRows<M, NT> &st, int ks, float c, fl
 }
 
 constexpr int kWaves = 4;  // of a workgroup
-// Private blocks of a set from which on those of one row tile have rounds of their own: 64 branches of four rows each, eight blocks long, took
+// Private blocks of a set from which on those of one row tile have rounds of their own: 64 trees of 32 branches of eight blocks took
 // 171 us without and 160 with; two or three blocks a branch 140 and 152.
 constexpr int kAlone = 16;
 
 // The blocks of one of the wavefronts that hold the same rows: every stride-th record of a list, 64 of them at a time in registers, a lane
 // each.  read(i, r): record i, for a lane; false where it does not concern the wavefront's rows.
 struct MxLanes {
-  int64_t at[2];
-  int vp_a, vp_b, rows;
+  int page[2], vp_a, vp_b, rows;
 };
 template <int M>
 __device__ __forceinline__ int64_t tile_at(int page, int page_tiles, int g) {
   return (static_cast<int64_t>(page) * page_tiles + g) * mx_tile_bytes(M);
 }
+// Rows from row_end on are not there and need no mask (eight of sixteen rows on 48 paths of 16000 tokens: 30 us with one, 26 without).
 // Records from number `alone` on whose rows lie in one tile are left out of those for all tiles, and are the only ones of a single tile.
-template <int T0, int T1, int NT, class Read>
+template <int T0, int T1, int M, int NT, class Read>
 struct MxSource {
   Read read;
-  int n, at, stride, alone, row0;
+  int n, at, stride, alone, row0, row_end, g, page_tiles;
   bool &left_out;
   uint64_t left;
   MxLanes r;
@@ -487,7 +519,7 @@ struct MxSource {
       } else if (NT > 1) {
         concerns = concerns && (T0 == 0 ? hi <= row0 + 16 : lo >= row0 + 16);
       }
-      if (lo > row0 + 16 * T0 || hi < row0 + 16 * T1) r.vp_a |= kMasked;
+      if (lo > row0 + 16 * T0 || hi < min(row0 + 16 * T1, row_end)) r.vp_a |= kMasked;
       left = __ballot(concerns);
       at += 64 * stride;
     }
@@ -497,10 +529,7 @@ struct MxSource {
     const int none = b.live ? 0 : kMasked;  // a block that is not there is one of no rows
     left &= left - 1;
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      const uint32_t low = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.at[p]), l));
-      b.at[p] = static_cast<int64_t>(__builtin_amdgcn_readlane(static_cast<int>(r.at[p] >> 32), l)) << 32 | low;
-    }
+    for (int p = 0; p < 2; ++p) b.at[p] = tile_at<M>(__builtin_amdgcn_readlane(r.page[p], l), page_tiles, g);
     b.vp_a = __builtin_amdgcn_readlane(r.vp_a, l) | none;
     b.vp_b = __builtin_amdgcn_readlane(r.vp_b, l);
     b.rows = b.live ? __builtin_amdgcn_readlane(r.rows, l) : 0;
@@ -512,10 +541,10 @@ struct MxSource {
 // of the block before, so that matrix and vector instructions of one wavefront run at the same time; keys are requested two blocks ahead,
 // values one.  Otherwise a block at a time, the next one's keys and values requested where this one's have been used.
 template <int T0, int T1, bool TREE, bool OVERLAP, int M, int NT, class Read>
-__device__ __forceinline__ void walk_tiles(MxRows<M, NT> &st, const void *k, const void *v, int row0, float c, int n, int first, int stride,
-                                           int alone, bool &left_out, Read read) {
+__device__ __forceinline__ void walk_tiles(MxRows<M, NT> &st, const void *k, const void *v, int row0, int row_end, float c, int n, int first,
+                                           int stride, int alone, int g, int page_tiles, bool &left_out, Read read) {
   const float slack = kSlackLog2 / c;
-  MxSource<T0, T1, NT, Read> src{read, n, first, stride, alone, row0, left_out, 0, {}};
+  MxSource<T0, T1, M, NT, Read> src{read, n, first, stride, alone, row0, row_end, g, page_tiles, left_out, 0, {}};
   MxKeys<M> k0;
   MxValues<M> v0;
   MxScores<NT> y0;
@@ -529,15 +558,15 @@ __device__ __forceinline__ void walk_tiles(MxRows<M, NT> &st, const void *k, con
     MxScores<NT> y1;
     MxBlock b1 = src.next();
     load_keys<M>(k1, b1, k);
-    block_scores<T0, T1>(y0, st, k0);
+    block_scores<T0, T1, OVERLAP>(y0, st, k0);
     mask_block<T0, T1, TREE>(y0, st, b0, row0);
     // y, x: of block b; the block behind it has its keys in nk and its place in nb, the one behind that is requested into b and k
     auto step = [&](MxScores<NT> &y, MxValues<M> &x, MxKeys<M> &key, MxBlock &b, MxScores<NT> &ny, MxValues<M> &nx, MxKeys<M> &nk, MxBlock &nb) {
       b = src.next();
       load_keys<M>(key, b, k);
       load_values<M>(nx, nb, v);
-      move_references<T0, T1>(st, y, c, slack);
-      block_scores<T0, T1>(ny, st, nk);
+      move_references<T0, T1, OVERLAP>(st, y, c, slack);
+      block_scores<T0, T1, OVERLAP>(ny, st, nk);
       block_values<T0, T1, OVERLAP>(st, y, x, c);
       mask_block<T0, T1, TREE>(ny, st, nb, row0);
     };
@@ -546,35 +575,37 @@ __device__ __forceinline__ void walk_tiles(MxRows<M, NT> &st, const void *k, con
       step(y1, v1, k1, b1, y0, v0, k0, b0);
     } while (b0.live);
   } else {
-    do {
-      const MxBlock b = b0;
-      b0 = src.next();
-      block_scores<T0, T1>(y0, st, k0);
-      load_keys<M>(k0, b0, k);
+    auto step = [&](MxKeys<M> &key, MxValues<M> &x, MxBlock &at) {
+      const MxBlock b = at;
+      at = src.next();
+      block_scores<T0, T1, OVERLAP>(y0, st, key);
+      load_keys<M>(key, at, k);
       mask_block<T0, T1, TREE>(y0, st, b, row0);
-      move_references<T0, T1>(st, y0, c, slack);
-      block_values<T0, T1, OVERLAP>(st, y0, v0, c);
-      load_values<M>(v0, b0, v);
-    } while (b0.live);
+      move_references<T0, T1, OVERLAP>(st, y0, c, slack);
+      block_values<T0, T1, OVERLAP>(st, y0, x, c);
+      load_values<M>(x, at, v);
+    };
+    do step(k0, v0, b0);
+    while (b0.live);
   }
 }
 // Of two tiles, blocks that concern one of them only have rounds of their own from record `alone` on: half the products and weights.
 template <bool TREE, bool OVERLAP, int M, int NT, class Read>
-__device__ __forceinline__ void walk_blocks(MxRows<M, NT> &st, const void *k, const void *v, int row0, float c, int n, int first, int stride,
-                                            int alone, Read read) {
+__device__ __forceinline__ void walk_blocks(MxRows<M, NT> &st, const void *k, const void *v, int row0, int row_end, float c, int n, int first,
+                                            int stride, int alone, int g, int page_tiles, Read read) {
   bool left_out = false;
-  walk_tiles<0, NT, TREE, OVERLAP>(st, k, v, row0, c, n, first, stride, alone, left_out, read);
+  walk_tiles<0, NT, TREE, OVERLAP>(st, k, v, row0, row_end, c, n, first, stride, alone, g, page_tiles, left_out, read);
   if constexpr (NT == 2) {
     if (!left_out) return;
     const int from = first >= alone ? first : first + (alone - first + stride - 1) / stride * stride;
-    walk_tiles<0, 1, TREE, OVERLAP>(st, k, v, row0, c, n, from, stride, alone, left_out, read);
-    walk_tiles<1, 2, TREE, OVERLAP>(st, k, v, row0, c, n, from, stride, alone, left_out, read);
+    walk_tiles<0, 1, TREE, OVERLAP>(st, k, v, row0, row_end, c, n, from, stride, alone, g, page_tiles, left_out, read);
+    walk_tiles<1, 2, TREE, OVERLAP>(st, k, v, row0, row_end, c, n, from, stride, alone, g, page_tiles, left_out, read);
   }
 }
 
-// Overlapped where the registers for two blocks are there (heads of 128 and one tile would have two wavefronts a SIMD instead of three:
-// 177 us against 165).
-constexpr bool mx_overlap(int blocks, int row_tiles) { return row_tiles == 2 || blocks <= 2; }
+// With one row tile the registers go to more wavefronts instead, four a SIMD: 157 us for the 64 trees above, 177 with two that overlap, 165
+// with three that do not.  A second block of keys and values under way took three back and was no faster.
+constexpr bool mx_overlap(int blocks, int row_tiles) { return row_tiles == 2; }
 
 template <int M, int NT, bool TREE>
 __global__ __launch_bounds__(64 * kWaves, mx_occupancy(32 * M, NT)) void spex_mxfp4_split_kernel(AttnArgs p, Shape sh, SplitLists ls) {
@@ -590,11 +621,11 @@ __global__ __launch_bounds__(64 * kWaves, mx_occupancy(32 * M, NT)) void spex_mx
   MxRows<M, NT> st;
   load_rows<M, NT, TREE>(st, p.q, p.qt_rec, p.qt_mask, cur.qt_begin, cur.row0, rows, g, sh, c);
   const int n_blocks = (cur.pg_count + 1) >> 1;
-  walk_blocks<TREE, mx_overlap(M, NT)>(st, p.k_pool, p.v_pool, 0, c, n_blocks, w, kWaves, INT_MAX, [&](int i, MxLanes &r) {
+  walk_blocks<TREE, mx_overlap(M, NT)>(st, p.k_pool, p.v_pool, 0, INT_MAX, c, n_blocks, w, kWaves, INT_MAX, g, sh.page_tiles, [&](int i, MxLanes &r) {
     const int2 *pages = reinterpret_cast<const int2 *>(p.pg_rec) + cur.pg_begin + 2 * i;
     const bool has_b = 2 * i + 1 < cur.pg_count;
     const int2 a = pages[0], b = pages[has_b ? 1 : 0];
-    r = {{tile_at<M>(a.x, sh.page_tiles, g), tile_at<M>(b.x, sh.page_tiles, g)}, a.y | ((cur.flags & 1) || !has_b ? kMasked : 0), has_b ? b.y : 0,
+    r = {{a.x, b.x}, a.y | ((cur.flags & 1) || !has_b ? kMasked : 0), has_b ? b.y : 0,
          static_cast<int>(0xffff0000u)};
     return (a.y >> 7) < st.seen_end;
   });
@@ -651,15 +682,18 @@ __global__ __launch_bounds__(64 * kWaves, mx_occupancy(32 * M, NT)) void spex_mx
   load_rows<M, NT, TREE>(st, p.q, p.qt_rec, p.qt_mask, t.qt_begin, t.row_base, t.rows, t.g, sh, c);
   const int stride = together ? kWaves : 1;
   walk_blocks<TREE, mx_overlap(M, NT)>(
-      st, p.k_pool, p.v_pool, t.row0, c, min(end, t.n_shared + t.n_priv), begin + (together ? w : 0), stride,
-      t.n_priv >= kAlone * stride ? t.n_shared : INT_MAX,
+      st, p.k_pool, p.v_pool, t.row0, t.row0 + t.rows - t.row_base, c, min(end, t.n_shared + t.n_priv), begin + (together ? w : 0), stride,
+      t.n_priv >= kAlone * stride ? t.n_shared : INT_MAX, t.g, sh.page_tiles,
       [&](int i, MxLanes &r) {
         const u32x4 *rec =
             reinterpret_cast<const u32x4 *>(p.blocks) + 2 * static_cast<int64_t>(i < t.n_shared ? t.blk_begin + i : t.priv_begin + i - t.n_shared);
         const u32x4 a = rec[0], b = rec[1];
         const int lo = static_cast<int>(b[0] & 0xffffu), hi = static_cast<int>(b[0] >> 16);
-        r = {{tile_at<M>(static_cast<int>(a[0]), sh.page_tiles, t.g), tile_at<M>(static_cast<int>(a[3] != 0 ? a[2] : a[0]), sh.page_tiles, t.g)},
-             static_cast<int>(a[1]) | ((b[1] & 1) != 0 ? kMasked : 0), static_cast<int>(a[3]), static_cast<int>(b[0])};
+        r.page[0] = static_cast<int>(a[0]);
+        r.page[1] = static_cast<int>(a[3] != 0 ? a[2] : a[0]);
+        r.vp_a = static_cast<int>(a[1]) | ((b[1] & 1) != 0 ? kMasked : 0);
+        r.vp_b = static_cast<int>(a[3]);
+        r.rows = static_cast<int>(b[0]);
         return lo < t.row0 + 16 * NT && hi > t.row0 && (r.vp_a >> 7) < st.seen_end;
       });
   const bool whole = slot < 0;

@@ -872,8 +872,8 @@ void Planner::ensure_walk(const PageTable &pt, Plan *plan) {
   if (ntw == 0) {
     if (G > 64) return;
     if (pool.mxfp4) {
-      // Two tiles convert a block once for twice the rows, but leave half the wavefronts, and two of them on a SIMD instead of three.  Heads
-      // of 128, one tile / two, us: 6100 wavefronts of two tiles 170 / 155, 3300 221 / 207, 2050 182 / 171, 1600 68.4 / 68.9, 1200 16.2 / 19.7.
+      // Two tiles convert a block once for twice the rows, but leave half the wavefronts, and two of them on a SIMD instead of four.  Heads of
+      // 128, one tile / two, us: 6100 wavefronts of two tiles 150 / 127, 3300 198 / 186, 2050 158 / 150, 1600 66.3 / 68.4, 1200 15.5 / 20.0.
       int64_t sets = 0;
       for (int64_t r : root_rows) sets += (r + 31) / 32;
       ntw = mx_row_tiles(pool.head_dim, 2) == 2 && sets * num_kv_heads >= 4 * 256 * mx_occupancy(pool.head_dim, 2) ? 2 : 1;
@@ -1241,7 +1241,7 @@ void Planner::ensure_walk(const PageTable &pt, Plan *plan) {
   pl.walk_ok = true;
   pl.walk_halves = walk_in_halves(pl);
   pl.walk_by_tile = walk_by_tile(pl);
-  if (pool.mxfp4) build_pieces(&pl);
+  if (pool.mxfp4) build_pieces(root_order, rbs_of_root, &pl);
 }
 
 // MXFP4 pools: the workgroups of the walk.  A set of rows is 16 * mx_row_tiles() of a wavefront of the lists; it has the row block's
@@ -1249,9 +1249,13 @@ void Planner::ensure_walk(const PageTable &pt, Plan *plan) {
 // set's blocks in turn (`together`), which is four times the workgroups and a quarter of their steps: whichever takes fewer steps in
 // all, with about two for a wavefront to start and one more for four to join.  Lists much longer than the others', or few of
 // them, are cut into pieces of about equal length, together too, whose states a second launch merges.
-// The last piece of a set ends where its list does, so that blocks started by appends fall to it.  Launch order: workgroups that read the
-// same blocks go to one XCD, whose L2 they share, the one with the least work so far; the XCDs' lists are dealt in turn, short ones padded.
-void Planner::build_pieces(Plan *plan) const {
+// The last piece of a set ends where its list does, so that blocks started by appends fall to it.
+// Launch order: workgroups that read the same blocks go to one XCD, whose L2 they share, the one with the least work so far; the
+// XCDs' lists are dealt in turn, short ones padded.  Kept together are a root's sets and heads (a page's tiles lie side by side
+// and do not end with cache lines), else a root's sets of one head, else a row block's, whichever leaves the XCDs' work within a tenth of even;
+// of sets in pieces, those of the same blocks.
+void Planner::build_pieces(const std::vector<int32_t> &root_order, const std::vector<std::vector<int32_t>> &rbs_of_root,
+                           Plan *plan) const {
   Plan &pl = *plan;
   const int32_t NW = pl.walk_waves, ints = pl.item_ints(), G = pl.num_q_heads / pl.num_kv_heads;
   const int32_t tiles = mx_row_tiles(pool.head_dim, pl.walk_row_tiles), groups = pl.walk_row_tiles / tiles;
@@ -1289,44 +1293,62 @@ void Planner::build_pieces(Plan *plan) const {
       for (int32_t i = 0; i < n_items; ++i) each_set(i, [&](int32_t, int32_t, int64_t blocks) { n += pieces_of(blocks); });
       if (n > resident) length += std::max<int64_t>(1, length * (n - resident) / resident);
     }
-  int64_t rows = 0, load[8] = {0};
-  std::vector<int32_t> of_xcd[8], alone;
-  std::vector<std::vector<int32_t>> units;  // workgroups of one XCD: an item's sets, or its sets' pieces of the same blocks
+  struct Made {
+    int32_t root, g, rb, piece;  // piece: -1 for a wavefront's own set
+    int64_t steps;
+    int32_t rec[Plan::kPieceInts];
+  };
+  std::vector<Made> made;
+  int64_t rows = 0;
+  for (int32_t r : root_order)
+    for (int32_t g = 0; g < pl.num_kv_heads; ++g)
+      for (int32_t rb : rbs_of_root[r]) {
+        const int32_t i = pl.rb_item0[rb] + g;
+        each_set(i, [&](int32_t w, int32_t s, int64_t n) {
+          const bool together = all_together || n > most_alone;
+          const int64_t count = together ? pieces_of(n) : 1;
+          if (count > 1) pl.walk_merges.insert(pl.walk_merges.end(), {i, w | s << 8, static_cast<int32_t>(rows), static_cast<int32_t>(count)});
+          for (int64_t p = 0; p < count; ++p) {
+            const int32_t begin = static_cast<int32_t>(n * p / count), slot = count > 1 ? static_cast<int32_t>(rows) : -1;
+            const int32_t end = p + 1 == count ? std::numeric_limits<int32_t>::max() : static_cast<int32_t>(n * (p + 1) / count);
+            made.push_back({r, g, rb, together ? static_cast<int32_t>(p) : -1, together ? (n / count + 3) / 4 + 3 : (n + 5) / 4,
+                            {i, w | s << 8, begin, end, slot, together, 0, 0}});
+            if (count > 1) rows += 16 * tiles;
+          }
+        });
+      }
+  struct Unit {
+    std::vector<int32_t> recs;
+    int64_t steps = 0;
+  };
   const std::vector<int32_t> none = {-1, 0, 0, 0, -1, 0, 0, 0};
   constexpr size_t kGroup = static_cast<size_t>(4) * Plan::kPieceInts;
-  auto fill = [&](std::vector<int32_t> *out) {
-    while (out->size() % kGroup != 0) out->insert(out->end(), none.begin(), none.end());
-  };
-  auto place = [&](const std::vector<int32_t> &unit, int64_t steps) {
-    if (unit.empty()) return;
-    const int x = static_cast<int>(std::min_element(load, load + 8) - load);
-    of_xcd[x].insert(of_xcd[x].end(), unit.begin(), unit.end());
-    load[x] += steps * static_cast<int64_t>(unit.size() / kGroup);
-  };
-  for (int32_t i = 0; i < n_items; ++i) {
-    alone.clear();
-    units.clear();
-    int64_t longest_alone = 0, longest = 0;
-    each_set(i, [&](int32_t w, int32_t s, int64_t n) {
-      const bool together = all_together || n > most_alone;
-      const int64_t count = together ? pieces_of(n) : 1;
-      if (count > 1) pl.walk_merges.insert(pl.walk_merges.end(), {i, w | s << 8, static_cast<int32_t>(rows), static_cast<int32_t>(count)});
-      if (together && count > static_cast<int64_t>(units.size())) units.resize(static_cast<size_t>(count));
-      for (int64_t p = 0; p < count; ++p) {
-        const int32_t end = p + 1 == count ? std::numeric_limits<int32_t>::max() : static_cast<int32_t>(n * (p + 1) / count);
-        std::vector<int32_t> *to = together ? &units[static_cast<size_t>(p)] : &alone;
-        const int32_t begin = static_cast<int32_t>(n * p / count), slot = count > 1 ? static_cast<int32_t>(rows) : -1;
-        for (int k = together ? 4 : 1; k > 0; --k) to->insert(to->end(), {i, w | s << 8, begin, end, slot, together, 0, 0});
-        if (count > 1) rows += 16 * tiles;
+  std::vector<int32_t> of_xcd[8];
+  for (int level = 0; level < 3; ++level) {
+    std::vector<Unit> units;
+    std::vector<int32_t> unit_of;  // of the sets kept together: by piece + 1
+    for (size_t at = 0; at < made.size(); ++at) {
+      const Made &m = made[at];
+      if (at == 0 || m.root != made[at - 1].root || (level > 0 && m.g != made[at - 1].g) || (level > 1 && m.rb != made[at - 1].rb)) unit_of.clear();
+      if (m.piece + 1 >= static_cast<int32_t>(unit_of.size())) unit_of.resize(static_cast<size_t>(m.piece) + 2, -1);
+      int32_t &u = unit_of[static_cast<size_t>(m.piece + 1)];
+      if (u < 0) {
+        u = static_cast<int32_t>(units.size());
+        units.emplace_back();
       }
-      if (together)
-        longest = std::max(longest, (n / count + 3) / 4);
-      else
-        longest_alone = std::max(longest_alone, n);
-    });
-    fill(&alone);
-    place(alone, longest_alone + 2);
-    for (const std::vector<int32_t> &unit : units) place(unit, longest + 3);
+      for (int k = m.piece < 0 ? 1 : 4; k > 0; --k) units[u].recs.insert(units[u].recs.end(), m.rec, m.rec + Plan::kPieceInts);
+      units[u].steps += m.steps;
+    }
+    int64_t load[8] = {0}, all = 0;
+    for (std::vector<int32_t> &of : of_xcd) of.clear();
+    for (Unit &u : units) {
+      while (u.recs.size() % kGroup != 0) u.recs.insert(u.recs.end(), none.begin(), none.end());
+      const int x = static_cast<int>(std::min_element(load, load + 8) - load);
+      of_xcd[x].insert(of_xcd[x].end(), u.recs.begin(), u.recs.end());
+      load[x] += u.steps;
+      all += u.steps;
+    }
+    if (80 * *std::max_element(load, load + 8) <= 11 * all) break;
   }
   size_t most = 0;
   for (const std::vector<int32_t> &of : of_xcd) most = std::max(most, of.size());

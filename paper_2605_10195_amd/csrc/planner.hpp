@@ -178,7 +178,7 @@ class Planner {
   static float estimate_walk(const Plan &plan);
   bool walk_in_halves(const Plan &plan) const;
   bool walk_by_tile(const Plan &plan) const;
-  void build_pieces(Plan *plan) const;
+  void build_pieces(const std::vector<int32_t> &root_order, const std::vector<std::vector<int32_t>> &rbs_of_root, Plan *plan) const;
   std::vector<int32_t> multi_, last_pg_;
   std::vector<int32_t> stamp_, slot_;  // per-node scratch of build_walk, valid where stamp_ == current stamp
   // scratch of the request ordering in ensure_walk: pre-order rank and child ranges per node,
