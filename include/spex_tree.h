@@ -503,7 +503,8 @@ spex_status_t spex_tree_walk_dump(spex_tree_t *tree, const spex_node_t *leaves,
  * spex_tree_read_profile waits for those events and writes, for each recorded call in order,
  * milliseconds for ms[4*c+0] = the split path's launch or launches of shared and private items (the
  * generic kernels' likewise), ms[4*c+1] = 0, ms[4*c+2] = merge
- * kernel, ms[4*c+3] = tree-walk kernel (0 for a kernel that was not launched; cap counts calls,
+ * kernel, ms[4*c+3] = tree-walk kernel, for an MXFP4 pool with the merge of its pieces
+ * (0 for a kernel that was not launched; cap counts calls,
  * ms holds 4 * cap floats); *n = number of calls; the record is then
  * cleared.  SPEX_ERR_CAPACITY (with *n set) if cap calls are too few.  Enabling or disabling
  * profiling also clears the record.

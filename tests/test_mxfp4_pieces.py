@@ -113,3 +113,41 @@ def test_pieces_of_far_scores():
     f.check([0, 1], spread=8.0, loose=1e-4)
     assert f.tree.last_launch_info()["partial_rows"] > 0
     f.tree.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mode", [0, 2])
+@pytest.mark.parametrize("heads", [(80, 1, 64), (130, 2, 32), (65, 1, 256)])
+def test_groups_wider_than_a_wavefront_of_rows(heads, mode):
+    f = Forest(heads, [(-1, 200), (0, 33), (0, 1)], seed=heads[0], kernel_mode=mode)
+    f.check([1, 2])
+    f.check([1, 2, 0], [3, 1, 2])
+    f.tree.close()
+
+
+@pytest.mark.gpu
+def test_on_a_stream_of_its_own():
+    """Appends, attention in pieces and the reading back ordered by a stream that is not the default one, with work ahead of them."""
+    f = Forest((8, 2, 128), [(-1, 4000), (0, 20)], seed=7, spare=8)
+    x = [torch.as_tensor(f.rng.standard_normal((16, 2, 128))).to(torch.bfloat16) for _ in range(2)]
+    q = torch.as_tensor(f.rng.standard_normal((1, 8, 128))).to(torch.bfloat16)
+    side = torch.cuda.Stream()
+    busy = torch.randn(4096, 4096, device="cuda")
+    kd, vd, qd = torch.empty_like(x[0], device="cuda"), torch.empty_like(x[1], device="cuda"), torch.empty_like(q, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(8):
+            busy = busy @ busy * 1e-3
+        for dst, src in ((kd, x[0]), (vd, x[1]), (qd, q)):
+            dst.copy_(src.cuda())
+        f.tree.append_step(f.ids[1], kd, vd, quantize=True)
+        out, lse = f.tree.decode_attention([f.ids[1]], None, qd, 128 ** -0.5)
+        gk, gv = f.tree.read_back([f.ids[1]])
+    side.synchronize()
+    for i, w in enumerate("kv"):
+        old = (f.k, f.v)[i]
+        old[1] = np.concatenate([old[1], quantised(x[i].double().numpy(), w)])
+    assert np.array_equal(gk.cpu().double().numpy(), f.k[1]) and np.array_equal(gv.cpu().double().numpy(), f.v[1])
+    want, want_lse = f.check([1], q=q)
+    assert np.array_equal(out.cpu().double().numpy(), want) and np.array_equal(lse.cpu().double().numpy(), want_lse)
+    f.tree.close()
