@@ -489,7 +489,8 @@ constexpr int kWaves = 4;  // of a workgroup
 constexpr int kAlone = 16;
 
 // The blocks of one of the wavefronts that hold the same rows: every stride-th record of a list, 64 of them at a time in registers, a lane
-// each.  read(i, r): record i, for a lane; false where it does not concern the wavefront's rows.
+// each.  Read::fetch(i): record i as it lies in memory, for a lane; Read::make(raw, i, r): what it says, false where it does not concern the
+// wavefront's rows.
 struct MxLanes {
   int page[2], vp_a, vp_b, rows;
 };
@@ -506,23 +507,28 @@ struct MxSource {
   bool &left_out;
   uint64_t left;
   MxLanes r;
-  __device__ __forceinline__ MxBlock next() {
-    while (left == 0 && at < n) {
-      const int i = at + stride * static_cast<int>(threadIdx.x & 63);
-      bool concerns = i < n;
-      if (concerns) concerns = read(i, r);
-      const int lo = r.rows & 0xffff, hi = static_cast<int>(static_cast<uint32_t>(r.rows) >> 16);
-      if (NT > 1 && T1 - T0 == NT) {
-        const bool one = i >= alone && (lo >= row0 + 16 || hi <= row0 + 16);
-        left_out = left_out || __any(concerns && one);
-        concerns = concerns && !one;
-      } else if (NT > 1) {
-        concerns = concerns && (T0 == 0 ? hi <= row0 + 16 : lo >= row0 + 16);
-      }
-      if (lo > row0 + 16 * T0 || hi < min(row0 + 16 * T1, row_end)) r.vp_a |= kMasked;
-      left = __ballot(concerns);
-      at += 64 * stride;
+  __device__ __forceinline__ typename Read::Raw fetch() const {
+    const int i = at + stride * static_cast<int>(threadIdx.x & 63);
+    return i < n ? read.fetch(i) : typename Read::Raw{};
+  }
+  __device__ __forceinline__ void take(const typename Read::Raw &raw) {
+    const int i = at + stride * static_cast<int>(threadIdx.x & 63);
+    bool concerns = i < n;
+    if (concerns) concerns = read.make(raw, i, r);
+    const int lo = r.rows & 0xffff, hi = static_cast<int>(static_cast<uint32_t>(r.rows) >> 16);
+    if (NT > 1 && T1 - T0 == NT) {
+      const bool one = i >= alone && (lo >= row0 + 16 || hi <= row0 + 16);
+      left_out = left_out || __any(concerns && one);
+      concerns = concerns && !one;
+    } else if (NT > 1) {
+      concerns = concerns && (T0 == 0 ? hi <= row0 + 16 : lo >= row0 + 16);
     }
+    if (lo > row0 + 16 * T0 || hi < min(row0 + 16 * T1, row_end)) r.vp_a |= kMasked;
+    left = __ballot(concerns);
+    at += 64 * stride;
+  }
+  __device__ __forceinline__ MxBlock next() {
+    while (left == 0 && at < n) take(fetch());
     MxBlock b;
     b.live = left != 0;
     const int l = b.live ? __builtin_ctzll(left) : 0;
@@ -542,12 +548,14 @@ struct MxSource {
 // values one.  Otherwise a block at a time, the next one's keys and values requested where this one's have been used.
 template <int T0, int T1, bool TREE, bool OVERLAP, int M, int NT, class Read>
 __device__ __forceinline__ void walk_tiles(MxRows<M, NT> &st, const void *k, const void *v, int row0, int row_end, float c, int n, int first,
-                                           int stride, int alone, int g, int page_tiles, bool &left_out, Read read) {
+                                           int stride, int alone, int g, int page_tiles, bool &left_out, const Read &read,
+                                           const typename Read::Raw *raw) {
   const float slack = kSlackLog2 / c;
   MxSource<T0, T1, M, NT, Read> src{read, n, first, stride, alone, row0, row_end, g, page_tiles, left_out, 0, {}};
   MxKeys<M> k0;
   MxValues<M> v0;
   MxScores<NT> y0;
+  if (raw) src.take(*raw);
   MxBlock b0 = src.next();
   if (!b0.live) return;
   load_keys<M>(k0, b0, k);
@@ -590,22 +598,41 @@ __device__ __forceinline__ void walk_tiles(MxRows<M, NT> &st, const void *k, con
   }
 }
 // Of two tiles, blocks that concern one of them only have rounds of their own from record `alone` on: half the products and weights.
+// raw: the first 64 records, fetched before the rows were loaded.
 template <bool TREE, bool OVERLAP, int M, int NT, class Read>
 __device__ __forceinline__ void walk_blocks(MxRows<M, NT> &st, const void *k, const void *v, int row0, int row_end, float c, int n, int first,
-                                            int stride, int alone, int g, int page_tiles, Read read) {
+                                            int stride, int alone, int g, int page_tiles, const Read &read,
+                                            const typename Read::Raw &raw) {
   bool left_out = false;
-  walk_tiles<0, NT, TREE, OVERLAP>(st, k, v, row0, row_end, c, n, first, stride, alone, g, page_tiles, left_out, read);
+  walk_tiles<0, NT, TREE, OVERLAP>(st, k, v, row0, row_end, c, n, first, stride, alone, g, page_tiles, left_out, read, &raw);
   if constexpr (NT == 2) {
     if (!left_out) return;
     const int from = first >= alone ? first : first + (alone - first + stride - 1) / stride * stride;
-    walk_tiles<0, 1, TREE, OVERLAP>(st, k, v, row0, row_end, c, n, from, stride, alone, g, page_tiles, left_out, read);
-    walk_tiles<1, 2, TREE, OVERLAP>(st, k, v, row0, row_end, c, n, from, stride, alone, g, page_tiles, left_out, read);
+    walk_tiles<0, 1, TREE, OVERLAP>(st, k, v, row0, row_end, c, n, from, stride, alone, g, page_tiles, left_out, read, nullptr);
+    walk_tiles<1, 2, TREE, OVERLAP>(st, k, v, row0, row_end, c, n, from, stride, alone, g, page_tiles, left_out, read, nullptr);
   }
 }
 
 // With one row tile the registers go to more wavefronts instead, four a SIMD: 157 us for the 64 trees above, 177 with two that overlap, 165
 // with three that do not.  A second block of keys and values under way took three back and was no faster.
 constexpr bool mx_overlap(int blocks, int row_tiles) { return row_tiles == 2; }
+
+// Blocks of a split item: pairs of its pages' records {page, position << 7 | valid tokens}.
+struct SplitRecords {
+  struct Raw {
+    int2 a, b;
+  };
+  const int2 *pages;
+  int count;
+  bool masked;
+  int seen_end;
+  __device__ __forceinline__ Raw fetch(int i) const { return {pages[2 * i], pages[min(2 * i + 1, count - 1)]}; }
+  __device__ __forceinline__ bool make(const Raw &x, int i, MxLanes &r) const {
+    const bool has_b = 2 * i + 1 < count;
+    r = {{x.a.x, x.b.x}, x.a.y | (masked || !has_b ? kMasked : 0), has_b ? x.b.y : 0, static_cast<int>(0xffff0000u)};
+    return (x.a.y >> 7) < seen_end;
+  }
+};
 
 template <int M, int NT, bool TREE>
 __global__ __launch_bounds__(64 * kWaves, mx_occupancy(32 * M, NT)) void spex_mxfp4_split_kernel(AttnArgs p, Shape sh, SplitLists ls) {
@@ -618,17 +645,13 @@ __global__ __launch_bounds__(64 * kWaves, mx_occupancy(32 * M, NT)) void spex_mx
   if (cur.pg_count == 0 || cur.row0 >= rows) return;  // whole workgroup: padding item, or no such tile
   const int w = uniform(threadIdx.x >> 6), g = cur.g;
   const float c = p.scale_log2;
+  const int n_blocks = (cur.pg_count + 1) >> 1, first = w + kWaves * static_cast<int>(threadIdx.x & 63);
+  SplitRecords records{reinterpret_cast<const int2 *>(p.pg_rec) + cur.pg_begin, cur.pg_count, (cur.flags & 1) != 0, 0};
+  const auto raw = first < n_blocks ? records.fetch(first) : SplitRecords::Raw{};
   MxRows<M, NT> st;
   load_rows<M, NT, TREE>(st, p.q, p.qt_rec, p.qt_mask, cur.qt_begin, cur.row0, rows, g, sh, c);
-  const int n_blocks = (cur.pg_count + 1) >> 1;
-  walk_blocks<TREE, mx_overlap(M, NT)>(st, p.k_pool, p.v_pool, 0, INT_MAX, c, n_blocks, w, kWaves, INT_MAX, g, sh.page_tiles, [&](int i, MxLanes &r) {
-    const int2 *pages = reinterpret_cast<const int2 *>(p.pg_rec) + cur.pg_begin + 2 * i;
-    const bool has_b = 2 * i + 1 < cur.pg_count;
-    const int2 a = pages[0], b = pages[has_b ? 1 : 0];
-    r = {{a.x, b.x}, a.y | ((cur.flags & 1) || !has_b ? kMasked : 0), has_b ? b.y : 0,
-         static_cast<int>(0xffff0000u)};
-    return (a.y >> 7) < st.seen_end;
-  });
+  records.seen_end = st.seen_end;
+  walk_blocks<TREE, mx_overlap(M, NT)>(st, p.k_pool, p.v_pool, 0, INT_MAX, c, n_blocks, w, kWaves, INT_MAX, g, sh.page_tiles, records, raw);
   join_rows<M, NT, kWaves>(st, w, c, lds, p.finish ? p.out : p.part_o, p.finish ? nullptr : p.part_ml, p.lse, [&](int nt, int row) {
     const int r = cur.row0 + 16 * nt + row;
     if (r >= rows) return static_cast<int64_t>(-1);
@@ -665,6 +688,28 @@ __device__ __forceinline__ MxSet load_set(const int32_t *items, int item, int pa
   return t;
 }
 
+// Blocks of a set: records {page a, position << 7 | valid tokens, page b, valid tokens or 0, rows, flags}, first the shared ones.
+struct WalkRecords {
+  struct Raw {
+    u32x4 a, b;
+  };
+  const u32x4 *blocks;
+  int shared_begin, n_shared, priv_less_shared, row0, row1, seen_end;
+  __device__ __forceinline__ Raw fetch(int i) const {
+    const u32x4 *rec = blocks + 2 * static_cast<int64_t>((i < n_shared ? shared_begin : priv_less_shared) + i);
+    return {rec[0], rec[1]};
+  }
+  __device__ __forceinline__ bool make(const Raw &x, int, MxLanes &r) const {
+    const int lo = static_cast<int>(x.b[0] & 0xffffu), hi = static_cast<int>(x.b[0] >> 16);
+    r.page[0] = static_cast<int>(x.a[0]);
+    r.page[1] = static_cast<int>(x.a[3] != 0 ? x.a[2] : x.a[0]);
+    r.vp_a = static_cast<int>(x.a[1]) | ((x.b[1] & 1) != 0 ? kMasked : 0);
+    r.vp_b = static_cast<int>(x.a[3]);
+    r.rows = static_cast<int>(x.b[0]);
+    return lo < row1 && hi > row0 && (r.vp_a >> 7) < seen_end;
+  }
+};
+
 // A workgroup of four pieces, a wavefront each, or of one whose blocks the four wavefronts take in turn (Planner::build_pieces).
 template <int M, int NT, bool TREE>
 __global__ __launch_bounds__(64 * kWaves, mx_occupancy(32 * M, NT)) void spex_mxfp4_walk_kernel(WalkArgs p, Shape sh, int nw, int ntw) {
@@ -678,24 +723,15 @@ __global__ __launch_bounds__(64 * kWaves, mx_occupancy(32 * M, NT)) void spex_mx
   const MxSet t = load_set<NT>(p.items, item, sload(p.pieces, pr + 1), nw, ntw, sh.G);
   const int G = sh.G;
   const float c = p.scale_log2;
+  const int stride = together ? kWaves : 1, first = begin + (together ? w : 0), n = min(end, t.n_shared + t.n_priv);
+  WalkRecords records{reinterpret_cast<const u32x4 *>(p.blocks), t.blk_begin, t.n_shared, t.priv_begin - t.n_shared, t.row0, t.row0 + 16 * NT, 0};
+  const int mine = first + stride * static_cast<int>(threadIdx.x & 63);
+  const auto raw = mine < n ? records.fetch(mine) : WalkRecords::Raw{};
   MxRows<M, NT> st;
   load_rows<M, NT, TREE>(st, p.q, p.qt_rec, p.qt_mask, t.qt_begin, t.row_base, t.rows, t.g, sh, c);
-  const int stride = together ? kWaves : 1;
-  walk_blocks<TREE, mx_overlap(M, NT)>(
-      st, p.k_pool, p.v_pool, t.row0, t.row0 + t.rows - t.row_base, c, min(end, t.n_shared + t.n_priv), begin + (together ? w : 0), stride,
-      t.n_priv >= kAlone * stride ? t.n_shared : INT_MAX, t.g, sh.page_tiles,
-      [&](int i, MxLanes &r) {
-        const u32x4 *rec =
-            reinterpret_cast<const u32x4 *>(p.blocks) + 2 * static_cast<int64_t>(i < t.n_shared ? t.blk_begin + i : t.priv_begin + i - t.n_shared);
-        const u32x4 a = rec[0], b = rec[1];
-        const int lo = static_cast<int>(b[0] & 0xffffu), hi = static_cast<int>(b[0] >> 16);
-        r.page[0] = static_cast<int>(a[0]);
-        r.page[1] = static_cast<int>(a[3] != 0 ? a[2] : a[0]);
-        r.vp_a = static_cast<int>(a[1]) | ((b[1] & 1) != 0 ? kMasked : 0);
-        r.vp_b = static_cast<int>(a[3]);
-        r.rows = static_cast<int>(b[0]);
-        return lo < t.row0 + 16 * NT && hi > t.row0 && (r.vp_a >> 7) < st.seen_end;
-      });
+  records.seen_end = st.seen_end;
+  walk_blocks<TREE, mx_overlap(M, NT)>(st, p.k_pool, p.v_pool, t.row0, t.row0 + t.rows - t.row_base, c, n, first, stride,
+                                       t.n_priv >= kAlone * stride ? t.n_shared : INT_MAX, t.g, sh.page_tiles, records, raw);
   const bool whole = slot < 0;
   float *dst = whole ? p.out : p.part_o, *ml = whole ? nullptr : p.part_ml;
   auto place = [&](int nt, int row) {
@@ -713,16 +749,13 @@ __global__ __launch_bounds__(64 * kWaves, mx_occupancy(32 * M, NT)) void spex_mx
 // in turn and are summed through LDS.  Up to 64 pieces: a lane holds the weight of one.
 template <int M, int NT>
 __global__ __launch_bounds__(256) void spex_mxfp4_merge_kernel(WalkArgs p, Shape sh, int nw, int ntw) {
-  constexpr int D = 32 * M, kLanes = D / 4, kGroups = 256 / kLanes, kBatch = (64 + kGroups - 1) / kGroups < 4 ? (64 + kGroups - 1) / kGroups : 4;
+  constexpr int D = 32 * M, kLanes = D / 4, kGroups = 256 / kLanes, kEach = (64 + kGroups - 1) / kGroups, kBatch = kEach < 8 ? kEach : 8;
   __shared__ __attribute__((aligned(16))) float lds[kGroups * D];
   const int tid = threadIdx.x, lane = tid & 63;
   const int merge = static_cast<int>(blockIdx.x) / (16 * NT), row = static_cast<int>(blockIdx.x) - merge * 16 * NT;
   const int item = sload(p.merges, 4 * static_cast<int64_t>(merge)), part = sload(p.merges, 4 * static_cast<int64_t>(merge) + 1);
   const int64_t slot = sload(p.merges, 4 * static_cast<int64_t>(merge) + 2);
   const int n = sload(p.merges, 4 * static_cast<int64_t>(merge) + 3);
-  const MxSet t = load_set<NT>(p.items, item, part, nw, ntw, sh.G);
-  const int r = t.row_base + row;
-  if (r >= t.rows) return;  // the whole workgroup
   f32x2 ml = {kNegInf, 0.f};
   if (lane < n) ml = *reinterpret_cast<const f32x2 *>(p.part_ml + 2 * (slot + static_cast<int64_t>(lane) * 16 * NT + row));
   const int group = tid / kLanes, d = (tid - group * kLanes) * 4;
@@ -734,6 +767,9 @@ __global__ __launch_bounds__(256) void spex_mxfp4_merge_kernel(WalkArgs p, Shape
     const int at = group + k * kGroups;
     x[k] = *reinterpret_cast<const f32x4 *>(src + (group < kGroups && at < n ? at : 0) * kStep);
   }
+  const MxSet t = load_set<NT>(p.items, item, part, nw, ntw, sh.G);  // behind the loads, which do not wait for it
+  const int r = t.row_base + row;
+  if (r >= t.rows) return;  // the whole workgroup; what it loaded is room of its set's states
   float m = ml[0];
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
