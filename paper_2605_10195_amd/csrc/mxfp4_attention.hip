@@ -51,11 +51,11 @@ constexpr float kFarLog2 = 4194304.f;
 // A block of 32 tokens: pages a and b, wave-uniform.
 struct MxBlock {
   int64_t at[2];   // where the pages' tiles begin in a pool
-  int vp_a, vp_b;  // position << 7 | kMasked | valid tokens; vp_b 0: no page b
+  int vp_a, vp_b;  // position << 7 | kMasked | kRowMasked | valid tokens; vp_b 0: no page b
   int rows;        // first row | (last row + 1) << 16 of the row block whose path holds it
   bool live;       // there is such a block
 };
-constexpr int kMasked = 64, kValid = 63;  // of page a: some row of the wavefront does not see all of the block
+constexpr int kMasked = 64, kRowMasked = 32, kValid = 31;  // of page a: some row sees a part of the block; some row is not on its path
 
 // The keys and the values of a block as they lie in memory.
 template <int M>
@@ -237,19 +237,29 @@ __device__ __forceinline__ void block_scores(MxScores<NT> &y, const MxRows<M, NT
 // Those that a row does not see become -inf.  row0: the wavefront's first row in the row block.
 template <int T0, int T1, bool TREE, int M, int NT>
 __device__ __forceinline__ void mask_block(MxScores<NT> &y, const MxRows<M, NT> &st, const MxBlock &b, int row0) {
-  if (!(b.vp_a & kMasked)) return;
-  const int lane = threadIdx.x & 63, jj = lane >> 4, lo = b.rows & 0xffff, hi = static_cast<int>(static_cast<uint32_t>(b.rows) >> 16);
+  if (!(b.vp_a & (kMasked | kRowMasked))) return;
+  const int lane = threadIdx.x & 63, jj = lane >> 4;
+  int lo = b.rows & 0xffff, hi = static_cast<int>(static_cast<uint32_t>(b.rows) >> 16), vp_a = b.vp_a, vp_b = b.vp_b;
+  asm volatile("" : "+s"(lo), "+s"(hi), "+s"(vp_a), "+s"(vp_b));  // nothing of this is computed ahead of the branch
 #pragma unroll
   for (int nt = T0; nt < T1; ++nt) {
     const int row = row0 + 16 * nt + (lane & 15);
-    uint32_t seen = seen_bits<TREE>(st.limit[nt], st.qidx[nt], st.dmask[nt], b.vp_a, 4 * jj) |
-                    seen_bits<TREE>(st.limit[nt], st.qidx[nt], st.dmask[nt], b.vp_b, 4 * jj) << 4;
-    if (row < lo || row >= hi) seen = 0;
+    const bool on_path = row >= lo && row < hi;
+    uint32_t keep[8];
+    if (vp_a & kMasked) {
+      uint32_t seen = seen_bits<TREE>(st.limit[nt], st.qidx[nt], st.dmask[nt], vp_a, 4 * jj) |
+                      seen_bits<TREE>(st.limit[nt], st.qidx[nt], st.dmask[nt], vp_b, 4 * jj) << 4;
+      if (!on_path) seen = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) keep[i] = static_cast<uint32_t>(static_cast<int32_t>(seen << (31 - i)) >> 31);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) keep[i] = on_path ? 0xffffffffu : 0u;
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t keep = static_cast<uint32_t>(static_cast<int32_t>(seen << (31 - i)) >> 31);
       const float score = y.s[nt][i >> 2][i & 3];  // a select here compiles to three instructions a score
-      y.s[nt][i >> 2][i & 3] = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, score) & keep) | (0xff800000u & ~keep));
+      y.s[nt][i >> 2][i & 3] = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, score) & keep[i]) | (0xff800000u & ~keep[i]));
     }
   }
 }
@@ -523,7 +533,7 @@ struct MxSource {
     } else if (NT > 1) {
       concerns = concerns && (T0 == 0 ? hi <= row0 + 16 : lo >= row0 + 16);
     }
-    if (lo > row0 + 16 * T0 || hi < min(row0 + 16 * T1, row_end)) r.vp_a |= kMasked;
+    if (lo > row0 + 16 * T0 || hi < min(row0 + 16 * T1, row_end)) r.vp_a |= kRowMasked;
     left = __ballot(concerns);
     at += 64 * stride;
   }
@@ -532,7 +542,7 @@ struct MxSource {
     MxBlock b;
     b.live = left != 0;
     const int l = b.live ? __builtin_ctzll(left) : 0;
-    const int none = b.live ? 0 : kMasked;  // a block that is not there is one of no rows
+    const int none = b.live ? 0 : kRowMasked;  // a block that is not there is one of no rows
     left &= left - 1;
 #pragma unroll
     for (int p = 0; p < 2; ++p) b.at[p] = tile_at<M>(__builtin_amdgcn_readlane(r.page[p], l), page_tiles, g);
