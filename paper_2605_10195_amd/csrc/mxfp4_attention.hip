@@ -245,21 +245,16 @@ __device__ __forceinline__ void mask_block(MxScores<NT> &y, const MxRows<M, NT> 
   for (int nt = T0; nt < T1; ++nt) {
     const int row = row0 + 16 * nt + (lane & 15);
     const bool on_path = row >= lo && row < hi;
-    uint32_t keep[8];
-    if (vp_a & kMasked) {
-      uint32_t seen = seen_bits<TREE>(st.limit[nt], st.qidx[nt], st.dmask[nt], vp_a, 4 * jj) |
-                      seen_bits<TREE>(st.limit[nt], st.qidx[nt], st.dmask[nt], vp_b, 4 * jj) << 4;
-      if (!on_path) seen = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) keep[i] = static_cast<uint32_t>(static_cast<int32_t>(seen << (31 - i)) >> 31);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) keep[i] = on_path ? 0xffffffffu : 0u;
-    }
+    uint32_t seen = 0xff;
+    if (vp_a & kMasked)
+      seen = seen_bits<TREE>(st.limit[nt], st.qidx[nt], st.dmask[nt], vp_a, 4 * jj) |
+             seen_bits<TREE>(st.limit[nt], st.qidx[nt], st.dmask[nt], vp_b, 4 * jj) << 4;
+    if (!on_path) seen = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
+      const uint32_t keep = static_cast<uint32_t>(static_cast<int32_t>(seen << (31 - i)) >> 31);
       const float score = y.s[nt][i >> 2][i & 3];  // a select here compiles to three instructions a score
-      y.s[nt][i >> 2][i & 3] = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, score) & keep[i]) | (0xff800000u & ~keep[i]));
+      y.s[nt][i >> 2][i & 3] = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, score) & keep) | (0xff800000u & ~keep));
     }
   }
 }

@@ -151,3 +151,21 @@ def test_on_a_stream_of_its_own():
     want, want_lse = f.check([1], q=q)
     assert np.array_equal(out.cpu().double().numpy(), want) and np.array_equal(lse.cpu().double().numpy(), want_lse)
     f.tree.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [(16, 2, 64), (32, 8, 128), (12, 4, 96)])
+def test_a_full_card_gives_the_same_bits_every_time(heads):
+    """As many wavefronts as run at a time, all of them working: every pass equals the first, which is right."""
+    f = Forest(heads, [(-1, 600 + 20 * i) for i in range(48)] + [(i, 1 + i % 40) for i in range(48)], seed=heads[2])
+    leaves = list(range(48, 96))
+    q = torch.as_tensor(f.rng.standard_normal((48, heads[0], heads[2])) * 2).to(torch.bfloat16)
+    want, want_lse = f.check(leaves, q=q)
+    ids, qd = [f.ids[u] for u in leaves], q.cuda()
+    first = None
+    for _ in range(30):
+        out, lse = f.tree.decode_attention(ids, None, qd, heads[2] ** -0.5)
+        first = first or (out, lse)
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+    assert np.array_equal(first[0].cpu().double().numpy(), want) and np.array_equal(first[1].cpu().double().numpy(), want_lse)
+    f.tree.close()
