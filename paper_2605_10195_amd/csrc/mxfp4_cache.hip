@@ -12,7 +12,10 @@
 // This is the conversion of the OCP microscaling formats.  E comes from amax's exponent bits, x 2^-E is exact, so the rounding to four
 // bits is the only one.  The bounds of the values' E keep code * 2^E an IEEE half without rounding, as which attention multiplies it.
 //
-// Bound: memory, and for steps of one token latency.
+// Bound: memory.  8763 tokens of 8 prompts (32 / 8 heads of 128, rotated keys written back) are appended in 53 to 57 us, 207 MB, 76 to 81 % of
+// a large copy's rate; 48000 tokens are read in 42 to 44, 249 MB, at more than that rate (the codes come out of the last-level cache).
+// Steps of one token: latency, 4.7 us for 16 nodes, of it 1.6 an empty launch, and 12.9 for 1024, whose records come over the bus.
+// Values are handled four tokens at a time, because a word of a tile holds four, keys by the token: their words do.
 #include <algorithm>
 #include <type_traits>
 
