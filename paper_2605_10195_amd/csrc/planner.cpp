@@ -1247,7 +1247,8 @@ void Planner::ensure_walk(const PageTable &pt, Plan *plan) {
 // MXFP4 pools: the workgroups of the walk.  A set of rows is 16 * mx_row_tiles() of a wavefront of the lists; it has the row block's
 // shared blocks and then the wavefront's private ones.  Four sets are a workgroup, a wavefront each, or the four wavefronts of one take a
 // set's blocks in turn (`together`), which is four times the workgroups and a quarter of their steps: whichever takes fewer steps in
-// all, with about two for a wavefront to start and one more for four to join.  Lists much longer than the others', or few of
+// all, with about two for a wavefront to start and one more for four to join.  Us alone / together: 3300 sets of 38 blocks 207 / 250, 2050 of
+// 142 171 / 195, 2080 of 40 45.6 / 39.9, 1860 of 8 17.5 / 24.0, 405 of 60 24.5 / 13.9.  Lists much longer than the others', or few of
 // them, are cut into pieces of about equal length, together too, whose states a second launch merges.
 // The last piece of a set ends where its list does, so that blocks started by appends fall to it.
 // Launch order: workgroups that read the same blocks go to one XCD, whose L2 they share, the one with the least work so far; the
@@ -1274,9 +1275,9 @@ void Planner::build_pieces(const std::vector<int32_t> &root_order, const std::ve
   }
   if (sets == 0) return;
   const int64_t resident = 256 * mx_occupancy(pool.head_dim, tiles), mean = (total + sets - 1) / sets;  // workgroups; blocks
-  const int64_t steps_alone = (sets + 4 * resident - 1) / (4 * resident) * (mean + 2);
-  const int64_t steps_together = (sets + resident - 1) / resident * ((mean + 3) / 4 + 3);
-  const bool all_together = steps_together <= steps_alone;
+  // steps of `n` workgroups of `each`: those of one if all run at a time, else their share of a slot and half a round until the last ends
+  auto steps = [&](int64_t n, int64_t each, int64_t body) { return n <= resident ? each : n * each / resident + body / 2; };
+  const bool all_together = steps(sets, (mean + 3) / 4 + 3, (mean + 3) / 4) <= steps((sets + 3) / 4, mean + 2, mean);
   int64_t length = std::max<int64_t>(kPieceBlocks, (total + resident - 1) / resident);
   const int64_t most_alone = 3 * std::max<int64_t>(kWholeBlocks, (total + 4 * resident - 1) / (4 * resident)) / 2;
   auto pieces_of = [&](int64_t blocks) -> int64_t {
@@ -1296,10 +1297,11 @@ void Planner::build_pieces(const std::vector<int32_t> &root_order, const std::ve
     }
   struct Made {
     int32_t root, g, rb, piece;  // piece: -1 for a wavefront's own set
+    int32_t rec[6];
     int64_t steps;
-    int32_t rec[Plan::kPieceInts];
   };
   std::vector<Made> made;
+  made.reserve(static_cast<size_t>(sets) + 64);
   int64_t rows = 0;
   for (int32_t r : root_order)
     for (int32_t g = 0; g < pl.num_kv_heads; ++g)
@@ -1313,55 +1315,59 @@ void Planner::build_pieces(const std::vector<int32_t> &root_order, const std::ve
           for (int64_t p = 0; p < count; ++p) {
             const int32_t begin = static_cast<int32_t>(n * p / count), slot = count > 1 ? static_cast<int32_t>(rows) : -1;
             const int32_t end = p + 1 == count ? std::numeric_limits<int32_t>::max() : static_cast<int32_t>(n * (p + 1) / count);
-            made.push_back({r, g, rb, together ? static_cast<int32_t>(p) : -1, together ? (n / count + 3) / 4 + 3 : (n + 5) / 4,
-                            {i, set, begin, end, slot, together, 0, 0}});
+            made.push_back({r, g, rb, together ? static_cast<int32_t>(p) : -1, {i, set, begin, end, slot, together},
+                            together ? (n / count + 3) / 4 + 3 : (n + 5) / 4});
             if (count > 1) rows += 16 * tiles;
           }
         });
       }
+  // Units of workgroups that stay together, and the XCD of each.
   struct Unit {
-    std::vector<int32_t> recs;
-    int64_t steps = 0;
+    int64_t steps;
+    int32_t recs, xcd, at;  // records, padded to whole workgroups; the first one's place among the XCD's
   };
-  const std::vector<int32_t> none = {-1, 0, 0, 0, -1, 0, 0, 0};
-  constexpr size_t kGroup = static_cast<size_t>(4) * Plan::kPieceInts;
-  std::vector<int32_t> of_xcd[8];
+  std::vector<Unit> units;
+  std::vector<int32_t> unit_of(made.size()), by_piece;  // by_piece: the present sets' units, by piece + 1
+  int32_t recs[8];
   for (int level = 0; level < 3; ++level) {
-    std::vector<Unit> units;
-    std::vector<int32_t> unit_of;  // of the sets kept together: by piece + 1
+    units.clear();
     for (size_t at = 0; at < made.size(); ++at) {
-      const Made &m = made[at];
-      const Made &before = made[at > 0 ? at - 1 : 0];
-      if (m.root != before.root || (level > 0 && m.g != before.g) || (level > 1 && m.rb != before.rb)) unit_of.clear();
-      if (m.piece + 1 >= static_cast<int32_t>(unit_of.size())) unit_of.resize(static_cast<size_t>(m.piece) + 2, -1);
-      int32_t &u = unit_of[static_cast<size_t>(m.piece + 1)];
-      if (u < 0) {
-        u = static_cast<int32_t>(units.size());
-        units.emplace_back();
+      const Made &m = made[at], &before = made[at > 0 ? at - 1 : 0];
+      if (m.root != before.root || (level > 0 && m.g != before.g) || (level > 1 && m.rb != before.rb)) by_piece.clear();
+      if (at == 0) by_piece.clear();
+      const size_t k = static_cast<size_t>(m.piece + 1);
+      if (k >= by_piece.size()) by_piece.resize(k + 1, -1);
+      if (by_piece[k] < 0) {
+        by_piece[k] = static_cast<int32_t>(units.size());
+        units.push_back({0, 0, 0, 0});
       }
-      for (int k = m.piece < 0 ? 1 : 4; k > 0; --k) units[u].recs.insert(units[u].recs.end(), m.rec, m.rec + Plan::kPieceInts);
-      units[u].steps += m.steps;
+      unit_of[at] = by_piece[k];
+      units[by_piece[k]].steps += m.steps;
+      units[by_piece[k]].recs += m.piece < 0 ? 1 : 4;
     }
     int64_t load[8] = {0}, all = 0;
-    for (std::vector<int32_t> &of : of_xcd) of.clear();
+    std::fill(recs, recs + 8, 0);
     for (Unit &u : units) {
-      while (u.recs.size() % kGroup != 0) u.recs.insert(u.recs.end(), none.begin(), none.end());
-      const int x = static_cast<int>(std::min_element(load, load + 8) - load);
-      of_xcd[x].insert(of_xcd[x].end(), u.recs.begin(), u.recs.end());
-      load[x] += u.steps;
+      u.recs = (u.recs + 3) / 4 * 4;
+      u.xcd = static_cast<int32_t>(std::min_element(load, load + 8) - load);
+      u.at = recs[u.xcd];
+      recs[u.xcd] += u.recs;
+      load[u.xcd] += u.steps;
       all += u.steps;
     }
     if (80 * *std::max_element(load, load + 8) <= 11 * all) break;
   }
-  size_t most = 0;
-  for (const std::vector<int32_t> &of : of_xcd) most = std::max(most, of.size());
-  for (size_t at = 0; at < most; at += kGroup)
-    for (const std::vector<int32_t> &of : of_xcd) {
-      if (at < of.size())
-        pl.walk_pieces.insert(pl.walk_pieces.end(), of.begin() + at, of.begin() + at + kGroup);
-      else
-        for (int32_t k = 0; k < 4; ++k) pl.walk_pieces.insert(pl.walk_pieces.end(), none.begin(), none.end());
+  const size_t groups_all = static_cast<size_t>(*std::max_element(recs, recs + 8)) / 4 * 8;  // workgroups, in turn of the XCDs
+  pl.walk_pieces.assign(groups_all * 4 * Plan::kPieceInts, 0);
+  for (size_t at = 0; at < pl.walk_pieces.size(); at += Plan::kPieceInts) pl.walk_pieces[at] = -1;
+  for (size_t at = 0; at < made.size(); ++at) {
+    const Made &m = made[at];
+    Unit &u = units[unit_of[at]];
+    for (int k = m.piece < 0 ? 1 : 4; k > 0; --k, ++u.at) {
+      const size_t place = (static_cast<size_t>(u.at / 4) * 8 + u.xcd) * 4 + u.at % 4;
+      std::copy(m.rec, m.rec + 6, &pl.walk_pieces[place * Plan::kPieceInts]);
     }
+  }
   pl.walk_partial_rows = rows;
 }
 
