@@ -720,7 +720,7 @@ struct WalkRecords {
 // A workgroup of four pieces, a wavefront each, or of one whose blocks the four wavefronts take in turn (Planner::build_pieces).
 // Measured, heads 32 / 8 / 128: 64 trees of 2500 tokens with 32 branches of 256 (474 MB) 150 us, 3.2 TB/s, 115 without the arithmetic; 32 trees
 // of 16 branches (137 MB) 27 us, 5.1 TB/s; 16 trees of 4 branches with 100 queries each 187 us, 600 TFLOP/s of the products that the
-// definition has, 900 with those of the second pieces; one document of 64000 tokens and 8 branches (71 MB) 24 us and 5 to merge.
+// definition has, 980 with those of the second pieces; one document of 64000 tokens and 8 branches (71 MB) 24 us and 5 to merge.
 template <int M, int NT, bool TREE>
 __global__ __launch_bounds__(64 * kWaves, mx_occupancy(32 * M, NT)) void spex_mxfp4_walk_kernel(WalkArgs p, Shape sh, int nw, int ntw) {
   constexpr int kOne = MxJoin<M, NT>::floats(1), kAll = MxJoin<M, NT>::floats(kWaves);
@@ -755,8 +755,8 @@ __global__ __launch_bounds__(64 * kWaves, mx_occupancy(32 * M, NT)) void spex_mx
     join_rows<M, NT, 1>(st, 0, c, lds + w * kOne, dst, ml, p.lse, place);
 }
 
-// Rows whose path was walked in pieces (256 rows of 63 pieces, 8 MB, 4.4 to 5.2 us, of it 1.6 an empty launch): a workgroup a row; threads of four dims each, in as many groups as fit, which take the pieces
-// in turn and are summed through LDS.  Up to 64 pieces: a lane holds the weight of one.
+// Rows whose path was walked in pieces (256 rows of 63 pieces, 8 MB: 4.4 to 5.2 us, of it 1.6 an empty launch): a workgroup a row; threads
+// of four dims each, in as many groups as fit, which take the pieces in turn and are summed through LDS.  Up to 64 pieces: a lane holds the weight of one.
 template <int M, int NT>
 __global__ __launch_bounds__(256) void spex_mxfp4_merge_kernel(WalkArgs p, Shape sh, int nw, int ntw) {
   constexpr int D = 32 * M, kLanes = D / 4, kGroups = 256 / kLanes, kEach = (64 + kGroups - 1) / kGroups, kBatch = kEach < 8 ? kEach : 8;
