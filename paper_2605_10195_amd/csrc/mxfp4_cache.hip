@@ -12,7 +12,7 @@
 // This is the conversion of the OCP microscaling formats.  E comes from amax's exponent bits, x 2^-E is exact, so the rounding to four
 // bits is the only one.  The bounds of the values' E keep code * 2^E an IEEE half without rounding, as which attention multiplies it.
 //
-// Bound: memory.  8763 tokens of 8 prompts (32 / 8 heads of 128, rotated keys written back) are appended in 53 to 57 us, 207 MB, 76 to 81 % of
+// Bound: memory.  8763 tokens of 8 prompts (32 / 8 heads of 128, rotated keys written back) are appended in 45 to 49 us, 207 MB, 88 to 96 % of
 // a large copy's rate; 48000 tokens are read in 42 to 44, 249 MB, at more than that rate (the codes come out of the last-level cache).
 // Steps of one token: latency, 4.7 us for 16 nodes, of it 1.6 an empty launch, and 12.9 for 1024, whose records come over the bus.
 // Values are handled four tokens at a time, because a word of a tile holds four, keys by the token: their words do.
@@ -267,6 +267,8 @@ __global__ __launch_bounds__(256) void spex_mxfp4_read_kernel(ReadBackArgs a, Sh
   }
 }
 
+// Ranges of kv heads that a page's work is cut into.
+int32_t parts_of(const Shape &sh, int32_t n_recs, int32_t workgroups) { return std::max(1, std::min(sh.Hkv, workgroups / n_recs)); }
 bool aligned16(const void *x) { return (reinterpret_cast<uintptr_t>(x) & 15) == 0; }
 
 // f(integral constant M)
@@ -294,7 +296,9 @@ hipError_t launch_mxfp4_append(const Shape &sh, const RotateArgs &args, const Ro
   bool wide = a.rotary_dim % (a.interleaved ? 8 : 16) == 0;
   for (const void *x : {a.q, a.k, a.v, static_cast<const void *>(a.q_out), static_cast<const void *>(a.k_out)}) wide = wide && aligned16(x);
   for (int64_t s : {a.q_stride, a.k_stride, a.v_stride, a.q_out_stride, a.k_out_stride}) wide = wide && s % 8 == 0;
-  a.parts = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(sh.Hkv, 1024 / a.n_recs)));
+  // Workgroups wanted.  Pages of 16 tokens (550 of 8 heads) take 57.8 us in 1024, 48.0 in 2048, 51.7 in 4096; single tokens (1024 of 4
+  // heads), where the record and the angles are most of a workgroup's time, 12.8 / 14.4 / 17.4.
+  a.parts = parts_of(sh, a.n_recs, a.most_tokens > 4 ? 2048 : 1024);
   const dim3 grid(static_cast<unsigned>(a.n_recs), static_cast<unsigned>(a.parts)), block(256);
   const size_t lds = static_cast<size_t>(a.most_tokens) * (a.rotary_dim / 2) * sizeof(float) * 2;
   return with_blocks(sh.D, [&](auto m) {
@@ -309,7 +313,7 @@ hipError_t launch_mxfp4_read(const Shape &sh, const ReadBackArgs &args, const Ro
   if (args.n_recs <= 0) return hipSuccess;
   ReadBackArgs a = args;
   const bool wide = aligned16(a.k_out) && aligned16(a.v_out);
-  a.parts = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(sh.Hkv, 1024 / a.n_recs)));
+  a.parts = parts_of(sh, a.n_recs, 2048);  // 550 pages of 8 heads 12.8 us in 1024, 10.5 in 2048, 11.2 in 4096; 1024 of 4 9.3 / 9.0 / 10.3
   const dim3 grid(static_cast<unsigned>(a.n_recs), static_cast<unsigned>(a.parts)), block(256);
   return with_blocks(sh.D, [&](auto m) {
     if (wide)
