@@ -313,7 +313,10 @@ hipError_t launch_mxfp4_read(const Shape &sh, const ReadBackArgs &args, const Ro
   if (args.n_recs <= 0) return hipSuccess;
   ReadBackArgs a = args;
   const bool wide = aligned16(a.k_out) && aligned16(a.v_out);
-  a.parts = parts_of(sh, a.n_recs, 2048);  // 550 pages of 8 heads 12.8 us in 1024, 10.5 in 2048, 11.2 in 4096; 1024 of 4 9.3 / 9.0 / 10.3
+  // 550 pages of 8 heads of 128 take 10.5 us in 2048 workgroups, 12.8 in 1024, 11.2 in 4096; 1024 of 4 9.0 / 9.3 / 10.3.  Many pages
+  // that are in no cache, us in one part / two: 8 heads of 128 79.1 / 72.0, 98.9 / 90.5, 75.6 / 67.0; 4 of 128 98.7 / 104.8, 4 of 96
+  // 51.7 / 53.3, 2 of 128 58.2 / 66.2, 2 of 64 32.8 / 41.8.
+  a.parts = std::max(sh.Hkv > 1 && sh.Hkv * sh.D >= 1024 ? 2 : 1, parts_of(sh, a.n_recs, 2048));
   const dim3 grid(static_cast<unsigned>(a.n_recs), static_cast<unsigned>(a.parts)), block(256);
   return with_blocks(sh.D, [&](auto m) {
     if (wide)
