@@ -151,7 +151,7 @@ __device__ __forceinline__ void load_rows(MxRows<M, NT> &st, const void *q, cons
     st.qtok[nt] = st.qidx[nt] = 0;
     st.dmask[nt] = 0;
     st.m[nt] = kMInit;
-    st.mc[nt] = kMInit * c - kWeightLog2;
+    st.mc[nt] = fmaxf(kMInit * c, -3.0e38f) - kWeightLog2;  // finite: a masked score less it stays -inf
     st.l[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 2 * M; ++i) st.o[nt][i] = f32x4{0.f, 0.f, 0.f, 0.f};

@@ -169,3 +169,26 @@ def test_a_full_card_gives_the_same_bits_every_time(heads):
         assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
     assert np.array_equal(first[0].cpu().double().numpy(), want) and np.array_equal(first[1].cpu().double().numpy(), want_lse)
     f.tree.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mode", [0, 2])
+@pytest.mark.parametrize("scale", [1e9, 1e25, 1e-35])
+def test_scales_far_from_one(scale, mode):
+    """Branches below an empty node, so that rows meet blocks that they do not see before any that they do.  A large scale leaves the
+    largest score's value, a small one the mean."""
+    f = Forest((4, 2, 64), [(-1, 0)] + [(0, 20 + 9 * i) for i in range(6)], seed=3, kernel_mode=mode)
+    q = torch.as_tensor(f.rng.standard_normal((6, 4, 64))).to(torch.bfloat16)
+    ids = f.ids[1:]
+    out, lse = f.tree.decode_attention(ids, None, q.cuda(), scale)
+    out, lse, q = out.cpu().double().numpy(), lse.cpu().double().numpy(), q.double().numpy()
+    for i in range(6):
+        k, v = f.path(i + 1)
+        for h in range(4):
+            scores = k[:, h // 2] @ q[i, h]
+            want = v[np.argmax(scores), h // 2] if scale > 1 else v[:, h // 2].mean(0)
+            # one weight of 2^7 and a division that gives 2^-7, or sums of equal weights: fp32 roundings of numbers up to 6 * 2
+            assert np.abs(out[i, h] - want).max() <= 64 * 2.0 ** -24 * 12
+            top = scale * scores.max() if scale > 1 else np.log(len(k))
+            assert abs(lse[i, h] - top) <= 2.0 ** -20 * abs(top) + 2.0 ** -20
+    f.tree.close()
