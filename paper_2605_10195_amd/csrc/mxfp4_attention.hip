@@ -48,6 +48,10 @@ constexpr int kEvenDims = static_cast<int>(0x88888888u), kOddDims = static_cast<
 // Scaled references from here on are not subtracted in scaled form: their rounding would shift weights by many units.
 constexpr float kFarLog2 = 4194304.f;
 
+// A reference as it is subtracted from scaled scores.  Finite: a row that has met no score keeps kMInit, whatever the scale, and a score that
+// it does not see has to stay -inf.
+__device__ __forceinline__ float scaled_reference(float m, float c) { return fmaxf(__builtin_fmaf(m, c, -kWeightLog2), -3.0e38f); }
+
 // A block of 32 tokens: pages a and b, wave-uniform.
 struct MxBlock {
   int64_t at[2];   // where the pages' tiles begin in a pool
@@ -151,7 +155,7 @@ __device__ __forceinline__ void load_rows(MxRows<M, NT> &st, const void *q, cons
     st.qtok[nt] = st.qidx[nt] = 0;
     st.dmask[nt] = 0;
     st.m[nt] = kMInit;
-    st.mc[nt] = fmaxf(kMInit * c, -3.0e38f) - kWeightLog2;  // finite: a masked score less it stays -inf
+    st.mc[nt] = scaled_reference(kMInit, c);
     st.l[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 2 * M; ++i) st.o[nt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -305,7 +309,7 @@ __device__ __forceinline__ void move_references(MxRows<M, NT> &st, MxScores<NT> 
       const float m_new = row_group_max(fmaxf(top[nt], st.m[nt]));
       const float alpha = fast_exp2((st.m[nt] - m_new) * c);
       st.m[nt] = m_new;
-      st.mc[nt] = __builtin_fmaf(m_new, c, -kWeightLog2);
+      st.mc[nt] = scaled_reference(m_new, c);
       st.far = st.far || __any(fabsf(st.mc[nt]) >= kFarLog2 && m_new != kMInit);
       f32x4 of_rows;  // the lane's accumulators are of four rows
 #pragma unroll
