@@ -946,6 +946,7 @@ static spex_status_t decode_attention_impl(spex_tree_t *t, const spex_node_t *le
   m.part_hstride = dp.part_hstride;
   m.part_o = part_o;
   m.part_ml = part_ml;
+  m.scale = mxfp4 ? a.scale_log2 : 1.f;
   m.out = out;
   m.lse = lse;
   // in phases the rows of suffixes in one piece are finished with the suffix

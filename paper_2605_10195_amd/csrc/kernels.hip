@@ -2285,13 +2285,13 @@ __global__ __launch_bounds__(kMergeThreads) void spex_lse_merge_kernel(MergeArgs
 #pragma unroll
       for (int k = 0; k < kMergeBatch; ++k) m_new = fmaxf(m_new, mj[k]);
       if (m_new == kNegInf) continue;  // nothing seen so far
-      const float fa = fast_exp2(m - m_new);
+      const float fa = fast_exp2((m - m_new) * a.scale);
       l *= fa;
 #pragma unroll
       for (int i = 0; i < VEC; ++i) acc[i] *= fa;
 #pragma unroll
       for (int k = 0; k < kMergeBatch; ++k) {
-        const float f = fast_exp2(mj[k] - m_new);
+        const float f = fast_exp2((mj[k] - m_new) * a.scale);
         l += lj[k] * f;
         if (lj[k] != 0.f) {
 #pragma unroll
@@ -2311,13 +2311,13 @@ __global__ __launch_bounds__(kMergeThreads) void spex_lse_merge_kernel(MergeArgs
     float m_all = m;
     for (int k = 1; k < slices; ++k) m_all = fmaxf(m_all, lds_ml[tid + k * dv][0]);
     const float m_safe = m_all == kNegInf ? 0.f : m_all;  // every score of the row is -inf: lse is -inf too
-    const float f0 = fast_exp2(m - m_safe);
+    const float f0 = fast_exp2((m - m_safe) * a.scale);
     l *= f0;
 #pragma unroll
     for (int i = 0; i < VEC; ++i) acc[i] *= f0;
     for (int k = 1; k < slices; ++k) {
       const int t = tid + k * dv;
-      const float f = fast_exp2(lds_ml[t][0] - m_safe);
+      const float f = fast_exp2((lds_ml[t][0] - m_safe) * a.scale);
       l += lds_ml[t][1] * f;
 #pragma unroll
       for (int i = 0; i < VEC; ++i) acc[i] += lds_o[t * VEC + i] * f;
@@ -2333,7 +2333,7 @@ __global__ __launch_bounds__(kMergeThreads) void spex_lse_merge_kernel(MergeArgs
 #pragma unroll
     for (int i = 0; i < VEC; ++i) out[i] = acc[i] * inv;
   }
-  if (a.lse && c == 0) a.lse[orow] = (m + __builtin_log2f(l)) * 0.6931471805599453f;
+  if (a.lse && c == 0) a.lse[orow] = __builtin_fmaf(m, a.scale, __builtin_log2f(l)) * 0.6931471805599453f;
 }
 
 // ---- append scatter / gather -----------------------------------------------------------------

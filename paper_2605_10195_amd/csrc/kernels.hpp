@@ -34,7 +34,7 @@ struct AttnArgs {
   const int32_t *pg_rec;  // 2 ints per page entry: {page id, path position << 7 | valid tokens}
   const int32_t *qt_rec;  // 2 ints per row-set entry: {query token, visible path length}
   float *part_o;   // [partial rows][D] unnormalised sum of exp2(x - m) * V
-  float *part_ml;  // [partial rows][2] = {m, l}: running maximum of x = score * log2(e), sum of exp2
+  float *part_ml;  // [partial rows][2] = {m, l}: running maximum of x = score * log2(e), sum of exp2(x - m); MXFP4 pools: m of the scores themselves
   // every row of the launch has one piece only: write finished rows to out / lse instead (not the
   // generic kernel)
   bool finish;
@@ -78,6 +78,7 @@ struct MergeArgs {
   const int32_t *rec;     // {base, hstride} of the query tokens' pieces, `stride` pairs each, base -1 behind the last one
   int32_t stride;
   const float *part_o, *part_ml;
+  float scale;            // of the references in part_ml: 1 where they are scaled (log2), MXFP4 pools keep them as scores
   float *out, *lse;
   const int32_t *qt_ids;  // query tokens to merge, or null for 0 .. n_qtok-1
   int32_t n_qtok;         // number of query tokens handled by the launch

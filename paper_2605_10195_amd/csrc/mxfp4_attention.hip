@@ -42,7 +42,7 @@ typedef f32x2 f32x2_out __attribute__((aligned(4)));
 constexpr float kMInit = -1.0e30f;
 // How far a score may exceed the reference before that moves, and the exponent of a weight at the reference: weights stay below 2^15,
 // fp16's largest, and the smallest fp16 step is 2^-31 of a row's largest weight at most.
-constexpr float kSlackLog2 = 8.f, kWeightLog2 = 7.f;
+constexpr float kSlackLog2 = 8.f, kWeightLog2 = 7.f, kWeightUnit = 1.f / 128.f;  // (2^-kWeightLog2)
 // Places of a sparse product's weights: 0 and 2, or 1 and 3, of every four.
 constexpr int kEvenDims = static_cast<int>(0x88888888u), kOddDims = static_cast<int>(0xddddddddu);
 // Scaled references from here on are not subtracted in scaled form: their rounding would shift weights by many units.
@@ -140,8 +140,15 @@ struct MxRows {
   f32x4 l[NT];                 // the weights' sums of rows 4 jj .. + 3, as a product with ones gives them
   float m[NT], mc[NT];         // reference as a score, and scaled less kWeightLog2
   int seen_end;                // path positions from here on no row sees (wave-uniform)
-  bool far;                    // wave-uniform: some reference is beyond kFarLog2
+  int far;                     // wave-uniform: bit nt, some reference of tile nt is beyond kFarLog2
 };
+
+// What a state's weights are subtracted is mc, as it is rounded, and not m c - kWeightLog2: by so much (log2) they are less than they would be.
+// Half a unit of mc, 2^-3 just below kFarLog2, which states with other references do not share.
+template <int M, int NT>
+__device__ __forceinline__ float rounded_off(const MxRows<M, NT> &st, int nt, float c) {
+  return (st.far >> nt & 1) != 0 || st.m[nt] == kMInit ? 0.f : -__builtin_fmaf(st.m[nt], c, -(st.mc[nt] + kWeightLog2));
+}
 
 template <int M, int NT, bool TREE>
 __device__ __forceinline__ void load_rows(MxRows<M, NT> &st, const void *q, const int32_t *qt_rec, const int32_t *qt_mask, int qt_begin,
@@ -180,14 +187,15 @@ __device__ __forceinline__ void load_rows(MxRows<M, NT> &st, const void *q, cons
 #pragma unroll
   for (int o = 8; o >= 1; o >>= 1) end = max(end, __shfl_xor(end, o));
   st.seen_end = uniform(end);
-  st.far = false;
+  st.far = 0;
 }
 
 // Which of the lane's four tokens of a page the row sees, as bits.
-template <bool TREE>
+template <bool TREE, bool REMAKE>
 __device__ __forceinline__ uint32_t seen_bits(int limit, int qidx, uint32_t dmask, int vp, int first) {
   const int valid = (vp & kValid) - first, pos = (vp >> 7) + first;
   if (TREE) {  // positions below base, and base + k for the set bits k of the mask
+    if (REMAKE) asm volatile("" : "+v"(dmask));  // the word below is made here and not kept in two registers for the whole path
     const int shift = pos - (limit - 1 - qidx) + 32;
     const uint64_t bits = (static_cast<uint64_t>(dmask) << 32) | 0xffffffffull;
     const uint32_t seen = shift <= 0 ? 0xfu : (shift >= 64 ? 0u : static_cast<uint32_t>(bits >> shift));
@@ -242,6 +250,9 @@ __device__ __forceinline__ void block_scores(MxScores<NT> &y, const MxRows<M, NT
 template <int T0, int T1, bool TREE, int M, int NT>
 __device__ __forceinline__ void mask_block(MxScores<NT> &y, const MxRows<M, NT> &st, const MxBlock &b, int row0) {
   if (!(b.vp_a & (kMasked | kRowMasked))) return;
+  // Two tiles of a head of 64 have no registers for their mask words, and spill.  (One tile of a head of 128 reloads its word where a block has
+  // masks, and spills queries if the word is remade.)
+  constexpr bool kRemake = NT == 2 && mx_occupancy(32 * M, NT) > 2;
   const int lane = threadIdx.x & 63, jj = lane >> 4;
   int lo = b.rows & 0xffff, hi = static_cast<int>(static_cast<uint32_t>(b.rows) >> 16), vp_a = b.vp_a, vp_b = b.vp_b;
   asm volatile("" : "+s"(lo), "+s"(hi), "+s"(vp_a), "+s"(vp_b));  // nothing of this is computed ahead of the branch
@@ -251,8 +262,8 @@ __device__ __forceinline__ void mask_block(MxScores<NT> &y, const MxRows<M, NT> 
     const bool on_path = row >= lo && row < hi;
     uint32_t seen = 0xff;
     if (vp_a & kMasked)
-      seen = seen_bits<TREE>(st.limit[nt], st.qidx[nt], st.dmask[nt], vp_a, 4 * jj) |
-             seen_bits<TREE>(st.limit[nt], st.qidx[nt], st.dmask[nt], vp_b, 4 * jj) << 4;
+      seen = seen_bits<TREE, kRemake>(st.limit[nt], st.qidx[nt], st.dmask[nt], vp_a, 4 * jj) |
+             seen_bits<TREE, kRemake>(st.limit[nt], st.qidx[nt], st.dmask[nt], vp_b, 4 * jj) << 4;
     if (!on_path) seen = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -307,10 +318,11 @@ __device__ __forceinline__ void move_references(MxRows<M, NT> &st, MxScores<NT> 
 #pragma unroll
     for (int nt = T0; nt < T1; ++nt) {
       const float m_new = row_group_max(fmaxf(top[nt], st.m[nt]));
-      const float alpha = fast_exp2((st.m[nt] - m_new) * c);
+      const float less = __builtin_fmaf(st.m[nt] - m_new, c, rounded_off(st, nt, c));
       st.m[nt] = m_new;
       st.mc[nt] = scaled_reference(m_new, c);
-      st.far = st.far || __any(fabsf(st.mc[nt]) >= kFarLog2 && m_new != kMInit);
+      st.far |= (__any(fabsf(st.mc[nt]) >= kFarLog2 && m_new != kMInit) ? 1 : 0) << nt;
+      const float alpha = fast_exp2(less - rounded_off(st, nt, c));
       f32x4 of_rows;  // the lane's accumulators are of four rows
 #pragma unroll
       for (int i = 0; i < 4; ++i) of_rows[i] = __shfl(alpha, 4 * (static_cast<int>(threadIdx.x & 63) >> 4) + i);
@@ -322,9 +334,11 @@ __device__ __forceinline__ void move_references(MxRows<M, NT> &st, MxScores<NT> 
   if (st.far) {
 #pragma unroll
     for (int nt = T0; nt < T1; ++nt) {
-      lower_by<!OVERLAP>(y.s[nt][0], st.m[nt]);
-      lower_by<!OVERLAP>(y.s[nt][1], st.m[nt]);
-      if (OVERLAP) st.mc[nt] = -kWeightLog2;
+      const bool far = (st.far >> nt & 1) != 0;
+      const float by = far ? st.m[nt] : 0.f;
+      lower_by<!OVERLAP>(y.s[nt][0], by);
+      lower_by<!OVERLAP>(y.s[nt][1], by);
+      if (OVERLAP) st.mc[nt] = far ? -kWeightLog2 : st.mc[nt];
     }
   }
 }
@@ -336,7 +350,7 @@ __device__ __forceinline__ void block_values(MxRows<M, NT> &st, const MxScores<N
 #pragma unroll
   for (int nt = T0; nt < T1; ++nt) {
     float w[8];
-    const float mc = !OVERLAP && st.far ? -kWeightLog2 : st.mc[nt];
+    const float mc = !OVERLAP && (st.far >> nt & 1) != 0 ? -kWeightLog2 : st.mc[nt];
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = fast_exp2(__builtin_fmaf(y.s[nt][i >> 2][i & 3], c, -mc));
     u32x4 h, rest;
@@ -399,20 +413,21 @@ template <int M, int NT>
 struct MxJoin {
   static constexpr int kRow = 32 * M + 4;  // the pad spreads rows over the banks
   static constexpr int kStage = 16 * kRow;
-  static constexpr int floats(int waves) { return waves * ((waves > 1 ? kStage : 0) + 2 * 16 * NT + 16) + 4 * 16; }
+  static constexpr int floats(int waves) { return waves * ((waves > 1 ? kStage : 0) + 3 * 16 * NT + 16) + 4 * 16; }
 };
 
 // Joins the states of the KS wavefronts (number ks of them calls) that hold the same rows, and writes the rows.  Several: called by all
-// of a workgroup together.  place(nt, row of the tile): the destination row or -1.
+// of a workgroup together.  place(nt, row of the tile): the destination row or -1.  ml (of several): the rows are partial states, weights
+// 2^(c (s - m)) with m a score, because of two far references only the difference may be scaled; else they are finished.
 template <int M, int NT, int KS, class Place>
 __device__ __forceinline__ void join_rows(MxRows<M, NT> &st, int ks, float c, float *area, float *dst, float *ml, float *lse, Place place) {
   constexpr int kRow = MxJoin<M, NT>::kRow, kStage = KS > 1 ? MxJoin<M, NT>::kStage : 0, D = 32 * M;
   constexpr int kRun = kMxRun<M> ? 2 * M : 2;  // dims of a lane that follow each other
   const int lane = threadIdx.x & 63, row = lane & 15, jj = lane >> 4;
   RowPlace *places = reinterpret_cast<RowPlace *>(area);
-  float *states = area + 4 * 16;  // [wavefront][m of all rows, l of all rows]
-  float *factors = states + KS * 2 * 16 * NT + 16 * ks;
-  float *stage = states + KS * (2 * 16 * NT + 16);
+  float *states = area + 4 * 16;  // [wavefront][m of all rows, l of all rows, what was rounded off m c]
+  float *factors = states + KS * 3 * 16 * NT + 16 * ks;
+  float *stage = states + KS * (3 * 16 * NT + 16);
   auto meet = [&]() {
     if (KS > 1) {
       __syncthreads();
@@ -423,8 +438,11 @@ __device__ __forceinline__ void join_rows(MxRows<M, NT> &st, int ks, float c, fl
   };
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    float *mine = states + ks * 2 * 16 * NT + 16 * nt;
-    if (jj == 0) mine[row] = st.m[nt];
+    float *mine = states + ks * 3 * 16 * NT + 16 * nt;
+    if (jj == 0) {
+      mine[row] = st.m[nt];
+      mine[2 * 16 * NT + row] = rounded_off(st, nt, c);
+    }
     if (row == 0) *reinterpret_cast<f32x4 *>(mine + 16 * NT + 4 * jj) = st.l[nt];
   }
   meet();
@@ -434,22 +452,27 @@ __device__ __forceinline__ void join_rows(MxRows<M, NT> &st, int ks, float c, fl
     float m = st.m[nt], l = of[16 * NT], factor = 1.f;
     if (KS > 1) {
 #pragma unroll
-      for (int k = 0; k < KS; ++k) m = fmaxf(m, of[k * 2 * 16 * NT]);
+      for (int k = 0; k < KS; ++k) m = fmaxf(m, of[3 * k * 16 * NT]);
+      auto weight = [&](int k) { return fast_exp2(__builtin_fmaf(of[3 * k * 16 * NT] - m, c, of[(3 * k + 2) * 16 * NT])); };
       l = 0.f;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) l += of[(2 * k + 1) * 16 * NT] * fast_exp2((of[k * 2 * 16 * NT] - m) * c);
-      factor = fast_exp2((st.m[nt] - m) * c);
+      for (int k = 0; k < KS; ++k) l += of[(3 * k + 1) * 16 * NT] * weight(k);
+      factor = weight(ks);
+      if (ml) {
+        l *= kWeightUnit;
+        factor *= kWeightUnit;
+      }
     }
     if (jj == 0) {
-      const float inv = ml ? 1.f : 1.f / l;
+      const float inv = KS > 1 && ml ? 1.f : 1.f / l;
       if (ks == 0) {
         const int64_t at = place(nt, row);
         places[row] = {at, inv};
         if (at >= 0) {
-          if (ml)
-            *reinterpret_cast<f32x2 *>(ml + 2 * at) = f32x2{__builtin_fmaf(m, c, -kWeightLog2), l};
+          if (KS > 1 && ml)
+            *reinterpret_cast<f32x2 *>(ml + 2 * at) = f32x2{m, l};
           else if (lse)
-            lse[at] = (__builtin_fmaf(m, c, -kWeightLog2) + __builtin_log2f(l)) * 0.6931471805599453f;
+            lse[at] = (__builtin_fmaf(m, c, -kWeightLog2) + (__builtin_log2f(l) + (KS > 1 ? 0.f : of[2 * 16 * NT]))) * 0.6931471805599453f;
         }
       }
       factors[row] = factor;
@@ -756,7 +779,7 @@ __global__ __launch_bounds__(64 * kWaves, mx_occupancy(32 * M, NT)) void spex_mx
   if (together)
     join_rows<M, NT, kWaves>(st, w, c, lds, dst, ml, p.lse, place);
   else
-    join_rows<M, NT, 1>(st, 0, c, lds + w * kOne, dst, ml, p.lse, place);
+    join_rows<M, NT, 1>(st, 0, c, lds + w * kOne, p.out, nullptr, p.lse, place);  // pieces are walked together
 }
 
 // Rows whose path was walked in pieces (256 rows of 63 pieces, 8 MB: 4.4 to 5.2 us, of it 1.6 an empty launch): a workgroup a row; threads
@@ -787,7 +810,7 @@ __global__ __launch_bounds__(256) void spex_mxfp4_merge_kernel(WalkArgs p, Shape
   float m = ml[0];
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  const float weight = fast_exp2(ml[0] - m);
+  const float weight = fast_exp2((ml[0] - m) * p.scale_log2);
   float l = weight * ml[1];
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) l += __shfl_xor(l, o);
@@ -813,7 +836,7 @@ __global__ __launch_bounds__(256) void spex_mxfp4_merge_kernel(WalkArgs p, Shape
   const int qtok = sload(p.qt_rec, 2 * (static_cast<int64_t>(t.qt_begin) + r / sh.G));
   const int64_t at = static_cast<int64_t>(qtok) * sh.Hq + t.g * sh.G + r % sh.G;
   *reinterpret_cast<f32x4_out *>(p.out + at * D + d) = o * (1.f / l);
-  if (tid == 0 && p.lse) p.lse[at] = (m + __builtin_log2f(l)) * 0.6931471805599453f;
+  if (tid == 0 && p.lse) p.lse[at] = __builtin_fmaf(m, p.scale_log2, __builtin_log2f(l)) * 0.6931471805599453f;
 }
 
 // f(integral constant M)
