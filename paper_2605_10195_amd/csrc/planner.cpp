@@ -143,6 +143,11 @@ Chunks choose_chunks(const std::vector<Run> &groups, const std::vector<Run> &suf
 // set kMostPieces at most.  A cut costs a second launch: paths of 60 to 90 blocks on 30 to 250 workgroups took 14 to 17 us whole and 15 to
 // 24 in pieces of 16.
 constexpr int64_t kWholeBlocks = 96, kPieceBlocks = 32, kMostPieces = 64;
+// So one set of rows of one kv head gets 64 workgroups however long its path is, where the split path cuts into as many as the card runs.
+// From so many blocks on, for each row tile of the set, the split path serves it.  One path, heads 4/1/128, us walk / split: 64000 tokens
+// 13 / 27, 500000 45 / 60, 700000 59 / 63, a million 79 / 68, two 164 / 132; two row tiles (32/1/128) a million 117 / 129, two 224 / 157; heads of
+// 64 a million 62 / 58; of 256, bound by the blocks' bytes in either, 121 / 124.  Two sets (8/2/128) 91 / 94 and 191 / 204, four 168 / 224 at 1.4 million.
+constexpr int64_t kCappedBlocks = 28672;
 
 struct Segment {
   std::vector<int32_t> ids, valid, pos;
@@ -758,9 +763,9 @@ bool Planner::prefers_walk(const PageTable &pt, Plan *plan) {
   Plan &pl = *plan;
   if (pl.route >= 0) return pl.route == 1;
   bool walk = false;
-  if (pool.mxfp4) {  // long paths go in pieces: the walk serves every shape that has lists
+  if (pool.mxfp4) {  // long paths go in pieces: the walk serves the shapes that have lists, but for a set on its own that runs out of pieces
     ensure_walk(pt, &pl);
-    walk = pl.walk_ok && (pl.req_masks.empty() || pl.walk_waves != 2);
+    walk = pl.walk_ok && !pl.walk_capped && (pl.req_masks.empty() || pl.walk_waves != 2);
     pl.route = walk ? 1 : 0;
     return walk;
   }
@@ -1274,6 +1279,7 @@ void Planner::build_pieces(const std::vector<int32_t> &root_order, const std::ve
     }
   }
   if (sets == 0) return;
+  pl.walk_capped = sets == 1 && pool.head_dim <= 128 && total >= kCappedBlocks * tiles;
   const int64_t resident = 256 * mx_occupancy(pool.head_dim, tiles), mean = (total + sets - 1) / sets;  // workgroups; blocks
   // steps of `n` workgroups of `each`: those of one if all run at a time, else their share of a slot and half a round until the last ends
   auto steps = [&](int64_t n, int64_t each, int64_t body) { return n <= resident ? each : n * each / resident + body / 2; };

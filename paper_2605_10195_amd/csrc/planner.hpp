@@ -122,6 +122,7 @@ struct Plan {
   static constexpr int kPieceInts = 8, kMergeInts = 4;
   std::vector<int32_t> walk_pieces, walk_merges;
   int64_t walk_partial_rows = 0;
+  bool walk_capped = false;  // one set of rows on a path that is too long for as many pieces as a set may have
   int32_t walk_real_items = 0;       // workgroups with work
   int32_t walk_max_item_blocks = 0;  // longest workgroup: shared blocks + most private blocks of a wavefront
   int64_t walk_tiles_touched = 0, walk_tiles_held = 0;  // row tiles a block's rows lie in / its wavefronts hold, over all blocks
