@@ -26,7 +26,7 @@ def test_rows_that_meet_no_score_at_first(scale, top, mode):
 class FarScores:
     """Scores 2^23 + 0 .. 6 times the scale: whole numbers in fp32 whatever the order of the sums."""
 
-    def __init__(self, nodes, **kw):
+    def __init__(self, nodes, heads=(8, 2, 128), **kw):
         def value(rng, shape):
             if self.of_values:
                 x = rng.standard_normal(shape)
@@ -40,23 +40,27 @@ class FarScores:
             return x
 
         self.of_values = False
-        self.f = Forest((8, 2, 128), nodes, value=value, **kw)
+        self.f = Forest(heads, nodes, value=value, **kw)
 
-    def check(self, leaves, scale, q_lens=None):
+    def check(self, leaves, scale, q_lens=None, masks=None):
         f, lens = self.f, q_lens or [1] * len(leaves)
-        q = np.zeros((sum(lens), 8, 128))
+        q = np.zeros((sum(lens), f.hq, f.dim))
         q[..., 0] = 2.0 ** 11
         q[..., 32] = 1
-        out, lse = f.tree.decode_attention([f.ids[u] for u in leaves], q_lens, torch.as_tensor(q).to(torch.bfloat16).cuda(), scale)
+        out, lse = f.tree.decode_attention([f.ids[u] for u in leaves], q_lens, torch.as_tensor(q).to(torch.bfloat16).cuda(), scale, draft_masks=masks)
         out, lse = out.cpu().double().numpy(), lse.cpu().double().numpy()
         at = 0
         for u, n in zip(leaves, lens):
             k, v = f.path(u)
             see = np.arange(len(k))[None] <= len(k) - n + np.arange(n)[:, None]
-            for h in range(8):
-                o, z, mean, _ = attention(q[at:at + n, h], k[:, h // 4], v[:, h // 4], see, scale)
+            if masks is not None:
+                for j in range(n):
+                    see[j, len(k) - n:] = [(int(masks[at + j]) >> i) & 1 for i in range(n)]
+            for h in range(f.hq):
+                g = h // (f.hq // f.hkv)
+                o, z, mean, _ = attention(q[at:at + n, h], k[:, g], v[:, g], see, scale)
                 # differences of scores, up to 6 and exact, are what is scaled
-                assert (np.abs(out[at:at + n, h] - o) <= row_error(128, len(k), np.full(n, 6 * scale), mean)).all(), (u, h)
+                assert (np.abs(out[at:at + n, h] - o) <= row_error(f.dim, len(k), np.full(n, 6 * scale), mean)).all(), (u, h)
                 # a constant rounded twice, the scaled reference, a sum with a logarithm, another constant and its product
                 assert (np.abs(lse[at:at + n, h] - z) <= 6 * 2.0 ** -24 * np.abs(z) + 2.0 ** -15).all(), (u, h)
             at += n
@@ -95,4 +99,17 @@ def test_far_scores_of_many_short_paths(scale):
     """Enough sets of rows for a wavefront each."""
     x = FarScores([(-1, 10 + 7 * i % 190) for i in range(1400)], seed=35)
     x.check(list(range(1400)), scale)
+    x.f.tree.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mode", [2, 3])
+@pytest.mark.parametrize("tiles", [1, 2])
+@pytest.mark.parametrize("heads", [(16, 2, 64), (12, 4, 96), (3, 1, 160), (8, 2, 256)])
+@pytest.mark.parametrize("scale", [0.25, 1.0])
+def test_far_scores_of_other_heads(scale, heads, tiles, mode):
+    """Every shape of the kernels, chains and draft masks, paths in pieces beside short ones."""
+    x = FarScores([(-1, 4300), (0, 90), (0, 40), (-1, 300), (3, 33)], heads, seed=37, kernel_mode=mode, walk_row_tiles=tiles)
+    x.check([1, 2, 4], scale)
+    x.check([1, 4, 2], scale, [6, 2, 5], np.concatenate([1 << np.arange(n) | 1 for n in (6, 2, 5)]).astype(np.uint32))
     x.f.tree.close()
