@@ -310,7 +310,7 @@ spex_status_t spex_tree_prune(spex_tree_t *tree, spex_node_t node);
  *   tree-walk: one workgroup carries a block of up to 16 * walk_row_tiles * walk_waves query rows (requested
  *     nodes that are neighbours in the tree) from the root to the requested nodes; pages shared
  *     by rows of several wavefronts are fetched once per workgroup, the softmax state stays in
- *     registers, only the output is written.  Needs MFMA-tiled pools and Hq / Hkv <= 64 (one
+ *     registers, only the output is written.  Needs MFMA-tiled pools (MXFP4: below) and Hq / Hkv <= 64 (one
  *     query token's rows fit a wavefront; a requested node with more rows than a wavefront takes
  *     is cut into pieces of whole query tokens).  Chosen automatically when it yields >= 128
  *     workgroups, or when no wavefront has more two-page blocks to walk than 20 (up to 32
@@ -319,6 +319,11 @@ spex_status_t spex_tree_prune(spex_tree_t *tree, spex_node_t node);
  *     a plan is made and kept while appends are patched into it;
  *   shared-prefix + suffix + merge: every shared node is read once for all rows below it, private
  *     suffixes are split for parallelism, partial softmax states go through memory.  Any shape.
+ * MXFP4 pools have kernels of their own for both sets.  Their tree walk goes by sets of rows, those of one or two row tiles of a
+ * wavefront: four sets are a workgroup, or a set's path is taken by a whole workgroup or, if it is long, by up to 64, whose partial
+ * states go through the handle's workspace and are merged by a second launch.  It is chosen automatically wherever its lists exist
+ * (Hq / Hkv <= 64), unless one set of rows is all there is, head_dim is 128 or less and the path has 28672 two-page blocks or
+ * more for each row tile of the set.
  * Consecutive calls on one handle must use one stream or be separated by a synchronisation,
  * because they share the handle's workspace.  A call that repeats the previous request on an
  * unchanged tree (plan state 0, profiling off) only launches kernels -- no planning, allocation,
@@ -333,10 +338,10 @@ spex_status_t spex_tree_decode_attention(spex_tree_t *tree, const spex_node_t *l
  * For callers that cannot allocate device memory (code under HIP graph capture set-up, tight
  * serving loops, harnesses that forbid hipMalloc): spex_tree_decode_attention with the same
  * arguments, result and kernels, except that the call allocates nothing -- no hipMalloc, hipFree,
- * pinned host memory or event.  The launch lists and the partial softmax states of the
- * shared-prefix / suffix kernels go into a 64 MiB array that the library holds statically on every
- * GPU it runs on, from the load of its code object until the process ends (16 MiB for the lists,
- * 48 MiB for partial states), instead of the handle's grow-only workspace; the lists are copied
+ * pinned host memory or event.  The launch lists and the partial softmax states (of the
+ * shared-prefix / suffix kernels, and of paths that the MXFP4 walk cuts) go into a 64 MiB array that
+ * the library holds statically on every GPU it runs on, from the load of its code object until the
+ * process ends (16 MiB for the lists, 48 MiB for partial states), instead of the handle's grow-only workspace; the lists are copied
  * there from pageable host memory on every call, so nothing stays cached on the device between
  * calls and no plan state is shared with spex_tree_decode_attention's device copy (the host side
  * of the plan -- planning afresh, patching after appends -- is shared).  A request whose lists or
@@ -487,6 +492,7 @@ spex_status_t spex_tree_set_tuning(spex_tree_t *tree, int32_t prefix_chunk_pages
  *   items[S * n_items], S = 16 for NW = 4 and 32 for NW = 8: launch order, one workgroup each:
  *     {kv head, copy of row block fields 1.., zeros, row block index in the last int}; index -1 =
  *     padding that keeps the row blocks of one root on one XCD when fewer than 8 kv heads exist.
+ *     MXFP4 pools: what their workgroups are made of, not the launch order.
  */
 typedef struct {
   int32_t available, row_tiles, waves, n_row_blocks, n_blocks, n_qt, n_items;
@@ -518,13 +524,14 @@ spex_status_t spex_tree_read_profile(spex_tree_t *tree, float *ms, int32_t cap, 
  * [7] 0 = shared-prefix + suffix + merge kernels ran ([1] tokens in shared-prefix tasks, [2] tokens in
  * suffix tasks, [3] prefix work items, [4] suffix work items, [5] partial rows), else the tree-walk
  * kernel ran with [7] = row tiles per wavefront + 256 * wavefronts per workgroup ([3] workgroups
- * with work, [4] two-page blocks summed over workgroups of one kv head, [5] 0). */
+ * with work, [4] two-page blocks summed over workgroups of one kv head, [5] 0; MXFP4 pools: [3] and
+ * [4] of the lists' items, [5] rows of partial states, 0 if no path was cut). */
 spex_status_t spex_tree_last_launch_info(const spex_tree_t *tree, int64_t info[8]);
 
 /* How the split path runs the cached plan (made by plan_dump or a decode_attention call), for tests: -1 = the plan
  * has no lists of the split path; 0 = one launch, on MFMA-tiled pools with nodes of more than 16 query rows through LDS;
  * 1 = the same with one set of K and V registers; 2 = such nodes as row tiles, a workgroup each; 3 = launches
- * one after another. */
+ * one after another.  (MXFP4 pools: always one launch of their own kernel, whatever the form.) */
 spex_status_t spex_tree_split_form(const spex_tree_t *tree, int32_t *form);
 
 #ifdef __cplusplus

@@ -51,8 +51,9 @@ inline SplitForm split_form(const SplitSizes &s) {
 
 // MXFP4 pools: row tiles of 16 that a workgroup holds, of lists for `list_tiles`; wide heads have registers for one.
 constexpr int32_t mx_row_tiles(int32_t head_dim, int32_t list_tiles) { return list_tiles == 1 || head_dim > 128 ? 1 : 2; }
-// Workgroups of four wavefronts on a compute unit, what the registers allow.  (With one the compiler would keep accumulators in the
-// other half of the register file and move them for every block.)
+// Workgroups of four wavefronts on a compute unit: a bound on the registers.  (With one the compiler would keep accumulators in the
+// other half of the register file and move them for every block.)  One row tile of a head of 128 does not quite fit and spills three to
+// seven registers around its loop, where a block with draft masks reloads two; the others fit.
 constexpr int32_t mx_occupancy(int32_t head_dim, int32_t row_tiles) {
   return row_tiles == 1 ? (head_dim <= 128 ? 4 : (head_dim <= 160 ? 3 : 2)) : (head_dim <= 64 ? 3 : 2);
 }

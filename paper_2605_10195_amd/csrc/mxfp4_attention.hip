@@ -45,7 +45,8 @@ constexpr float kMInit = -1.0e30f;
 constexpr float kSlackLog2 = 8.f, kWeightLog2 = 7.f, kWeightUnit = 1.f / 128.f;  // (2^-kWeightLog2)
 // Places of a sparse product's weights: 0 and 2, or 1 and 3, of every four.
 constexpr int kEvenDims = static_cast<int>(0x88888888u), kOddDims = static_cast<int>(0xddddddddu);
-// Scaled references from here on are not subtracted in scaled form: their rounding would shift weights by many units.
+// From here on references are subtracted as scores.  Scaled ones are rounded by up to 2^-2 here, by 1 from 2^24 on, and all weights are off
+// by as much: more would take them out of fp16.
 constexpr float kFarLog2 = 4194304.f;
 
 // A reference as it is subtracted from scaled scores.  Finite: a row that has met no score keeps kMInit, whatever the scale, and a score that
@@ -143,8 +144,8 @@ struct MxRows {
   int far;                     // wave-uniform: bit nt, some reference of tile nt is beyond kFarLog2
 };
 
-// What a state's weights are subtracted is mc, as it is rounded, and not m c - kWeightLog2: by so much (log2) they are less than they would be.
-// Half a unit of mc, 2^-3 just below kFarLog2, which states with other references do not share.
+// A state's weights are 2^(c s - mc) with mc as it is rounded.  Log2 of how much less that is than 2^(c (s - m) + kWeightLog2): up to half a unit
+// of mc, 2^-3 just below kFarLog2, which states with other references do not share.  Joins make up for it.
 template <int M, int NT>
 __device__ __forceinline__ float rounded_off(const MxRows<M, NT> &st, int nt, float c) {
   return (st.far >> nt & 1) != 0 || st.m[nt] == kMInit ? 0.f : -__builtin_fmaf(st.m[nt], c, -(st.mc[nt] + kWeightLog2));
